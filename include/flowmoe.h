@@ -303,7 +303,14 @@ enum {
   FLOWMOE_K_ATTN_DGRAD = 21,      /* attention: dA = dI' W^O^T, dI = d[Q|K|V] [W^Q|W^K|W^V]^T */
   FLOWMOE_K_ATTN_BWD_DQ = 22,     /* attention backward: dQ and rowsum(dA * A) */
   FLOWMOE_K_ATTN_BWD_DKDV = 23,   /* attention backward: dK, dV */
-  FLOWMOE_K_ATTN_WGRAD = 24       /* attention: dW^O, d[W^Q | W^K | W^V] */
+  FLOWMOE_K_ATTN_WGRAD = 24,      /* attention: dW^O, d[W^Q | W^K | W^V] */
+  FLOWMOE_K_ROPE = 25,            /* rotary positions, either direction */
+  FLOWMOE_K_DIFF_FWD = 26,        /* differential attention */
+  FLOWMOE_K_DIFF_BWD_DQ = 27,     /* differential attention backward: dQ and the row sums */
+  FLOWMOE_K_DIFF_BWD_DKDV = 28,   /* differential attention backward: dK, dV */
+  FLOWMOE_K_DIFF_JOIN = 29,       /* differential attention backward: sums of partial results */
+  FLOWMOE_K_HEAD_NORM = 30,       /* head norm */
+  FLOWMOE_K_HEAD_NORM_BWD = 31    /* head norm backward */
 };
 
 /* Start tracing on the calling host thread: every later kernel launch whose
@@ -424,6 +431,148 @@ flowmoe_status_t flowmoe_mha_bwd(const flowmoe_shape_t* shape, const flowmoe_mha
                                  const void* d_out, void* d_attn, void* d_qkv, float* delta,
                                  void* d_in, float* dw_qkv, float* dw_o, int32_t accumulate,
                                  void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---- rotary positions ------------------------------------------------------- */
+
+/* Pairs of a head's columns turned by an angle that grows with the token's
+ * position (arXiv 2104.09864). Pair i of rot_dim / 2 turns by
+ *   phi = position * theta_i,  theta_i = base^(-2 i / rot_dim),
+ * scaled for contexts longer than those trained on:
+ *   NONE    as above
+ *   LINEAR  theta_i / factor (positions interpolated)
+ *   BASE    the base raised to base * factor^(rot_dim / (rot_dim - 2)), so that
+ *           the slowest pair is slowed down by factor (rot_dim > 2)
+ *   BANDS   by how often pair i turns over the original context (arXiv
+ *           2309.00071, Sec. 3.2): with r = orig_len theta_i / (2 pi) and
+ *           g = clamp((r - low) / (high - low), 0, 1), theta_i (g + (1 - g) / factor).
+ * Angles are computed in double. */
+enum { FLOWMOE_ROPE_HALF = 0, FLOWMOE_ROPE_PAIRS = 1 };
+enum {
+  FLOWMOE_ROPE_NONE = 0,
+  FLOWMOE_ROPE_LINEAR = 1,
+  FLOWMOE_ROPE_BASE = 2,
+  FLOWMOE_ROPE_BANDS = 3
+};
+typedef struct {
+  int32_t heads;    /* heads that turn, side by side from column 0: heads * head_dim <= M */
+  int32_t head_dim; /* a multiple of 8, 8..512 */
+  int32_t rot_dim;  /* columns of a head that turn, its first: even, 2..head_dim; the
+                       others are copied */
+  int32_t layout;   /* FLOWMOE_ROPE_HALF: columns i and i + rot_dim / 2 are a pair;
+                       FLOWMOE_ROPE_PAIRS: columns 2 i and 2 i + 1 */
+  int32_t scaling;  /* FLOWMOE_ROPE_NONE .. _BANDS */
+  int32_t seq_len;  /* without positions, token t stands at t % seq_len */
+  double base;      /* > 1 */
+  double factor;    /* LINEAR, BASE, BANDS: >= 1 */
+  double orig_len;  /* BANDS: the context trained on, in tokens (> 0) */
+  double low, high; /* BANDS: low < high turns */
+  double mscale;    /* of cosine and sine, so of every turned element (1: a rotation) */
+} flowmoe_rope_shape_t;
+
+/* y = x turned: for the pair (u, v) at angle phi,
+ *   (mscale (u cos phi - v sin phi), mscale (u sin phi + v cos phi)).
+ *   x, y      T x M layer dtype (shape->T, M, dtype; nothing else of shape is
+ *             used): rows of M elements of which the first heads * head_dim are
+ *             read and written; the others of y are left as they are. y may be x
+ *             (in place); else they must not overlap.
+ *   positions T int32, nullable (then t % seq_len); any value
+ * Q and K of qkv (T x 3M') turn in one call: M = 3 M', heads = 2 M' / head_dim. */
+flowmoe_status_t flowmoe_rope_fwd(const flowmoe_shape_t* shape, const flowmoe_rope_shape_t* rope,
+                                  const void* x, const int32_t* positions, void* y,
+                                  hipStream_t stream);
+
+/* Its gradient: dx = dy turned back (phi -> -phi), times mscale. dx may be dy. */
+flowmoe_status_t flowmoe_rope_bwd(const flowmoe_shape_t* shape, const flowmoe_rope_shape_t* rope,
+                                  const void* dy, const int32_t* positions, void* dx,
+                                  hipStream_t stream);
+
+/* ---- head norm --------------------------------------------------------------- */
+
+typedef struct {
+  int32_t heads;    /* M = heads * head_dim */
+  int32_t head_dim; /* a multiple of 8, 8..512 */
+  float eps;        /* > 0 */
+  float scale;      /* a constant factor (differential attention: 1 - lambda_init) */
+} flowmoe_norm_shape_t;
+
+/* RMS norm of each head's columns of a row:
+ *   y = scale * gain * x / sqrt(mean(x^2) + eps).
+ *   x, y  T x M layer dtype (y may be x); only shape->T, M and dtype are used
+ *   gain  head_dim float, nullable (ones), shared by the heads */
+flowmoe_status_t flowmoe_head_norm_fwd(const flowmoe_shape_t* shape,
+                                       const flowmoe_norm_shape_t* norm, const void* x,
+                                       const float* gain, void* y, hipStream_t stream);
+
+/* Bytes of scratch flowmoe_head_norm_bwd needs (0 for an invalid shape). */
+size_t flowmoe_head_norm_ws_bytes(const flowmoe_shape_t* shape, const flowmoe_norm_shape_t* norm);
+
+/* Its gradients, from x as the forward read it:
+ *   dx    T x M layer dtype (out; may be dy)
+ *   dgain head_dim float (out, nullable: not computed), summed over tokens and
+ *         heads; with accumulate != 0 added to
+ *   ws    flowmoe_head_norm_ws_bytes bytes, nullable without dgain */
+flowmoe_status_t flowmoe_head_norm_bwd(const flowmoe_shape_t* shape,
+                                       const flowmoe_norm_shape_t* norm, const void* x,
+                                       const float* gain, const void* dy, void* dx, float* dgain,
+                                       int32_t accumulate, void* ws, size_t ws_bytes,
+                                       hipStream_t stream);
+
+/* ---- differential attention --------------------------------------------------- */
+
+/* In the place of the softmax attention: head h takes the difference of two
+ * softmax maps with a learned weight (arXiv 2410.05258). shape->M = heads *
+ * head_dim; a head's head_dim query columns are [Q_1 | Q_2], its key columns
+ * [K_1 | K_2] (d = head_dim / 2 each), its value columns V (head_dim). kv_heads
+ * key/value heads are shared by heads / kv_heads query heads each (query head h
+ * reads key head h / (heads / kv_heads)). qkv rows hold W = M + 2 * kv_heads *
+ * head_dim elements, [Q | K | V]. bf16 only; 16-byte aligned; only shape->T, M
+ * and dtype are used. */
+typedef struct {
+  int32_t seq_len;  /* tokens per sequence; shape->T is a whole number of sequences */
+  int32_t heads;
+  int32_t kv_heads; /* divides heads */
+  int32_t head_dim; /* 64 or 128 (else FLOWMOE_ERR_UNSUPPORTED) */
+  int32_t causal;   /* 1: token i attends to tokens j <= i of its sequence */
+} flowmoe_diff_shape_t;
+
+/* Per sequence and head, over the tokens a row sees:
+ *   P_i = softmax(Q_i K_i^T / sqrt(d)), attn = P_1 V - lambda[h] P_2 V.
+ *   qkv    T x W (in)
+ *   lambda heads float (in)
+ *   lens   T / seq_len int32 (in, nullable: all seq_len): the valid tokens of each
+ *          sequence, from its first on (device data: cut to 0 .. seq_len). Later
+ *          tokens are seen by no row and may hold anything, NaN as well; their
+ *          rows of every output are zeros. A length of 0 leaves only such rows.
+ *   attn   T x M (out)
+ *   attn2  T x M (out, nullable): P_2 V, which the backward needs
+ *   lse    2 x heads x T float (out, nullable): the natural log of each map's
+ *          softmax denominator sum_j exp(s_ij), which the backward needs
+ * Probabilities are rounded to bf16 before they multiply V; sums in float. */
+flowmoe_status_t flowmoe_diff_attention_fwd(const flowmoe_shape_t* shape,
+                                            const flowmoe_diff_shape_t* diff, const void* qkv,
+                                            const float* lambda, const int32_t* lens, void* attn,
+                                            void* attn2, float* lse, hipStream_t stream);
+
+/* Bytes of scratch flowmoe_diff_attention_bwd needs (0 for an invalid shape). */
+size_t flowmoe_diff_attention_ws_bytes(const flowmoe_shape_t* shape,
+                                       const flowmoe_diff_shape_t* diff);
+
+/* Its gradients, from d_attn (T x M) and the forward's inputs, attn, attn2 and
+ * lse:
+ *   d_qkv    T x W (out); shared key/value heads get the sum over their group;
+ *            rows past a sequence's length are zeros
+ *   delta    2 x heads x T float (out): rowsum(d_attn_h * (P_i V)_h) of each map,
+ *            an intermediate (written, then read)
+ *   d_lambda heads float (out): -sum over tokens of delta's second map; with
+ *            accumulate != 0 added to
+ *   ws       flowmoe_diff_attention_ws_bytes bytes (nullable when that is 0) */
+flowmoe_status_t flowmoe_diff_attention_bwd(const flowmoe_shape_t* shape,
+                                            const flowmoe_diff_shape_t* diff, const void* qkv,
+                                            const float* lambda, const int32_t* lens,
+                                            const void* attn, const void* attn2, const float* lse,
+                                            const void* d_attn, void* d_qkv, float* delta,
+                                            float* d_lambda, int32_t accumulate, void* ws,
+                                            size_t ws_bytes, hipStream_t stream);
 
 /* ---- the R-chunk two-stream layer (Sec. 3.2, Eqs. 3-6) -------------------- */
 

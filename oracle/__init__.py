@@ -34,6 +34,9 @@ Pins (what each function is checked against, in tests/test_oracle_pins.py):
                   lse = log(number of visible tokens); one-token sequences
                   give I W^V W^O; non-causal attention is equivariant under
                   a permutation of a sequence's tokens
+  rope, head_norm(+bwd), diff_attention(+bwd)
+                  (differential attention block) complex rotations; central
+                  finite differences; a softmax written for one row
 No function here is pinned to values printed in the paper: the paper prints
 no numeric output of an MoE layer.
 """
@@ -43,3 +46,6 @@ from .moe_ref import (  # noqa: F401
     gelu, gelu_grad, silu, silu_grad, layer_chunk, layer_fwd_bwd,
 )
 from .mha_ref import attention, attention_bwd, mha_fwd, mha_bwd  # noqa: F401
+from .diff_ref import (  # noqa: F401
+    rope, rope_angles, head_norm, head_norm_bwd, diff_attention, diff_attention_bwd,
+)

@@ -41,6 +41,23 @@ class MhaShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("seq_len", "heads", "head_dim", "causal")]
 
 
+class RopeShape(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32)
+                 for n in ("heads", "head_dim", "rot_dim", "layout", "scaling", "seq_len")] +
+                [(n, ctypes.c_double)
+                 for n in ("base", "factor", "orig_len", "low", "high", "mscale")])
+
+
+class NormShape(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("scale", ctypes.c_float)]
+
+
+class DiffShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32)
+                for n in ("seq_len", "heads", "kv_heads", "head_dim", "causal")]
+
+
 _VP = ctypes.c_void_p
 _LAYER_FIELDS = [
     "w_gate", "bias", "w1", "w3", "w2", "b1", "b3", "b2",
@@ -76,6 +93,7 @@ def load():
     P, I32, SZ = _VP, ctypes.c_int32, ctypes.c_size_t
     SP = ctypes.POINTER(Shape)
     MP = ctypes.POINTER(MhaShape)
+    RP, NP, DP = (ctypes.POINTER(c) for c in (RopeShape, NormShape, DiffShape))
     sig = {
         "flowmoe_version": ([], ctypes.c_char_p),
         "flowmoe_last_error": ([], ctypes.c_char_p),
@@ -102,6 +120,14 @@ def load():
         "flowmoe_attention_bwd": ([SP, MP, P, P, P, P, P, P, P], I32),
         "flowmoe_mha_fwd": ([SP, MP, P, P, P, P, P, P, P, P], I32),
         "flowmoe_mha_bwd": ([SP, MP] + [P] * 13 + [I32, P, SZ, P], I32),
+        "flowmoe_rope_fwd": ([SP, RP, P, P, P, P], I32),
+        "flowmoe_rope_bwd": ([SP, RP, P, P, P, P], I32),
+        "flowmoe_head_norm_fwd": ([SP, NP, P, P, P, P], I32),
+        "flowmoe_head_norm_ws_bytes": ([SP, NP], SZ),
+        "flowmoe_head_norm_bwd": ([SP, NP] + [P] * 5 + [I32, P, SZ, P], I32),
+        "flowmoe_diff_attention_fwd": ([SP, DP] + [P] * 7, I32),
+        "flowmoe_diff_attention_ws_bytes": ([SP, DP], SZ),
+        "flowmoe_diff_attention_bwd": ([SP, DP] + [P] * 10 + [I32, P, SZ, P], I32),
         "flowmoe_layer_fwd": ([SP, I32, ctypes.POINTER(LayerBufs), P, P, P], I32),
         "flowmoe_layer_bwd": ([SP, I32, ctypes.POINTER(LayerBufs), P, P, P], I32),
     }
@@ -264,11 +290,79 @@ def flowmoe_mha_bwd(shape, mha, inp, w_qkv, w_o, qkv, attn, lse, d_out, d_attn, 
                                   int(accumulate), ptr(ws), int(ws_bytes), _stream(stream)))
 
 
+# ---- rotary positions, head norm, differential attention -----------------------------
+ROPE_LAYOUTS = {"half": 0, "pairs": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3}
+
+
+def make_rope_shape(heads, head_dim, rot_dim, seq_len, layout="half", base=10000.0,
+                    scaling="none", factor=1.0, orig_len=0.0, low=1.0, high=32.0,
+                    mscale=1.0) -> RopeShape:
+    return RopeShape(heads, head_dim, rot_dim,
+                     ROPE_LAYOUTS[layout] if isinstance(layout, str) else layout,
+                     ROPE_SCALINGS[scaling] if isinstance(scaling, str) else scaling,
+                     seq_len, base, factor, orig_len, low, high, mscale)
+
+
+def flowmoe_rope_fwd(shape, rope, x, positions, y, stream=None):
+    _check(load().flowmoe_rope_fwd(ctypes.byref(shape), ctypes.byref(rope), ptr(x), ptr(positions),
+                                   ptr(y), _stream(stream)))
+
+
+def flowmoe_rope_bwd(shape, rope, dy, positions, dx, stream=None):
+    _check(load().flowmoe_rope_bwd(ctypes.byref(shape), ctypes.byref(rope), ptr(dy), ptr(positions),
+                                   ptr(dx), _stream(stream)))
+
+
+def make_norm_shape(heads, head_dim, eps=1e-5, scale=1.0) -> NormShape:
+    return NormShape(heads, head_dim, eps, scale)
+
+
+def flowmoe_head_norm_fwd(shape, norm, x, gain, y, stream=None):
+    _check(load().flowmoe_head_norm_fwd(ctypes.byref(shape), ctypes.byref(norm), ptr(x), ptr(gain),
+                                        ptr(y), _stream(stream)))
+
+
+def flowmoe_head_norm_ws_bytes(shape, norm) -> int:
+    return load().flowmoe_head_norm_ws_bytes(ctypes.byref(shape), ctypes.byref(norm))
+
+
+def flowmoe_head_norm_bwd(shape, norm, x, gain, dy, dx, dgain, accumulate, ws=None, ws_bytes=0,
+                          stream=None):
+    _check(load().flowmoe_head_norm_bwd(ctypes.byref(shape), ctypes.byref(norm), ptr(x), ptr(gain),
+                                        ptr(dy), ptr(dx), ptr(dgain), int(accumulate), ptr(ws),
+                                        int(ws_bytes), _stream(stream)))
+
+
+def make_diff_shape(seq_len, heads, kv_heads, head_dim, causal) -> DiffShape:
+    return DiffShape(seq_len, heads, kv_heads, head_dim, int(bool(causal)))
+
+
+def flowmoe_diff_attention_fwd(shape, diff, qkv, lam, lens, attn, attn2, lse, stream=None):
+    _check(load().flowmoe_diff_attention_fwd(ctypes.byref(shape), ctypes.byref(diff), ptr(qkv),
+                                             ptr(lam), ptr(lens), ptr(attn), ptr(attn2), ptr(lse),
+                                             _stream(stream)))
+
+
+def flowmoe_diff_attention_ws_bytes(shape, diff) -> int:
+    return load().flowmoe_diff_attention_ws_bytes(ctypes.byref(shape), ctypes.byref(diff))
+
+
+def flowmoe_diff_attention_bwd(shape, diff, qkv, lam, lens, attn, attn2, lse, d_attn, d_qkv, delta,
+                               d_lambda, accumulate, ws=None, ws_bytes=0, stream=None):
+    _check(load().flowmoe_diff_attention_bwd(ctypes.byref(shape), ctypes.byref(diff), ptr(qkv),
+                                             ptr(lam), ptr(lens), ptr(attn), ptr(attn2), ptr(lse),
+                                             ptr(d_attn), ptr(d_qkv), ptr(delta), ptr(d_lambda),
+                                             int(accumulate), ptr(ws), int(ws_bytes),
+                                             _stream(stream)))
+
+
 # ---- kernel tracing --------------------------------------------------------------
 K_NAMES = ["gate", "route", "scan", "gather", "ffn1", "ffn2", "swiglu_act", "combine",
            "combine_bwd", "dgrad1", "wgrad2", "wgrad1", "dgrad2", "gate_bwd_wt", "gate_bwd_token",
            "gate_bwd_dw", "gate_bwd_reduce", "bias_grad", "attn_qkv", "attn_fwd", "attn_out",
-           "attn_dgrad", "attn_bwd_dq", "attn_bwd_dkdv", "attn_wgrad"]
+           "attn_dgrad", "attn_bwd_dq", "attn_bwd_dkdv", "attn_wgrad", "rope", "diff_fwd",
+           "diff_bwd_dq", "diff_bwd_dkdv", "diff_join", "head_norm", "head_norm_bwd"]
 K = {n: i for i, n in enumerate(K_NAMES)}
 K_GEMM = ("ffn1", "ffn2", "dgrad1", "wgrad2", "wgrad1", "dgrad2")
 

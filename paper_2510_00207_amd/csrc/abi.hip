@@ -698,6 +698,272 @@ flowmoe_status_t flowmoe_mha_bwd(const flowmoe_shape_t* shape, const flowmoe_mha
 
 }  // extern "C"
 
+// ---------------------------------------------------------------------------
+// rotary positions, head norm, differential attention
+// ---------------------------------------------------------------------------
+namespace {
+
+// T, M and dtype, all that these calls use of a shape
+flowmoe_status_t check_rows(const flowmoe_shape_t* s) {
+  if (s == nullptr) return fail(FLOWMOE_ERR_INVALID, "shape is null");
+  if (s->dtype != FLOWMOE_F32 && s->dtype != FLOWMOE_BF16)
+    return fail(FLOWMOE_ERR_INVALID, "dtype %d is not FLOWMOE_F32 or FLOWMOE_BF16", s->dtype);
+  if (s->T < 0) return fail(FLOWMOE_ERR_INVALID, "T = %d < 0", s->T);
+  if (s->M < 8 || s->M % 8)
+    return fail(FLOWMOE_ERR_INVALID, "M = %d must be a positive multiple of 8", s->M);
+  if ((long)s->T * s->M > (1L << 40) || s->M > (1 << 26))
+    return fail(FLOWMOE_ERR_UNSUPPORTED, "tensor too large");
+  return FLOWMOE_OK;
+}
+
+flowmoe_status_t check_head_dim(int32_t head_dim) {
+  if (head_dim < 8 || head_dim % 8)
+    return fail(FLOWMOE_ERR_INVALID, "head_dim = %d must be a positive multiple of 8", head_dim);
+  if (head_dim > 512) return fail(FLOWMOE_ERR_UNSUPPORTED, "head_dim = %d > 512", head_dim);
+  return FLOWMOE_OK;
+}
+
+flowmoe_status_t check_rope(const flowmoe_shape_t* s, const flowmoe_rope_shape_t* r,
+                            RopeShape* out) {
+  flowmoe_status_t st = check_rows(s);
+  if (st != FLOWMOE_OK) return st;
+  if (r == nullptr) return fail(FLOWMOE_ERR_INVALID, "rope is null");
+  st = check_head_dim(r->head_dim);
+  if (st != FLOWMOE_OK) return st;
+  if (r->heads < 1 || (long)r->heads * r->head_dim > s->M)
+    return fail(FLOWMOE_ERR_INVALID, "heads * head_dim = %d * %d is not in [1, M = %d]", r->heads,
+                r->head_dim, s->M);
+  if (r->rot_dim < 2 || r->rot_dim % 2 || r->rot_dim > r->head_dim)
+    return fail(FLOWMOE_ERR_INVALID, "rot_dim = %d must be even, in [2, head_dim = %d]", r->rot_dim,
+                r->head_dim);
+  if (r->layout != FLOWMOE_ROPE_HALF && r->layout != FLOWMOE_ROPE_PAIRS)
+    return fail(FLOWMOE_ERR_INVALID, "layout %d is not FLOWMOE_ROPE_HALF or FLOWMOE_ROPE_PAIRS",
+                r->layout);
+  if (r->scaling < FLOWMOE_ROPE_NONE || r->scaling > FLOWMOE_ROPE_BANDS)
+    return fail(FLOWMOE_ERR_INVALID, "scaling %d is not a FLOWMOE_ROPE_* scaling", r->scaling);
+  if (r->seq_len < 1) return fail(FLOWMOE_ERR_INVALID, "seq_len = %d < 1", r->seq_len);
+  if (!(r->base > 1.0) || !isfinite(r->base))
+    return fail(FLOWMOE_ERR_INVALID, "base = %g must be finite and > 1", r->base);
+  if (!isfinite(r->mscale)) return fail(FLOWMOE_ERR_INVALID, "mscale is not finite");
+  const bool bands = r->scaling == FLOWMOE_ROPE_BANDS;
+  if (r->scaling != FLOWMOE_ROPE_NONE && (!(r->factor >= 1.0) || !isfinite(r->factor)))
+    return fail(FLOWMOE_ERR_INVALID, "factor = %g must be finite and >= 1", r->factor);
+  if (r->scaling == FLOWMOE_ROPE_BASE && r->rot_dim == 2)
+    return fail(FLOWMOE_ERR_INVALID, "FLOWMOE_ROPE_BASE needs rot_dim > 2");
+  if (bands && (!(r->orig_len > 0.0) || !isfinite(r->orig_len)))
+    return fail(FLOWMOE_ERR_INVALID, "orig_len = %g must be finite and > 0", r->orig_len);
+  if (bands && (!(r->low < r->high) || !isfinite(r->low) || !isfinite(r->high)))
+    return fail(FLOWMOE_ERR_INVALID, "low = %g must be below high = %g", r->low, r->high);
+  RopeShape& o = *out;
+  o = RopeShape{};
+  o.heads = r->heads;
+  o.D = r->head_dim;
+  o.rot = r->rot_dim;
+  o.seq_len = r->seq_len;
+  o.half_layout = r->layout == FLOWMOE_ROPE_HALF;
+  o.bands = bands;
+  o.base = r->base;
+  if (r->scaling == FLOWMOE_ROPE_BASE)
+    o.base *= pow(r->factor, (double)r->rot_dim / (r->rot_dim - 2));
+  if (!isfinite(o.base)) return fail(FLOWMOE_ERR_INVALID, "base and factor are too large");
+  o.linear = r->scaling == FLOWMOE_ROPE_LINEAR ? 1.0 / r->factor : 1.0;
+  if (bands) {
+    o.inv_factor = 1.0 / r->factor;
+    o.orig = r->orig_len;
+    o.low = r->low;
+    o.high = r->high;
+  }
+  o.mscale = (float)r->mscale;
+  return FLOWMOE_OK;
+}
+
+flowmoe_status_t check_norm(const flowmoe_shape_t* s, const flowmoe_norm_shape_t* n,
+                            NormShape* out) {
+  flowmoe_status_t st = check_rows(s);
+  if (st != FLOWMOE_OK) return st;
+  if (n == nullptr) return fail(FLOWMOE_ERR_INVALID, "norm is null");
+  st = check_head_dim(n->head_dim);
+  if (st != FLOWMOE_OK) return st;
+  if (n->heads < 1 || (long)n->heads * n->head_dim != s->M)
+    return fail(FLOWMOE_ERR_INVALID, "heads * head_dim = %d * %d is not M = %d", n->heads,
+                n->head_dim, s->M);
+  if (!(n->eps > 0.0f) || !isfinite(n->eps))
+    return fail(FLOWMOE_ERR_INVALID, "eps = %g must be finite and > 0", n->eps);
+  if (!isfinite(n->scale)) return fail(FLOWMOE_ERR_INVALID, "scale is not finite");
+  *out = NormShape{n->heads, n->head_dim, n->eps, n->scale};
+  return FLOWMOE_OK;
+}
+
+flowmoe_status_t check_diff(const flowmoe_shape_t* s, const flowmoe_diff_shape_t* m,
+                            DiffShape* out) {
+  flowmoe_status_t st = check_rows(s);
+  if (st != FLOWMOE_OK) return st;
+  if (m == nullptr) return fail(FLOWMOE_ERR_INVALID, "diff is null");
+  if (s->dtype != FLOWMOE_BF16)
+    return fail(FLOWMOE_ERR_UNSUPPORTED, "the attention runs in FLOWMOE_BF16 only");
+  if (m->head_dim != 64 && m->head_dim != 128)
+    return fail(FLOWMOE_ERR_UNSUPPORTED, "head_dim = %d is not 64 or 128", m->head_dim);
+  if (m->heads < 1 || (long)m->heads * m->head_dim != s->M)
+    return fail(FLOWMOE_ERR_INVALID, "heads * head_dim = %d * %d is not M = %d", m->heads,
+                m->head_dim, s->M);
+  if (m->kv_heads < 1 || m->heads % m->kv_heads)
+    return fail(FLOWMOE_ERR_INVALID, "kv_heads = %d does not divide heads = %d", m->kv_heads,
+                m->heads);
+  if (m->seq_len < 1) return fail(FLOWMOE_ERR_INVALID, "seq_len = %d < 1", m->seq_len);
+  if (s->T % m->seq_len)
+    return fail(FLOWMOE_ERR_INVALID, "T = %d is not a whole number of sequences of %d tokens",
+                s->T, m->seq_len);
+  if (m->causal != 0 && m->causal != 1)
+    return fail(FLOWMOE_ERR_INVALID, "causal = %d is not 0 or 1", m->causal);
+  // (a tile's rows are reached by 32-bit byte offsets; a grid holds 2^32 threads)
+  if ((long)s->T * 3 * s->M > (1L << 40) || s->T > (1 << 30) || s->M > (1 << 22))
+    return fail(FLOWMOE_ERR_UNSUPPORTED, "tensor too large");
+  if (((m->seq_len + 127L) / 128) * m->heads * (s->T / m->seq_len) >= (1L << 32) / 512)
+    return fail(FLOWMOE_ERR_UNSUPPORTED, "too many attention tiles");
+  *out = DiffShape{m->seq_len, m->heads, m->kv_heads, m->head_dim, m->causal};
+  return FLOWMOE_OK;
+}
+
+// int32 or float data of the caller, nullable
+#define CHECK_A4(p, name)                                            \
+  if (reinterpret_cast<uintptr_t>(p) % 4 != 0)                       \
+    return fail(FLOWMOE_ERR_INVALID, "%s is not 4-byte aligned", name)
+
+flowmoe_status_t rope_call(const flowmoe_shape_t* shape, const flowmoe_rope_shape_t* rope,
+                           const void* x, const int32_t* positions, void* y, bool back,
+                           const char* names[3], hipStream_t stream) {
+  RopeShape r;
+  flowmoe_status_t st = check_rope(shape, rope, &r);
+  if (st != FLOWMOE_OK) return st;
+  if (shape->T == 0) return ok();
+  REQUIRE_T(x, names[0]);
+  REQUIRE_T(y, names[1]);
+  CHECK_A4(positions, "positions");
+  return hip_status(launch_rope(r, shape->dtype, shape->T, shape->M, back, x, positions, y, stream),
+                    names[2]);
+}
+
+}  // namespace
+
+extern "C" {
+
+flowmoe_status_t flowmoe_rope_fwd(const flowmoe_shape_t* shape, const flowmoe_rope_shape_t* rope,
+                                  const void* x, const int32_t* positions, void* y,
+                                  hipStream_t stream) {
+  const char* names[3] = {"x", "y", "flowmoe_rope_fwd"};
+  return rope_call(shape, rope, x, positions, y, false, names, stream);
+}
+
+flowmoe_status_t flowmoe_rope_bwd(const flowmoe_shape_t* shape, const flowmoe_rope_shape_t* rope,
+                                  const void* dy, const int32_t* positions, void* dx,
+                                  hipStream_t stream) {
+  const char* names[3] = {"dy", "dx", "flowmoe_rope_bwd"};
+  return rope_call(shape, rope, dy, positions, dx, true, names, stream);
+}
+
+flowmoe_status_t flowmoe_head_norm_fwd(const flowmoe_shape_t* shape,
+                                       const flowmoe_norm_shape_t* norm, const void* x,
+                                       const float* gain, void* y, hipStream_t stream) {
+  NormShape n;
+  flowmoe_status_t st = check_norm(shape, norm, &n);
+  if (st != FLOWMOE_OK) return st;
+  if (shape->T == 0) return ok();
+  REQUIRE_T(x, "x");
+  REQUIRE_T(y, "y");
+  CHECK_A4(gain, "gain");
+  return hip_status(launch_head_norm_fwd(n, shape->dtype, shape->T, x, gain, y, stream),
+                    "flowmoe_head_norm_fwd");
+}
+
+size_t flowmoe_head_norm_ws_bytes(const flowmoe_shape_t* shape, const flowmoe_norm_shape_t* norm) {
+  NormShape n;
+  if (check_norm(shape, norm, &n) != FLOWMOE_OK) return 0;
+  return head_norm_ws_bytes(shape->T, n.heads, n.D);
+}
+
+flowmoe_status_t flowmoe_head_norm_bwd(const flowmoe_shape_t* shape,
+                                       const flowmoe_norm_shape_t* norm, const void* x,
+                                       const float* gain, const void* dy, void* dx, float* dgain,
+                                       int32_t accumulate, void* ws, size_t ws_bytes,
+                                       hipStream_t stream) {
+  NormShape n;
+  flowmoe_status_t st = check_norm(shape, norm, &n);
+  if (st != FLOWMOE_OK) return st;
+  if (shape->T > 0) {
+    REQUIRE_T(x, "x");
+    REQUIRE_T(dy, "dy");
+    REQUIRE_T(dx, "dx");
+  }
+  CHECK_A4(gain, "gain");
+  CHECK_A4(dgain, "dgain");
+  if (dgain != nullptr) {
+    st = check_ws(ws, ws_bytes, head_norm_ws_bytes(shape->T, n.heads, n.D), "flowmoe_head_norm_bwd");
+    if (st != FLOWMOE_OK) return st;
+    CHECK_A4(ws, "ws");
+  }
+  return hip_status(launch_head_norm_bwd(n, shape->dtype, shape->T, x, gain, dy, dx, dgain,
+                                         accumulate != 0, ws, stream),
+                    "flowmoe_head_norm_bwd");
+}
+
+flowmoe_status_t flowmoe_diff_attention_fwd(const flowmoe_shape_t* shape,
+                                            const flowmoe_diff_shape_t* diff, const void* qkv,
+                                            const float* lambda, const int32_t* lens, void* attn,
+                                            void* attn2, float* lse, hipStream_t stream) {
+  DiffShape m;
+  flowmoe_status_t st = check_diff(shape, diff, &m);
+  if (st != FLOWMOE_OK) return st;
+  if (shape->T == 0) return ok();
+  REQUIRE_T(qkv, "qkv");
+  REQUIRE_F(lambda, "lambda");
+  CHECK_A4(lens, "lens");
+  REQUIRE_T(attn, "attn");
+  if (attn2 != nullptr) REQUIRE_T(attn2, "attn2");
+  CHECK_A4(lse, "lse");
+  return hip_status(launch_diff_attn_fwd(m, shape->T, qkv, lambda, lens, attn, attn2, lse, stream),
+                    "flowmoe_diff_attention_fwd");
+}
+
+size_t flowmoe_diff_attention_ws_bytes(const flowmoe_shape_t* shape,
+                                       const flowmoe_diff_shape_t* diff) {
+  DiffShape m;
+  if (check_diff(shape, diff, &m) != FLOWMOE_OK) return 0;
+  return diff_attn_ws_bytes(m, shape->T);
+}
+
+flowmoe_status_t flowmoe_diff_attention_bwd(const flowmoe_shape_t* shape,
+                                            const flowmoe_diff_shape_t* diff, const void* qkv,
+                                            const float* lambda, const int32_t* lens,
+                                            const void* attn, const void* attn2, const float* lse,
+                                            const void* d_attn, void* d_qkv, float* delta,
+                                            float* d_lambda, int32_t accumulate, void* ws,
+                                            size_t ws_bytes, hipStream_t stream) {
+  DiffShape m;
+  flowmoe_status_t st = check_diff(shape, diff, &m);
+  if (st != FLOWMOE_OK) return st;
+  REQUIRE_F(d_lambda, "d_lambda");
+  if (shape->T > 0) {
+    REQUIRE_T(qkv, "qkv");
+    REQUIRE_F(lambda, "lambda");
+    CHECK_A4(lens, "lens");
+    REQUIRE_T(attn, "attn");
+    REQUIRE_T(attn2, "attn2");
+    REQUIRE_F(lse, "lse");
+    REQUIRE_T(d_attn, "d_attn");
+    REQUIRE_T(d_qkv, "d_qkv");
+    REQUIRE_F(delta, "delta");
+  }
+  const size_t need = diff_attn_ws_bytes(m, shape->T);
+  st = check_ws(ws, ws_bytes, need, "flowmoe_diff_attention_bwd");
+  if (st != FLOWMOE_OK) return st;
+  if (need > 0) REQUIRE_T(ws, "ws");
+  return hip_status(launch_diff_attn_bwd(m, shape->T, qkv, lambda, lens, attn, attn2, lse, d_attn,
+                                         d_qkv, delta, d_lambda, accumulate != 0, ws, stream),
+                    "flowmoe_diff_attention_bwd");
+}
+
+}  // extern "C"
+
 namespace {
 
 struct Chunk {

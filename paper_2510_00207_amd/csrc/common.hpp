@@ -411,6 +411,43 @@ hipError_t launch_mha_wgrad(int T, int M, int R, const void* in, const void* att
                             const void* d_out, const void* d_qkv, float* dw_qkv, float* dw_o,
                             int accumulate, void* ws, hipStream_t st);
 
+// Differential attention: T tokens = T / N sequences of N, `heads` query heads and `kv`
+// key/value heads of width D (64 or 128), two maps of width D / 2 each, bf16
+struct DiffShape {
+  int N, heads, kv, D, causal;
+};
+size_t diff_attn_ws_bytes(const DiffShape& m, int T);
+// out2, lse: null where no backward follows
+hipError_t launch_diff_attn_fwd(const DiffShape& m, int T, const void* qkv, const float* lambda,
+                                const int32_t* lens, void* out, void* out2, float* lse,
+                                hipStream_t st);
+hipError_t launch_diff_attn_bwd(const DiffShape& m, int T, const void* qkv, const float* lambda,
+                                const int32_t* lens, const void* o, const void* o2,
+                                const float* lse, const void* d_o, void* d_qkv, float* delta,
+                                float* d_lambda, int accumulate, void* ws, hipStream_t st);
+// Rotary positions of the first heads * D columns of T rows of ld elements
+struct RopeShape {
+  int heads, D, rot, seq_len;
+  bool half_layout, bands;
+  double base;                         // after the `base` scaling
+  double linear;                       // the scale of every angle
+  double inv_factor, orig, low, high;  // bands
+  float mscale;
+};
+hipError_t launch_rope(const RopeShape& m, int dtype, int T, long ld, bool back, const void* x,
+                       const int32_t* pos, void* y, hipStream_t st);
+// RMS norm of each of a row's heads
+struct NormShape {
+  int heads, D;
+  float eps, scale;
+};
+size_t head_norm_ws_bytes(int T, int heads, int D);
+hipError_t launch_head_norm_fwd(const NormShape& m, int dtype, int T, const void* x,
+                                const float* gain, void* y, hipStream_t st);
+hipError_t launch_head_norm_bwd(const NormShape& m, int dtype, int T, const void* x,
+                                const float* gain, const void* dy, void* dx, float* dgain,
+                                int accumulate, void* ws, hipStream_t st);
+
 // Kernel tracing (flowmoe_trace_start): record a begin/end event around a
 // launch when the kind is selected. Defined in abi.hip.
 hipError_t trace_mark(int kind, bool end, hipStream_t st);

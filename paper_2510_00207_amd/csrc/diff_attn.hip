@@ -1,0 +1,620 @@
+// Differential attention (arXiv 2410.05258, Sec. 2.1) in the place of AT_r's softmax
+// attention: head h has two query/key pairs of width d = D / 2, one value of width D,
+// and a learned weight lambda_h,
+//   P_i = softmax(Q_i K_i^T / sqrt(d)),   A = P_1 V - lambda_h P_2 V.
+// Q_1 | Q_2 and K_1 | K_2 lie side by side in the head's D columns, so that a tile of
+// K rows in LDS holds both maps' keys: k steps 0 .. KS/2 - 1 of a row read are the
+// first map's, the others the second's. Query heads share key/value heads in groups.
+//
+// The tiles, operand forms and softmax are those of attn.hip. A padded batch gives
+// each sequence's number of valid tokens: later tokens are no one's keys, their
+// K, V, Q and dO rows are never used (tile loads past a sequence's length give
+// zeros, without traffic, so that whatever they hold cannot reach a sum), and their
+// outputs and gradients are zeros.
+//
+// Forward: blocks of 8 waves, two (one a map) for each 32 of 128 queries; each runs
+// the online softmax of its map and its own P_i V, and the second hands P_2 V to
+// the first through LDS at the end. P_2 V is kept for the backward as well.
+//
+// Backward (no atomics; every sum in a fixed order), with dP = dA V^T, which both
+// maps share, d2 = rowsum(dA * P_2 V) and d1 = rowsum(dA * A) + lambda d2:
+//   dS_1 = P_1 (dP - d1), dS_2 = -lambda P_2 (dP - d2),
+//   dQ_i = dS_i K_i / sqrt(d), dK_i = dS_i^T Q_i / sqrt(d),
+//   dV = (P_1 - lambda P_2)^T dA (one product), dlambda_h = -sum of d2 over the rows.
+// A key/value head's gradients are sums over the query heads of its group, in order.
+#include <math.h>
+
+#include "attn_tiles.hpp"
+#include "common.hpp"
+
+namespace flowmoe {
+namespace {
+
+struct DiffArgs {
+  const bf16_t* qkv;     // T x W = [Q | K | V], W = (heads + 2 kv) D
+  const float* lambda;   // heads
+  const int32_t* lens;   // valid tokens of each sequence, or null
+  const bf16_t* o;       // T x M: A (backward)
+  const bf16_t* o2;      // T x M: P_2 V (backward)
+  const bf16_t* d_o;     // T x M: dA (backward)
+  bf16_t* out;           // forward: A
+  bf16_t* out2;          // forward: P_2 V, or null
+  bf16_t* d_qkv;         // backward: T x W
+  float* lse;            // 2 x heads x T: log-sum-exp of each map's rows (forward: or null)
+  float* delta;          // 2 x heads x T: d1, d2
+  float* d_lambda;       // heads
+  int T, N, heads, kv, nseq;
+  int accumulate;        // add to d_lambda
+  long M, W;             // columns of a row of A, of qkv
+  float c2;              // log2(e) / sqrt(d)
+  float rs;              // 1 / sqrt(d)
+};
+
+// the valid tokens of sequence sq
+__device__ __forceinline__ int seq_end(const DiffArgs& a, int sq) {
+  return a.lens == nullptr ? a.N : min(max(a.lens[sq], 0), a.N);
+}
+
+// block -> (tile, head, sequence): tiles of the most causal work first (`rev`: the
+// last query tiles), all heads of a tile side by side
+__device__ __forceinline__ void diff_decode(const DiffArgs& a, int heads, bool rev, int rows,
+                                            int& tile, int& hd, int& sq) {
+  const int per = heads * a.nseq, nt = (a.N + rows - 1) / rows;
+  const int u = (int)(blockIdx.x / per), rest = (int)(blockIdx.x % per);
+  tile = rev ? nt - 1 - u : u;
+  hd = rest % heads;
+  sq = rest / heads;
+}
+
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(512, 2) void diff_fwd_kernel(DiffArgs a) {
+  constexpr int KS = D / 32, DB = D / 32, NW = 8, QB = 128;  // KS: k steps of one map
+  using Dma = TileDma<D, 64, NW>;
+  constexpr int TB = Dma::TB;
+  // K slots 0, 1, then V slots 0, 1; at the end P_2 V (float) of the 128 queries
+  __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
+  static_assert(4 * TB == QB * D * 4, "P_2 V fits the tiles' place");
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
+            h2 = lane >> 5, lq = lane & 31;
+  const int map = w & 1, grp = w >> 1;
+  int qt, hd, sq;
+  diff_decode(a, a.heads, CAUSAL, QB, qt, hd, sq);
+  const int end = seq_end(a, sq);
+  const long tok0 = (long)sq * a.N, ld = a.W;
+  const int kh = hd / (a.heads / a.kv);
+  const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
+  const bf16_t* Kg = a.qkv + tok0 * ld + a.M + (long)kh * D;
+  const bf16_t* Vg = Kg + (long)a.kv * D;
+  const int q0 = qt * QB, qw = q0 + 32 * grp + lq;
+  const long srow = ((long)map * a.heads + hd) * a.T + tok0 + qw;
+  bf16_t* Og = a.out + (tok0 + qw) * a.M + (long)hd * D;
+  bf16_t* O2g = a.out2 + (tok0 + qw) * a.M + (long)hd * D;
+
+  floatx16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = zero16();
+  if (q0 >= end) {  // padding only
+    if (qw < a.N) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        if (map == 0) store_cols(Og + 32 * db, o[db], h2, 0.0f);
+        else if (a.out2 != nullptr) store_cols(O2g + 32 * db, o[db], h2, 0.0f);
+      }
+      if (h2 == 0 && a.lse != nullptr) a.lse[srow] = 0.0f;
+    }
+    return;
+  }
+
+  const int kend = CAUSAL ? min(end, q0 + QB) : end;
+  const int nk = (kend + 63) / 64;
+  // (causal: a wave whose queries all precede a tile has nothing in it)
+  const int nkw = CAUSAL ? min(nk, (q0 + 32 * grp + 31) / 64 + 1) : nk;
+  const Dma dma(lds_base(lds), w, lane, ld);
+  const long kstep = 64 * ld;
+  dma.load(Kg, kend, 0);
+  dma.load(Vg, kend, 2 * TB);
+
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+    qf[ks] = qw < end ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * (KS * map + ks) + 8 * h2)
+                      : zero8();
+  float m = -INFINITY, l = 0.0f;
+  int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
+
+  auto step = [&](const int t, auto stc) {
+    constexpr int st = decltype(stc)::value;
+    opaque(rbase, tb0, tb1);
+    wait_vm<0>();   // K(t) and V(t): loaded a step ago
+    lds_barrier();  // and every wave's reads of the slots refilled now are done
+    const char* tk = lds + st * TB;
+    const char* tv = lds + (2 + st) * TB;
+    Kg += kstep;  // K(t + 1), V(t + 1)
+    Vg += kstep;
+    dma.load(Kg, kend - 64 * (t + 1), (st ^ 1) * TB);
+    dma.load(Vg, kend - 64 * (t + 1), (2 + (st ^ 1)) * TB);
+    if (t >= nkw) return;
+    floatx16 s[2];
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        s[u] = mfma(frag_row_x<D>(tk, rbase, 32 * u, KS * map + i), qf[i], i == 0 ? zero16() : s[u]);
+    const int kb0 = 64 * t;
+    if (kb0 + 64 > end || (CAUSAL && kb0 + 63 > q0 + 32 * grp)) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = kb0 + 32 * kb + 8 * (r >> 2) + 4 * h2 + (r & 3);
+          if (key >= end || (CAUSAL && key > qw)) s[kb][r] = -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+    // the reference moves only when a score exceeds it by more than 2^8 (attn.hip);
+    // every query sees key 0 in the first tile, so it is finite from then on
+    mx = pair_max(mx) * a.c2;
+    const bool up = mx > m + 8.0f;
+    if (__any(up)) {
+      const float mn = up ? mx : m;
+      const float al = exp2_fast(m - mn);
+      l *= al;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] *= al;
+      m = mn;
+    }
+    unsigned pw[16];  // the 32 probabilities of this lane, rounded to bf16 for the product
+    float rsum = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 32; q += 2) {
+      const float p0 = exp2_fast(fmaf(s[q >> 4][q & 15], a.c2, -m));
+      const float p1 = exp2_fast(fmaf(s[q >> 4][(q & 15) + 1], a.c2, -m));
+      rsum += p0;
+      rsum += p1;
+      pw[q >> 1] = pack_bf16x2(p0, p1);
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{pw[4 * g], pw[4 * g + 1], pw[4 * g + 2], pw[4 * g + 3]});
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] = mfma(frag_tr_x<D>(tv, tb0, tb1, 16 * g, 32 * db), pb, o[db]);
+    }
+    l += pair_sum(rsum);
+  };
+  for (int t = 0; t < nk; t += 2) {
+    step(t, Stage<0>{});
+    if (t + 1 < nk) step(t + 1, Stage<1>{});
+  }
+
+  // the second map's waves hand their rows to the first's, lane by lane
+  wait_vm<0>();  // (the loads past the last tile write zeros)
+  lds_barrier();
+  const float inv = qw < end ? 1.0f / l : 0.0f;
+  float4* xch = reinterpret_cast<float4*>(lds) + (long)grp * DB * 4 * 64 + lane;
+  if (map == 1) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      o[db] *= inv;
+#pragma unroll
+      for (int J = 0; J < 4; ++J)
+        xch[(4 * db + J) * 64] = make_float4(o[db][4 * J], o[db][4 * J + 1], o[db][4 * J + 2], o[db][4 * J + 3]);
+    }
+  }
+  lds_barrier();
+  if (qw < a.N) {
+    if (map == 0) {
+      const float lam = qw < end ? a.lambda[hd] : 0.0f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+#pragma unroll
+        for (int J = 0; J < 4; ++J) {
+          const float4 v = xch[(4 * db + J) * 64];
+          const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[db][4 * J + j] = o[db][4 * J + j] * inv - lam * x[j];
+        }
+        store_cols(Og + 32 * db, o[db], h2, 1.0f);
+      }
+    } else if (a.out2 != nullptr) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) store_cols(O2g + 32 * db, o[db], h2, 1.0f);
+    }
+    if (h2 == 0 && a.lse != nullptr) a.lse[srow] = qw < end ? (m + log2f(l)) * kLn2 : 0.0f;
+  }
+}
+
+// dQ, and d1 and d2: blocks of 4 waves of 32 queries over 32-key tiles, both maps in a
+// wave (they share dP)
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffArgs a) {
+  constexpr int KS = D / 16, DB = D / 32, NW = 4, QB = 32 * NW;
+  using Dma = TileDma<D, 32, NW>;
+  constexpr int TB = Dma::TB, VB = 2 * TB, GB = 4 * TB;  // K slots, V slots, the dO rows
+  __shared__ __attribute__((aligned(1024))) char lds[GB + QB * D * 2];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
+            h2 = lane >> 5, lq = lane & 31;
+  int qt, hd, sq;
+  diff_decode(a, a.heads, CAUSAL, QB, qt, hd, sq);
+  const int end = seq_end(a, sq);
+  const long tok0 = (long)sq * a.N, ld = a.W;
+  const int kh = hd / (a.heads / a.kv);
+  const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
+  const bf16_t* Kg = a.qkv + tok0 * ld + a.M + (long)kh * D;
+  const bf16_t* Vg = Kg + (long)a.kv * D;
+  const bf16_t* Gg = a.d_o + tok0 * a.M + (long)hd * D;
+  const bf16_t* Og = a.o + tok0 * a.M + (long)hd * D;
+  const bf16_t* O2g = a.o2 + tok0 * a.M + (long)hd * D;
+  const int q0 = qt * QB, qw = q0 + 32 * w + lq;
+  const bool live = qw < end;
+  const long srow = (long)hd * a.T + tok0 + qw, smap = (long)a.heads * a.T;
+  bf16_t* dst = a.d_qkv + (tok0 + qw) * ld + (long)hd * D;
+
+  floatx16 dq[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) dq[db] = zero16();
+  if (q0 >= end) {  // padding only
+    if (qw < a.N) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) store_cols(dst + 32 * db, dq[db], h2, 0.0f);
+      if (h2 == 0) a.delta[srow] = a.delta[srow + smap] = 0.0f;
+    }
+    return;
+  }
+  const int kend = CAUSAL ? min(end, q0 + QB) : end;
+  const int nk = (kend + 31) / 32;
+  const int nkw = CAUSAL ? min(nk, (q0 + 32 * w + 31) / 32 + 1) : nk;
+  const long kstep = 32 * ld;
+  const Dma dma(lds_base(lds), w, lane, ld);
+  {
+    const Dma dmag(lds_base(lds), w, lane, a.M);
+#pragma unroll
+    for (int i = 0; i < NW; ++i)
+      dmag.load(Gg + (long)(q0 + 32 * i) * a.M, end - q0 - 32 * i, GB + i * TB);
+  }
+  dma.load(Kg, kend, 0);
+  dma.load(Vg, kend, VB);
+  const float lam = a.lambda[hd];
+  bf16x8 qf[KS];
+  float d1 = 0.0f, d2 = 0.0f;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    const int c = 16 * ks + 8 * h2;
+    qf[ks] = live ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + c) : zero8();
+    const bf16x8 gv = live ? *reinterpret_cast<const bf16x8*>(Gg + (long)qw * a.M + c) : zero8();
+    const bf16x8 ov = live ? *reinterpret_cast<const bf16x8*>(Og + (long)qw * a.M + c) : zero8();
+    const bf16x8 pv = live ? *reinterpret_cast<const bf16x8*>(O2g + (long)qw * a.M + c) : zero8();
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      d1 += (float)gv[t] * (float)ov[t];
+      d2 += (float)gv[t] * (float)pv[t];
+    }
+  }
+  d1 = pair_sum(d1);
+  d2 = pair_sum(d2);
+  d1 += lam * d2;
+  if (qw < a.N && h2 == 0) {
+    a.delta[srow] = d1;
+    a.delta[srow + smap] = d2;
+  }
+  const float l1 = live ? a.lse[srow] * kLog2e : 0.0f, l2 = live ? a.lse[srow + smap] * kLog2e : 0.0f;
+  int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
+
+  auto step = [&](const int t, auto stc) {
+    constexpr int st = decltype(stc)::value;
+    opaque(rbase, tb0, tb1);
+    wait_vm<0>();
+    lds_barrier();
+    const char* tk = lds + st * TB;
+    const char* tv = lds + VB + st * TB;
+    Kg += kstep;
+    Vg += kstep;
+    dma.load(Kg, kend - 32 * (t + 1), (st ^ 1) * TB);
+    dma.load(Vg, kend - 32 * (t + 1), VB + (st ^ 1) * TB);
+    if (t >= nkw) return;
+    floatx16 s1, s2, dp;
+#pragma unroll
+    for (int i = 0; i < KS / 2; ++i) {
+      s1 = mfma(frag_row_x<D>(tk, rbase, 0, i), qf[i], i == 0 ? zero16() : s1);
+      s2 = mfma(frag_row_x<D>(tk, rbase, 0, KS / 2 + i), qf[KS / 2 + i], i == 0 ? zero16() : s2);
+    }
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+      dp = mfma(frag_row_x<D>(tv, rbase, 0, i), frag_row_x<D>(lds + GB, rbase, 32 * w, i),
+                i == 0 ? zero16() : dp);
+    const int kb0 = 32 * t;
+    if (kb0 + 32 > end || (CAUSAL && kb0 + 31 > q0 + 32 * w)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = kb0 + 8 * (r >> 2) + 4 * h2 + (r & 3);
+        if (key >= end || (CAUSAL && key > qw)) s1[r] = s2[r] = -INFINITY;
+      }
+    }
+    unsigned pw[2][8];  // dS^T of each map in this lane, rounded to bf16 for the product
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      float e[2], f[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        e[j] = exp2_fast(fmaf(s1[r + j], a.c2, -l1)) * (dp[r + j] - d1);
+        f[j] = exp2_fast(fmaf(s2[r + j], a.c2, -l2)) * (dp[r + j] - d2);
+      }
+      pw[0][r >> 1] = pack_bf16x2(e[0], e[1]);
+      pw[1][r >> 1] = pack_bf16x2(f[0], f[1]);  // (times -lambda at the end)
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const unsigned* p = pw[db >= DB / 2 ? 1 : 0] + 4 * g;
+        dq[db] = mfma(frag_tr_x<D>(tk, tb0, tb1, 16 * g, 32 * db),
+                      __builtin_bit_cast(bf16x8, u32x4{p[0], p[1], p[2], p[3]}), dq[db]);
+      }
+  };
+  for (int t = 0; t < nk; t += 2) {
+    step(t, Stage<0>{});
+    if (t + 1 < nk) step(t + 1, Stage<1>{});
+  }
+  if (qw < a.N) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      if (!live) dq[db] = zero16();
+      store_cols(dst + 32 * db, dq[db], h2, db >= DB / 2 ? -lam * a.rs : a.rs);
+    }
+  }
+}
+
+// dK and dV: blocks of 4 waves of 32 keys over the 32-query tiles of every query head of
+// the group
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffArgs a) {
+  constexpr int KS = D / 16, DB = D / 32, NW = 4, KB = 32 * NW;
+  using Dma = TileDma<D, 32, NW>;
+  constexpr int TQ = Dma::TB;          // one 32-row tile
+  constexpr int VT = 4 * TQ;           // two slots of Q and dO, then the block's V rows,
+  constexpr int ST = VT + KB * D * 2;  // then two slots of 32 x (lse 1, lse 2, d1, d2)
+  __shared__ __attribute__((aligned(1024))) char lds[ST + 2 * 512];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
+            h2 = lane >> 5, lq = lane & 31;
+  int kt, kh, sq;
+  diff_decode(a, a.kv, false, KB, kt, kh, sq);
+  const int end = seq_end(a, sq);
+  const long tok0 = (long)sq * a.N, ld = a.W;
+  const int group = a.heads / a.kv;
+  const int k0 = kt * KB, kw = k0 + 32 * w + lq;
+  const bool live = kw < end;
+  const long kcol = a.M + (long)kh * D, vcol = kcol + (long)a.kv * D;
+  bf16_t* dst = a.d_qkv + (tok0 + kw) * ld;
+  floatx16 dv[DB], dk[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    dv[db] = zero16();
+    dk[db] = zero16();
+  }
+  if (k0 < end) {
+    const bf16_t* rows = a.qkv + tok0 * ld;
+    const Dma dma(lds_base(lds), w, lane, ld), dmag(lds_base(lds), w, lane, a.M);
+#pragma unroll
+    for (int i = 0; i < NW; ++i)
+      dma.load(rows + vcol + (long)(k0 + 32 * i) * ld, end - k0 - 32 * i, VT + i * TQ);
+    bf16x8 kf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      kf[ks] = live ? *reinterpret_cast<const bf16x8*>(rows + kcol + kw * ld + 16 * ks + 8 * h2) : zero8();
+    // query steps of 32: causal keys k0.. are seen by queries >= k0 only
+    const int qs0 = CAUSAL ? k0 : 0;
+    const int nqs = (end - qs0 + 31) / 32;
+    int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
+
+    for (int gh = 0; gh < group; ++gh) {
+      const int hd = kh * group + gh;
+      const float lam = a.lambda[hd];
+      const bf16_t* Qt = rows + (long)hd * D + qs0 * ld;
+      const bf16_t* Gt = a.d_o + (tok0 + qs0) * a.M + (long)hd * D;
+      // the statistics of a step: 128 threads, one value each
+      float rstat = 0.0f;
+      const int which = (tid >> 5) & 3;
+      const float* sp = (which < 2 ? a.lse : a.delta) +
+                        ((long)(which & 1) * a.heads + hd) * a.T + tok0 + (tid & 31);
+      auto load_stat = [&](int qb) {
+        if (tid < 128) rstat = qb + (tid & 31) < end ? sp[qb] * (which < 2 ? kLog2e : 1.0f) : 0.0f;
+      };
+      auto store_stat = [&](int slot) {
+        if (tid < 128) reinterpret_cast<float*>(lds + ST + 512 * slot)[tid] = rstat;
+      };
+      if (gh > 0) {  // the last head's loads have landed and its reads are done
+        wait_vm<0>();
+        lds_barrier();
+      }
+      dma.load(Qt, end - qs0, 0);
+      dmag.load(Gt, end - qs0, TQ);
+      load_stat(qs0);
+      store_stat(0);
+
+      auto step = [&](const int it, auto stc) {
+        constexpr int st = decltype(stc)::value;
+        opaque(rbase, tb0, tb1);
+        const int qb = qs0 + 32 * it;
+        wait_vm<0>();   // this tile's loads
+        lds_barrier();  // and every wave's reads of the other slot are done
+        const char* tq = lds + st * 2 * TQ;
+        const char* tg = tq + TQ;
+        const float* stat = reinterpret_cast<const float*>(lds + ST + 512 * st);
+        Qt += 32 * ld;
+        Gt += 32 * a.M;
+        dma.load(Qt, end - qb - 32, (st ^ 1) * 2 * TQ);
+        dmag.load(Gt, end - qb - 32, (st ^ 1) * 2 * TQ + TQ);
+        if (it + 1 < nqs) load_stat(qb + 32);
+        if (!CAUSAL || qb + 31 >= k0 + 32 * w) {
+          floatx16 s1, s2, dp;
+#pragma unroll
+          for (int i = 0; i < KS; ++i)
+            dp = mfma(frag_row_x<D>(tg, rbase, 0, i), frag_row_x<D>(lds + VT, rbase, 32 * w, i),
+                      i == 0 ? zero16() : dp);
+#pragma unroll
+          for (int i = 0; i < KS / 2; ++i) {
+            s1 = mfma(frag_row_x<D>(tq, rbase, 0, i), kf[i], i == 0 ? zero16() : s1);
+            s2 = mfma(frag_row_x<D>(tq, rbase, 0, KS / 2 + i), kf[KS / 2 + i], i == 0 ? zero16() : s2);
+          }
+          if (qb + 32 > end || (CAUSAL && k0 + 32 * w + 31 > qb)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int q = qb + 8 * (r >> 2) + 4 * h2 + (r & 3);
+              if (q >= end || (CAUSAL && kw > q)) s1[r] = s2[r] = -INFINITY;
+            }
+          }
+          unsigned pp[8], pd[2][8];  // P_1 - lambda P_2 and dS of each map, bf16 pairs
+#pragma unroll
+          for (int J = 0; J < 4; ++J) {
+            float st4[4][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float4 v = *reinterpret_cast<const float4*>(stat + 32 * k + 8 * J + 4 * h2);
+              st4[k][0] = v.x; st4[k][1] = v.y; st4[k][2] = v.z; st4[k][3] = v.w;
+            }
+            float p[4], e[4], f[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int r = 4 * J + j;
+              const float p1 = exp2_fast(fmaf(s1[r], a.c2, -st4[0][j]));
+              const float p2 = lam * exp2_fast(fmaf(s2[r], a.c2, -st4[1][j]));
+              p[j] = p1 - p2;
+              e[j] = p1 * (dp[r] - st4[2][j]);
+              f[j] = p2 * (st4[3][j] - dp[r]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+              pp[2 * J + j / 2] = pack_bf16x2(p[j], p[j + 1]);
+              pd[0][2 * J + j / 2] = pack_bf16x2(e[j], e[j + 1]);
+              pd[1][2 * J + j / 2] = pack_bf16x2(f[j], f[j + 1]);
+            }
+          }
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+              const unsigned* d = pd[db >= DB / 2 ? 1 : 0] + 4 * g;
+              dv[db] = mfma(frag_tr_x<D>(tg, tb0, tb1, 16 * g, 32 * db),
+                            __builtin_bit_cast(bf16x8, u32x4{pp[4 * g], pp[4 * g + 1], pp[4 * g + 2], pp[4 * g + 3]}),
+                            dv[db]);
+              dk[db] = mfma(frag_tr_x<D>(tq, tb0, tb1, 16 * g, 32 * db),
+                            __builtin_bit_cast(bf16x8, u32x4{d[0], d[1], d[2], d[3]}), dk[db]);
+            }
+        }
+        if (it + 1 < nqs) store_stat(st ^ 1);
+      };
+      for (int it = 0; it < nqs; it += 2) {
+        step(it, Stage<0>{});
+        if (it + 1 < nqs) step(it + 1, Stage<1>{});
+      }
+    }
+  }
+  if (kw < a.N) {  // (rows past the end: their accumulators hold only masked zeros)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      if (!live) dk[db] = dv[db] = zero16();
+      store_cols(dst + kcol + 32 * db, dk[db], h2, a.rs);
+      store_cols(dst + vcol + 32 * db, dv[db], h2, 1.0f);
+    }
+  }
+}
+
+// dlambda_h = -sum of d2 over all rows: a block a head
+__global__ __launch_bounds__(1024) void diff_dlambda_kernel(DiffArgs a) {
+  __shared__ float part[16];
+  const float* d2 = a.delta + ((long)a.heads + blockIdx.x) * a.T;
+  float s = 0.0f;
+  for (int t = threadIdx.x; t < a.T; t += 1024) s += d2[t];
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) s += __shfl_xor(s, x);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0f;
+    for (int i = 0; i < 16; ++i) s += part[i];
+    a.d_lambda[blockIdx.x] = (a.accumulate ? a.d_lambda[blockIdx.x] : 0.0f) - s;
+  }
+}
+
+DiffArgs diff_args(const DiffShape& m, int T) {
+  DiffArgs a = {};
+  a.T = T;
+  a.N = m.N;
+  a.heads = m.heads;
+  a.kv = m.kv;
+  a.nseq = T / m.N;
+  a.M = (long)m.heads * m.D;
+  a.W = a.M + 2L * m.kv * m.D;
+  a.c2 = kLog2e / sqrtf((float)(m.D / 2));
+  a.rs = 1.0f / sqrtf((float)(m.D / 2));
+  return a;
+}
+
+#define FLOWMOE_DIFF_LAUNCH(KERNEL, blocks, threads)                                        \
+  do {                                                                                       \
+    const dim3 g((unsigned)(blocks)), b(threads);                                            \
+    if (m.D == 128) {                                                                        \
+      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true>), g, b, 0, st, a);                 \
+      else hipLaunchKernelGGL((KERNEL<128, false>), g, b, 0, st, a);                         \
+    } else {                                                                                 \
+      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true>), g, b, 0, st, a);                  \
+      else hipLaunchKernelGGL((KERNEL<64, false>), g, b, 0, st, a);                          \
+    }                                                                                        \
+  } while (0)
+
+long tiles(const DiffArgs& a, int heads) { return (long)((a.N + 127) / 128) * heads * a.nseq; }
+
+}  // namespace
+
+size_t diff_attn_ws_bytes(const DiffShape&, int) { return 0; }
+
+hipError_t launch_diff_attn_fwd(const DiffShape& m, int T, const void* qkv, const float* lambda,
+                                const int32_t* lens, void* out, void* out2, float* lse,
+                                hipStream_t st) {
+  if (T == 0) return hipSuccess;
+  DiffArgs a = diff_args(m, T);
+  a.qkv = static_cast<const bf16_t*>(qkv);
+  a.lambda = lambda;
+  a.lens = lens;
+  a.out = static_cast<bf16_t*>(out);
+  a.out2 = static_cast<bf16_t*>(out2);
+  a.lse = lse;
+  return traced(FLOWMOE_K_DIFF_FWD, st,
+                [&] { FLOWMOE_DIFF_LAUNCH(diff_fwd_kernel, tiles(a, a.heads), 512); });
+}
+
+hipError_t launch_diff_attn_bwd(const DiffShape& m, int T, const void* qkv, const float* lambda,
+                                const int32_t* lens, const void* o, const void* o2,
+                                const float* lse, const void* d_o, void* d_qkv, float* delta,
+                                float* d_lambda, int accumulate, void* ws, hipStream_t st) {
+  (void)ws;
+  DiffArgs a = diff_args(m, T);
+  a.qkv = static_cast<const bf16_t*>(qkv);
+  a.lambda = lambda;
+  a.lens = lens;
+  a.o = static_cast<const bf16_t*>(o);
+  a.o2 = static_cast<const bf16_t*>(o2);
+  a.d_o = static_cast<const bf16_t*>(d_o);
+  a.lse = const_cast<float*>(lse);
+  a.d_qkv = static_cast<bf16_t*>(d_qkv);
+  a.delta = delta;
+  a.d_lambda = d_lambda;
+  a.accumulate = accumulate;
+  hipError_t e = hipSuccess;
+  if (T > 0) {
+    e = traced(FLOWMOE_K_DIFF_BWD_DQ, st,
+               [&] { FLOWMOE_DIFF_LAUNCH(diff_dq_kernel, tiles(a, a.heads), 256); });
+    if (e != hipSuccess) return e;
+    e = traced(FLOWMOE_K_DIFF_BWD_DKDV, st,
+               [&] { FLOWMOE_DIFF_LAUNCH(diff_dkdv_kernel, tiles(a, a.kv), 256); });
+    if (e != hipSuccess) return e;
+  }
+  return traced(FLOWMOE_K_DIFF_JOIN, st, [&] {
+    hipLaunchKernelGGL(diff_dlambda_kernel, dim3(a.heads), dim3(1024), 0, st, a);
+  });
+}
+
+}  // namespace flowmoe

@@ -818,7 +818,7 @@ flowmoe_status_t check_diff(const flowmoe_shape_t* s, const flowmoe_diff_shape_t
   // (a tile's rows are reached by 32-bit byte offsets; a grid holds 2^32 threads)
   if ((long)s->T * 3 * s->M > (1L << 40) || s->T > (1 << 30) || s->M > (1 << 22))
     return fail(FLOWMOE_ERR_UNSUPPORTED, "tensor too large");
-  if (((m->seq_len + 127L) / 128) * m->heads * (s->T / m->seq_len) >= (1L << 32) / 512)
+  if (((m->seq_len + 31L) / 32) * m->heads * (s->T / m->seq_len) >= (1L << 32) / 512)
     return fail(FLOWMOE_ERR_UNSUPPORTED, "too many attention tiles");
   *out = DiffShape{m->seq_len, m->heads, m->kv_heads, m->head_dim, m->causal};
   return FLOWMOE_OK;

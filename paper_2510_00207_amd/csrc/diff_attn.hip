@@ -46,6 +46,7 @@ struct DiffArgs {
   int T, N, heads, kv, nseq;
   int accumulate;        // add to d_lambda
   long M, W;             // columns of a row of A, of qkv
+  int shared, pair;      // order of the blocks (diff_decode)
   float c2;              // log2(e) / sqrt(d)
   float rs;              // 1 / sqrt(d)
 };
@@ -56,175 +57,213 @@ __device__ __forceinline__ int seq_end(const DiffArgs& a, int sq) {
 }
 
 // block -> (tile, head, sequence): tiles of the most causal work first (`rev`: the
-// last query tiles), all heads of a tile side by side
+// last query tiles), all heads of a tile side by side. `pair` (every block resident at
+// once): the second half of the grid, which lands on the CUs of the first, runs the
+// least work first, so that a CU's blocks have complementary work. `shared`: the tiles
+// of a head one after the other on one XCD, so that its K and V are read through that
+// L2 once.
 __device__ __forceinline__ void diff_decode(const DiffArgs& a, int heads, bool rev, int rows,
                                             int& tile, int& hd, int& sq) {
   const int per = heads * a.nseq, nt = (a.N + rows - 1) / rows;
-  const int u = (int)(blockIdx.x / per), rest = (int)(blockIdx.x % per);
-  tile = rev ? nt - 1 - u : u;
+  if (a.shared && per % 8 == 0) {
+    const int i = blockIdx.x >> 3, rest = i / nt * 8 + (blockIdx.x & 7);
+    tile = rev ? nt - 1 - i % nt : i % nt;
+    hd = rest % heads;
+    sq = rest / heads;
+    return;
+  }
+  const int u = (int)(blockIdx.x / per), rest = (int)(blockIdx.x % per), h = (nt + 1) / 2;
+  const int r = a.pair && u >= h ? nt - 1 - (u - h) : u;
+  tile = rev ? nt - 1 - r : r;
   hd = rest % heads;
   sq = rest / heads;
 }
 
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(512, 2) void diff_fwd_kernel(DiffArgs a) {
-  constexpr int KS = D / 32, DB = D / 32, NW = 8, QB = 128;  // KS: k steps of one map
-  using Dma = TileDma<D, 64, NW>;
+// Forward: NW waves, two (one a map) for each 32 queries and each of S parts of a key
+// tile: with S > 1 a block has fewer queries and its waves share their keys.
+template <int NW, int S>
+struct FwdTile {
+  static constexpr int G = NW / (2 * S), QB = 32 * G;  // groups of 32 queries, queries
+  static constexpr int KB = S == 1 && NW == 8 ? 2 : 1, KT = 32 * KB * S;  // keys of a wave / 32, of a tile
+};
+template <int D, bool CAUSAL, int NW, int S>
+__global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffArgs a) {
+  using Tile = FwdTile<NW, S>;
+  constexpr int KS = D / 32, DB = D / 32, QB = Tile::QB, KT = Tile::KT;  // KS: k steps of one map
+  using Dma = TileDma<D, KT, NW>;
   constexpr int TB = Dma::TB;
-  // K slots 0, 1, then V slots 0, 1; at the end P_2 V (float) of the 128 queries
+  // K slots 0, 1, then V slots 0, 1; at the end the outputs (float) of half the waves
   __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
-  static_assert(4 * TB == QB * D * 4, "P_2 V fits the tiles' place");
+  __shared__ float2 stat[S > 1 ? NW / 2 * 64 : 1];  // and their references and sums
+  static_assert(4 * TB >= NW / 2 * 32 * D * 4, "the outputs fit the tiles' place");
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
-  const int map = w & 1, grp = w >> 1;
+  const int map = w & 1, grp = (w >> 1) % Tile::G, part = (w >> 1) / Tile::G;
   int qt, hd, sq;
   diff_decode(a, a.heads, CAUSAL, QB, qt, hd, sq);
   const int end = seq_end(a, sq);
   const long tok0 = (long)sq * a.N, ld = a.W;
-  const int kh = hd / (a.heads / a.kv);
-  const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
-  const bf16_t* Kg = a.qkv + tok0 * ld + a.M + (long)kh * D;
-  const bf16_t* Vg = Kg + (long)a.kv * D;
   const int q0 = qt * QB, qw = q0 + 32 * grp + lq;
-  const long srow = ((long)map * a.heads + hd) * a.T + tok0 + qw;
-  bf16_t* Og = a.out + (tok0 + qw) * a.M + (long)hd * D;
-  bf16_t* O2g = a.out2 + (tok0 + qw) * a.M + (long)hd * D;
 
   floatx16 o[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = zero16();
-  if (q0 >= end) {  // padding only
-    if (qw < a.N) {
+  float m = -INFINITY, l = 1.0f;
+  if (q0 < end) {  // (else padding only)
+    const int kh = hd / (a.heads / a.kv);
+    const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
+    const bf16_t* Kg = a.qkv + tok0 * ld + a.M + (long)kh * D;
+    const bf16_t* Vg = Kg + (long)a.kv * D;
+    const int kend = CAUSAL ? min(end, q0 + QB) : end;
+    const int nk = (kend + KT - 1) / KT;
+    const Dma dma(lds_base(lds), w, lane, ld);
+    const long kstep = KT * ld;
+    dma.load(Kg, kend, 0);
+    dma.load(Vg, kend, 2 * TB);
+    bf16x8 qf[KS];
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        if (map == 0) store_cols(Og + 32 * db, o[db], h2, 0.0f);
-        else if (a.out2 != nullptr) store_cols(O2g + 32 * db, o[db], h2, 0.0f);
-      }
-      if (h2 == 0 && a.lse != nullptr) a.lse[srow] = 0.0f;
-    }
-    return;
-  }
+    for (int ks = 0; ks < KS; ++ks)
+      qf[ks] = qw < end ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * (KS * map + ks) + 8 * h2)
+                        : zero8();
+    l = 0.0f;
+    int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
 
-  const int kend = CAUSAL ? min(end, q0 + QB) : end;
-  const int nk = (kend + 63) / 64;
-  // (causal: a wave whose queries all precede a tile has nothing in it)
-  const int nkw = CAUSAL ? min(nk, (q0 + 32 * grp + 31) / 64 + 1) : nk;
-  const Dma dma(lds_base(lds), w, lane, ld);
-  const long kstep = 64 * ld;
-  dma.load(Kg, kend, 0);
-  dma.load(Vg, kend, 2 * TB);
-
-  bf16x8 qf[KS];
+    auto step = [&](const int t, auto stc) {
+      constexpr int st = decltype(stc)::value;
+      opaque(rbase, tb0, tb1);
+      wait_vm<0>();   // K(t) and V(t): loaded a step ago
+      lds_barrier();  // and every wave's reads of the slots refilled now are done
+      const char* tk = lds + st * TB;
+      const char* tv = lds + (2 + st) * TB;
+      Kg += kstep;  // K(t + 1), V(t + 1)
+      Vg += kstep;
+      dma.load(Kg, kend - KT * (t + 1), (st ^ 1) * TB);
+      dma.load(Vg, kend - KT * (t + 1), (2 + (st ^ 1)) * TB);
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
-    qf[ks] = qw < end ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * (KS * map + ks) + 8 * h2)
-                      : zero8();
-  float m = -INFINITY, l = 0.0f;
-  int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
-
-  auto step = [&](const int t, auto stc) {
-    constexpr int st = decltype(stc)::value;
-    opaque(rbase, tb0, tb1);
-    wait_vm<0>();   // K(t) and V(t): loaded a step ago
-    lds_barrier();  // and every wave's reads of the slots refilled now are done
-    const char* tk = lds + st * TB;
-    const char* tv = lds + (2 + st) * TB;
-    Kg += kstep;  // K(t + 1), V(t + 1)
-    Vg += kstep;
-    dma.load(Kg, kend - 64 * (t + 1), (st ^ 1) * TB);
-    dma.load(Vg, kend - 64 * (t + 1), (2 + (st ^ 1)) * TB);
-    if (t >= nkw) return;
-    floatx16 s[2];
+      for (int j = 0; j < Tile::KB; ++j) {
+        const int kb = Tile::KB * part + j, kb0 = KT * t + 32 * kb;
+        // (causal: nothing for a wave whose queries all precede these keys)
+        if (CAUSAL && kb0 > q0 + 32 * grp + 31) return;
+        floatx16 s;
 #pragma unroll
-    for (int i = 0; i < KS; ++i)
+        for (int i = 0; i < KS; ++i)
+          s = mfma(frag_row_x<D>(tk, rbase, 32 * kb, KS * map + i), qf[i], i == 0 ? zero16() : s);
+        if (kb0 + 32 > end || (CAUSAL && kb0 + 31 > q0 + 32 * grp)) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-        s[u] = mfma(frag_row_x<D>(tk, rbase, 32 * u, KS * map + i), qf[i], i == 0 ? zero16() : s[u]);
-    const int kb0 = 64 * t;
-    if (kb0 + 64 > end || (CAUSAL && kb0 + 63 > q0 + 32 * grp)) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = kb0 + 32 * kb + 8 * (r >> 2) + 4 * h2 + (r & 3);
-          if (key >= end || (CAUSAL && key > qw)) s[kb][r] = -INFINITY;
+          for (int r = 0; r < 16; ++r) {
+            const int key = kb0 + 8 * (r >> 2) + 4 * h2 + (r & 3);
+            if (key >= end || (CAUSAL && key > qw)) s[r] = -INFINITY;
+          }
         }
-    }
-    float mx = s[0][0];
+        float mx = s[0];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        // the reference moves only when a score exceeds it by more than 2^8 (attn.hip).
+        // Every query sees key 0, so it is finite from its first tile on, but in the
+        // waves that key 0 is not given to a row may see no key yet
+        mx = pair_max(mx) * a.c2;
+        const bool up = mx > m + 8.0f;
+        if (__any(up)) {
+          const float mn = up ? mx : m;
+          const float al = exp2_fast(m - mn);
+          l *= al;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
-    // the reference moves only when a score exceeds it by more than 2^8 (attn.hip);
-    // every query sees key 0 in the first tile, so it is finite from then on
-    mx = pair_max(mx) * a.c2;
-    const bool up = mx > m + 8.0f;
-    if (__any(up)) {
-      const float mn = up ? mx : m;
-      const float al = exp2_fast(m - mn);
-      l *= al;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[db] *= al;
-      m = mn;
-    }
-    unsigned pw[16];  // the 32 probabilities of this lane, rounded to bf16 for the product
-    float rsum = 0.0f;
-#pragma unroll
-    for (int q = 0; q < 32; q += 2) {
-      const float p0 = exp2_fast(fmaf(s[q >> 4][q & 15], a.c2, -m));
-      const float p1 = exp2_fast(fmaf(s[q >> 4][(q & 15) + 1], a.c2, -m));
-      rsum += p0;
-      rsum += p1;
-      pw[q >> 1] = pack_bf16x2(p0, p1);
-    }
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{pw[4 * g], pw[4 * g + 1], pw[4 * g + 2], pw[4 * g + 3]});
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[db] = mfma(frag_tr_x<D>(tv, tb0, tb1, 16 * g, 32 * db), pb, o[db]);
-    }
-    l += pair_sum(rsum);
-  };
-  for (int t = 0; t < nk; t += 2) {
-    step(t, Stage<0>{});
-    if (t + 1 < nk) step(t + 1, Stage<1>{});
-  }
-
-  // the second map's waves hand their rows to the first's, lane by lane
-  wait_vm<0>();  // (the loads past the last tile write zeros)
-  lds_barrier();
-  const float inv = qw < end ? 1.0f / l : 0.0f;
-  float4* xch = reinterpret_cast<float4*>(lds) + (long)grp * DB * 4 * 64 + lane;
-  if (map == 1) {
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      o[db] *= inv;
-#pragma unroll
-      for (int J = 0; J < 4; ++J)
-        xch[(4 * db + J) * 64] = make_float4(o[db][4 * J], o[db][4 * J + 1], o[db][4 * J + 2], o[db][4 * J + 3]);
-    }
-  }
-  lds_barrier();
-  if (qw < a.N) {
-    if (map == 0) {
-      const float lam = qw < end ? a.lambda[hd] : 0.0f;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-#pragma unroll
-        for (int J = 0; J < 4; ++J) {
-          const float4 v = xch[(4 * db + J) * 64];
-          const float x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[db][4 * J + j] = o[db][4 * J + j] * inv - lam * x[j];
+          for (int db = 0; db < DB; ++db) o[db] *= al;
+          m = mn;
         }
-        store_cols(Og + 32 * db, o[db], h2, 1.0f);
-      }
-    } else if (a.out2 != nullptr) {
+        const float ref = S > 1 && m == -INFINITY ? 0.0f : m;
+        unsigned pw[8];  // this lane's 16 probabilities, rounded to bf16 for the product
+        float rsum = 0.0f;
 #pragma unroll
-      for (int db = 0; db < DB; ++db) store_cols(O2g + 32 * db, o[db], h2, 1.0f);
+        for (int q = 0; q < 16; q += 2) {
+          const float p0 = exp2_fast(fmaf(s[q], a.c2, -ref));
+          const float p1 = exp2_fast(fmaf(s[q + 1], a.c2, -ref));
+          rsum += p0;
+          rsum += p1;
+          pw[q >> 1] = pack_bf16x2(p0, p1);
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const bf16x8 pb = __builtin_bit_cast(bf16x8, u32x4{pw[4 * g], pw[4 * g + 1], pw[4 * g + 2], pw[4 * g + 3]});
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            o[db] = mfma(frag_tr_x<D>(tv, tb0, tb1, 32 * kb + 16 * g, 32 * db), pb, o[db]);
+        }
+        l += pair_sum(rsum);
+      }
+    };
+    for (int t = 0; t < nk; t += 2) {
+      step(t, Stage<0>{});
+      if (t + 1 < nk) step(t + 1, Stage<1>{});
     }
-    if (h2 == 0 && a.lse != nullptr) a.lse[srow] = qw < end ? (m + log2f(l)) * kLn2 : 0.0f;
+    // waves that share rows hand them over, lane by lane: half the key parts to the
+    // other half until one is left, then the second map to the first
+    auto slot = [&](int owner) { return reinterpret_cast<float4*>(lds) + (long)owner * DB * 4 * 64 + lane; };
+    auto put = [&](float4* x) {
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i) {
+        const floatx16& v = o[i / 4];
+        const int r = 4 * (i % 4);
+        x[i * 64] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
+      }
+    };
+    wait_vm<0>();  // (the loads past the last tile write zeros)
+    lds_barrier();
+#pragma unroll
+    for (int n = S / 2; n > 0; n /= 2) {
+      const int owner = ((part & (n - 1)) * Tile::G + grp) * 2 + map;  // of n x 2 G
+      if (part >= n && part < 2 * n) {
+        put(slot(owner));
+        stat[owner * 64 + lane] = make_float2(m, l);
+      }
+      lds_barrier();
+      if (part < n) {
+        const float2 other = stat[owner * 64 + lane];
+        const float mn = fmaxf(m, other.x);  // (part 0 has key 0: finite where the row is live)
+        const float ref = mn == -INFINITY ? 0.0f : mn;
+        const float f = exp2_fast(m - ref), g = exp2_fast(other.x - ref);
+        l = l * f + other.y * g;
+        m = mn;
+        const float4* x = slot(owner);
+#pragma unroll
+        for (int i = 0; i < 4 * DB; ++i) {
+          const float4 v = x[i * 64];
+          const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int r = 4 * (i % 4) + j;
+            o[i / 4][r] = o[i / 4][r] * f + e[j] * g;
+          }
+        }
+      }
+      lds_barrier();
+    }
+    const float inv = qw < end ? 1.0f / l : 0.0f;
+    const float lam = qw < end ? a.lambda[hd] : 0.0f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] *= inv;
+    if (part == 0 && map == 1) put(slot(grp));
+    lds_barrier();
+    if (part == 0 && map == 0) {
+      const float4* x = slot(grp);
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i) {
+        const float4 v = x[i * 64];
+        const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[i / 4][4 * (i % 4) + j] -= lam * e[j];
+      }
+    }
   }
+  if (qw >= a.N || part > 0) return;
+  bf16_t* out = map == 0 ? a.out : a.out2;
+  if (out != nullptr) {
+    bf16_t* Og = out + (tok0 + qw) * a.M + (long)hd * D;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) store_cols(Og + 32 * db, o[db], h2, 1.0f);
+  }
+  if (h2 == 0 && a.lse != nullptr)
+    a.lse[((long)map * a.heads + hd) * a.T + tok0 + qw] = qw < end ? (m + log2f(l)) * kLn2 : 0.0f;
 }
 
 // dQ, and d1 and d2: blocks of 4 waves of 32 queries over 32-key tiles, both maps in a
@@ -565,7 +604,53 @@ DiffArgs diff_args(const DiffShape& m, int T) {
     }                                                                                        \
   } while (0)
 
-long tiles(const DiffArgs& a, int heads) { return (long)((a.N + 127) / 128) * heads * a.nseq; }
+long tiles(const DiffArgs& a, int heads, int rows) {
+  return (long)((a.N + rows - 1) / rows) * heads * a.nseq;
+}
+
+template <int D, int NW, int S>
+void launch_fwd(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
+  const dim3 g((unsigned)tiles(a, a.heads, FwdTile<NW, S>::QB)), b(64 * NW);
+  if (m.causal) hipLaunchKernelGGL((diff_fwd_kernel<D, true, NW, S>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((diff_fwd_kernel<D, false, NW, S>), g, b, 0, st, a);
+}
+
+// Forward blocks by the launch: 0: 32 queries, 8 waves, four parts of the keys; 1: 32
+// queries, 4 waves, two parts; 2: 64 queries, 4 waves; 3: 128 queries, 8 waves.
+// Few queries leave CUs idle and a block's walk over the keys is the time of the call, so
+// its waves share the keys; many are better served by blocks that read K and V less
+// often. us of variants 0, 1, 2, 3: 1 sequence of 2048, heads of 128, causal, 4 heads 23,
+// 26, 43, 55; 8 heads 30, 28, 44, 55; 16 heads 58, 44, 47, 56; 32 heads 116, 81, 67, 73;
+// 4 x 4096, 32 heads 1719, 1648, 904, 885; 8 x 2048, 16 heads, bidirectional 803, 736,
+// 424, 413; 50 x 300 -, 155, 78, 90; 32 x 512, 32 heads -, 443, 241, 246.
+int fwd_variant(const DiffShape& m, const DiffArgs& a) {
+  const long b32 = tiles(a, a.heads, 32), b128 = tiles(a, a.heads, 128);
+  if (b32 <= 256) return 0;
+  if (b32 <= 1024) return 1;
+  return m.N >= 1024 && (b128 >= 1024 || !m.causal) ? 3 : 2;
+}
+long fwd_blocks(const DiffArgs& a, int v) {
+  return tiles(a, a.heads, v < 2 ? 32 : v == 2 ? 64 : 128);
+}
+
+// Tiles of a head side by side? Bidirectional ones have equal work and lose nothing by
+// it. Causal ones then no longer run longest first over the launch; it pays where they
+// are few to a head, or K and V far exceed the 256 MB Infinity Cache. us, not shared and
+// shared: bidirectional 8 x 2048, 16 heads of 128 430, 413; 16 x 500, 16 heads of 64 37,
+// 31; causal 50 x 300, 16 heads of 128 98, 78; 32 x 512, 32 heads 289, 241; 32 x 2048, 16
+// heads (537 MB) 1190, 1031; 4 x 4096, 32 heads (268 MB) 885, 899; 4 x 4096, 24 heads of
+// 64 412, 439.
+int fwd_shared(const DiffShape& m, const DiffArgs& a) {
+  return !m.causal || m.N <= 512 || 4L * a.T * m.kv * m.D >= (400L << 20);
+}
+
+template <int D>
+void launch_fwd_variant(int v, const DiffShape& m, const DiffArgs& a, hipStream_t st) {
+  if (v == 0) launch_fwd<D, 8, 4>(m, a, st);
+  else if (v == 1) launch_fwd<D, 4, 2>(m, a, st);
+  else if (v == 2) launch_fwd<D, 4, 1>(m, a, st);
+  else launch_fwd<D, 8, 1>(m, a, st);
+}
 
 }  // namespace
 
@@ -582,8 +667,16 @@ hipError_t launch_diff_attn_fwd(const DiffShape& m, int T, const void* qkv, cons
   a.out = static_cast<bf16_t*>(out);
   a.out2 = static_cast<bf16_t*>(out2);
   a.lse = lse;
-  return traced(FLOWMOE_K_DIFF_FWD, st,
-                [&] { FLOWMOE_DIFF_LAUNCH(diff_fwd_kernel, tiles(a, a.heads), 512); });
+  a.shared = fwd_shared(m, a);
+  const int v = fwd_variant(m, a);
+  a.pair = m.causal && fwd_blocks(a, v) <= 1024;
+#ifdef XPAIR
+  a.pair = m.causal && fwd_blocks(a, v) <= XPAIR;
+#endif
+  return traced(FLOWMOE_K_DIFF_FWD, st, [&] {
+    if (m.D == 128) launch_fwd_variant<128>(v, m, a, st);
+    else launch_fwd_variant<64>(v, m, a, st);
+  });
 }
 
 hipError_t launch_diff_attn_bwd(const DiffShape& m, int T, const void* qkv, const float* lambda,
@@ -606,10 +699,10 @@ hipError_t launch_diff_attn_bwd(const DiffShape& m, int T, const void* qkv, cons
   hipError_t e = hipSuccess;
   if (T > 0) {
     e = traced(FLOWMOE_K_DIFF_BWD_DQ, st,
-               [&] { FLOWMOE_DIFF_LAUNCH(diff_dq_kernel, tiles(a, a.heads), 256); });
+               [&] { FLOWMOE_DIFF_LAUNCH(diff_dq_kernel, tiles(a, a.heads, 128), 256); });
     if (e != hipSuccess) return e;
     e = traced(FLOWMOE_K_DIFF_BWD_DKDV, st,
-               [&] { FLOWMOE_DIFF_LAUNCH(diff_dkdv_kernel, tiles(a, a.kv), 256); });
+               [&] { FLOWMOE_DIFF_LAUNCH(diff_dkdv_kernel, tiles(a, a.kv, 128), 256); });
     if (e != hipSuccess) return e;
   }
   return traced(FLOWMOE_K_DIFF_JOIN, st, [&] {

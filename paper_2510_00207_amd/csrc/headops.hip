@@ -39,63 +39,94 @@ __device__ __forceinline__ double pair_turns(const RopeArgs& a, int i) {
 
 constexpr int kRopeTokens = 4;  // tokens of a block
 
+// 8 elements at any element's address (half of rot_dim need be no multiple of a vector;
+// global memory takes 16-byte accesses there)
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Any8 {
+  u32x4v_t v[sizeof(T) / 2];
+};
+__device__ __forceinline__ void load8_any(const bf16_t* p, float v[8]) {
+  raw8_f32(Raw8b{reinterpret_cast<const Any8<bf16_t>*>(p)->v[0]}, v);
+}
+__device__ __forceinline__ void load8_any(const float* p, float v[8]) {
+  const Any8<float>* q = reinterpret_cast<const Any8<float>*>(p);
+  raw8_f32(Raw8f{q->v[0], q->v[1]}, v);
+}
+__device__ __forceinline__ void store8_any(bf16_t* p, const float v[8]) {
+  reinterpret_cast<Any8<bf16_t>*>(p)->v[0] =
+      u32x4v_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+               pack_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ void store8_any(float* p, const float v[8]) {
+  Any8<float>* q = reinterpret_cast<Any8<float>*>(p);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    q->v[i] = u32x4v_t{__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                       __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
+}
+
 // A block's threads first make the cosines and sines of its tokens, once for all heads,
-// then walk the heads. ELEMS elements of a head a thread and step: 16 for the half
-// layout (8 of each half), 8 for pairs; 2 (one pair) where rot is no multiple of those.
-template <typename T, bool HALF, bool VEC>
+// then walk the heads in pieces. HALF: 8 pairs, 8 columns of each half of rot_dim, and
+// then the copied columns by eights; the last piece of either may be short. Pairs: 8
+// columns, of which those past rot_dim turn by nothing.
+template <typename T, bool HALF>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  extern __shared__ float2 table[];  // kRopeTokens x rot / 2
-  const int half = a.rot / 2, t0 = blockIdx.x * kRopeTokens, nt = min(kRopeTokens, a.T - t0);
-  for (int i = threadIdx.x; i < half; i += 256) {
+  extern __shared__ float2 table[];  // kRopeTokens x (rot / 2, rounded up to 4)
+  const int half = a.rot / 2, tw = (half + 3) & ~3, t0 = blockIdx.x * kRopeTokens,
+            nt = min(kRopeTokens, a.T - t0);
+  for (int i = threadIdx.x; i < tw; i += 256) {
     const double f = pair_turns(a, i);
     for (int t = 0; t < nt; ++t) {
       const int p = a.pos ? a.pos[t0 + t] : (t0 + t) % a.seq_len;
       const double turns = (double)p * f;
       float s, c;
       sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-      table[t * half + i] = make_float2(c * a.mscale, s * a.mscale * a.sign);
+      table[t * tw + i] = i < half ? make_float2(c * a.mscale, s * a.mscale * a.sign)
+                                   : make_float2(1.0f, 0.0f);
     }
   }
   __syncthreads();
-  // a head's work: `np` pieces of turned elements, then the copied ones
-  constexpr int PAIRS = VEC ? (HALF ? 8 : 4) : 1;  // pairs of a piece
-  constexpr int CP = VEC ? 8 : 1;                  // copied elements of a piece
-  const int np = half / PAIRS, n = np + (a.copy ? (a.D - a.rot) / CP : 0);
+  // a head's pieces: np of turned columns, the others copied
+  const int np = HALF ? (half + 7) / 8 : (a.rot + 7) / 8;
+  const int rest = HALF ? a.rot : 8 * np;  // the first column that is only copied
+  const int n = np + (a.copy ? (a.D - rest + 7) / 8 : 0);
   for (int k = threadIdx.x; k < n * a.heads * nt; k += 256) {
     const int c = k % n, r = k / n, hd = r % a.heads, t = r / a.heads;
     const long at = (long)(t0 + t) * a.ld + (long)hd * a.D;
     const T* x = static_cast<const T*>(a.x) + at;
     T* y = static_cast<T*>(a.y) + at;
+    float u[8], p[8];
     if (c >= np) {
-      const int e = a.rot + (c - np) * CP;
-      if constexpr (VEC) {
-        float v[8];
-        load8(x + e, v);
-        store8(y + e, v);
+      const int e = rest + 8 * (c - np);
+      if (e + 8 <= a.D) {
+        load8_any(x + e, u);
+        store8_any(y + e, u);
       } else {
-        y[e] = x[e];
+        for (int i = e; i < a.D; ++i) y[i] = x[i];
       }
       continue;
     }
-    const float2* cs = table + t * half + c * PAIRS;
-    if constexpr (!VEC) {
-      const int ia = HALF ? c : 2 * c, ib = HALF ? c + half : 2 * c + 1;
-      const float u = Elem<T>::load(x + ia), v = Elem<T>::load(x + ib);
-      Elem<T>::store(y + ia, u * cs[0].x - v * cs[0].y);
-      Elem<T>::store(y + ib, u * cs[0].y + v * cs[0].x);
-    } else if constexpr (HALF) {
-      float u[8], v[8], p[8], q[8];
-      load8(x + 8 * c, u);
-      load8(x + half + 8 * c, v);
+    const float2* cs = table + t * tw + c * (HALF ? 8 : 4);
+    if constexpr (HALF) {
+      if (8 * c + 8 <= half) {
+        float v[8], q[8];
+        load8(x + 8 * c, u);
+        load8_any(x + half + 8 * c, v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = u[i] * cs[i].x - v[i] * cs[i].y;
-        q[i] = u[i] * cs[i].y + v[i] * cs[i].x;
+        for (int i = 0; i < 8; ++i) {
+          p[i] = u[i] * cs[i].x - v[i] * cs[i].y;
+          q[i] = u[i] * cs[i].y + v[i] * cs[i].x;
+        }
+        store8(y + 8 * c, p);
+        store8_any(y + half + 8 * c, q);
+      } else {
+        for (int i = 8 * c; i < half; ++i, ++cs) {
+          const float v = Elem<T>::load(x + i), w = Elem<T>::load(x + half + i);
+          Elem<T>::store(y + i, v * cs->x - w * cs->y);
+          Elem<T>::store(y + half + i, v * cs->y + w * cs->x);
+        }
       }
-      store8(y + 8 * c, p);
-      store8(y + half + 8 * c, q);
     } else {
-      float u[8], p[8];
       load8(x + 8 * c, u);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -110,15 +141,9 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 template <typename T>
 void run_rope(const RopeArgs& a, bool half_layout, hipStream_t st) {
   const dim3 g((unsigned)((a.T + kRopeTokens - 1) / kRopeTokens)), b(256);
-  const size_t lds = (size_t)kRopeTokens * (a.rot / 2) * sizeof(float2);
-  const bool vec = a.rot % (half_layout ? 16 : 8) == 0;
-  if (half_layout) {
-    if (vec) hipLaunchKernelGGL((rope_kernel<T, true, true>), g, b, lds, st, a);
-    else hipLaunchKernelGGL((rope_kernel<T, true, false>), g, b, lds, st, a);
-  } else {
-    if (vec) hipLaunchKernelGGL((rope_kernel<T, false, true>), g, b, lds, st, a);
-    else hipLaunchKernelGGL((rope_kernel<T, false, false>), g, b, lds, st, a);
-  }
+  const size_t lds = (size_t)kRopeTokens * ((a.rot / 2 + 3) & ~3) * sizeof(float2);
+  if (half_layout) hipLaunchKernelGGL((rope_kernel<T, true>), g, b, lds, st, a);
+  else hipLaunchKernelGGL((rope_kernel<T, false>), g, b, lds, st, a);
 }
 
 // ---------------------------------------------------------------------------

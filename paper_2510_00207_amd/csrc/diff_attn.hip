@@ -12,9 +12,9 @@
 // zeros, without traffic, so that whatever they hold cannot reach a sum), and their
 // outputs and gradients are zeros.
 //
-// Forward: blocks of 8 waves, two (one a map) for each 32 of 128 queries; each runs
-// the online softmax of its map and its own P_i V, and the second hands P_2 V to
-// the first through LDS at the end. P_2 V is kept for the backward as well.
+// Forward: a wave runs the online softmax of one map for 32 queries and its own P_i V;
+// the second map's hands P_2 V to the first's through LDS at the end. P_2 V is kept for
+// the backward as well.
 //
 // Backward (no atomics; every sum in a fixed order), with dP = dA V^T, which both
 // maps share, d2 = rowsum(dA * P_2 V) and d1 = rowsum(dA * A) + lambda d2:
@@ -81,6 +81,15 @@ __device__ __forceinline__ void diff_decode(const DiffArgs& a, int heads, bool r
 
 // Forward: NW waves, two (one a map) for each 32 queries and each of S parts of a key
 // tile: with S > 1 a block has fewer queries and its waves share their keys.
+//
+// A wave has one map, not both: both maps' P_i V of 32 queries would take 128 of a
+// lane's registers at D = 128, one map's take 64, and four waves fit a SIMD (128
+// registers), whose softmaxes and products overlap. The 32 keys' scores, their softmax
+// and their products follow each other in a wave. 4 x 4096 tokens, 32 heads of 128,
+// causal: two waves a SIMD, 64 keys at a time 1030 us; the same one tile ahead of itself
+// 973; four waves 897, 32 keys at a time 880 (936 TFLOP/s, 0.79 of what a large matrix
+// product reaches here). A timing copy without the exponentials takes 817: the matrix
+// products and their power bound it.
 template <int NW, int S>
 struct FwdTile {
   static constexpr int G = NW / (2 * S), QB = 32 * G;  // groups of 32 queries, queries
@@ -669,10 +678,10 @@ hipError_t launch_diff_attn_fwd(const DiffShape& m, int T, const void* qkv, cons
   a.lse = lse;
   a.shared = fwd_shared(m, a);
   const int v = fwd_variant(m, a);
-  a.pair = m.causal && fwd_blocks(a, v) <= 1024;
-#ifdef XPAIR
-  a.pair = m.causal && fwd_blocks(a, v) <= XPAIR;
-#endif
+  // (every block resident at once: two to a CU, four of variant 2; 1 x 4096, 8 heads,
+  // causal, 1024 blocks of variant 1: 87 us with, 78 without; 1 x 2048, 32 heads, of
+  // variant 2: 67 and 69)
+  a.pair = m.causal && fwd_blocks(a, v) <= (v == 2 ? 1024 : 512);
   return traced(FLOWMOE_K_DIFF_FWD, st, [&] {
     if (m.D == 128) launch_fwd_variant<128>(v, m, a, st);
     else launch_fwd_variant<64>(v, m, a, st);

@@ -135,6 +135,7 @@ struct TileDma {
   static constexpr int CPR = D / 8, RPB = 64 / CPR;  // chunks a row, rows a block
   static constexpr int NB = TB / 1024, LD = (NB + NW - 1) / NW;  // blocks, loads a wave
   static_assert(NB % NW == 0, "whole loads");
+  static_assert(LD == 1 || LD == 2 || LD % 4 == 0, "loads of one, two or four blocks");
   unsigned lds0, ld2, full;  // this wave's first block in slot 0; bytes of a row step, of a tile
   unsigned off[LD];
   __device__ __forceinline__ TileDma(unsigned lds, int w, int lane, long ld)
@@ -150,7 +151,15 @@ struct TileDma {
     const unsigned n = rows >= ROWS ? full : rows <= 0 ? 0u : (rows - 1) * ld2 + 2 * D;
     const unsigned long a = reinterpret_cast<unsigned long>(g);
     const u32x4 rs = {(unsigned)a, (unsigned)(a >> 32) & 0xFFFFu, n, 0x00020000u};
-    dma16_row<LD, NW * 1024>(rs, lds0 + slot, off);
+    if constexpr (LD <= 4) {
+      dma16_row<LD, NW * 1024>(rs, lds0 + slot, off);
+    } else {
+#pragma unroll
+      for (int g = 0; g < LD; g += 4) {
+        const unsigned o4[4] = {off[g], off[g + 1], off[g + 2], off[g + 3]};
+        dma16_row<4, NW * 1024>(rs, lds0 + slot + g * NW * 1024, o4);
+      }
+    }
   }
 };
 

@@ -24,6 +24,8 @@
 // A key/value head's gradients are sums over the query heads of its group, in order.
 #include <math.h>
 
+#include <algorithm>
+
 #include "attn_tiles.hpp"
 #include "common.hpp"
 
@@ -46,6 +48,8 @@ struct DiffArgs {
   int T, N, heads, kv, nseq;
   int accumulate;        // add to d_lambda
   long M, W;             // columns of a row of A, of qkv
+  float* part;           // sums of units (dK, dV)
+  int unit, units;       // steps of a unit (0: uncut), units of a key head of a sequence
   int shared, pair;      // order of the blocks (diff_decode)
   float c2;              // log2(e) / sqrt(d)
   float rs;              // 1 / sqrt(d)
@@ -275,167 +279,290 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
     a.lse[((long)map * a.heads + hd) * a.T + tok0 + qw] = qw < end ? (m + log2f(l)) * kLn2 : 0.0f;
 }
 
-// dQ, and d1 and d2: blocks of 4 waves of 32 queries over 32-key tiles, both maps in a
-// wave (they share dP)
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(256, 2) void diff_dq_kernel(DiffArgs a) {
-  constexpr int KS = D / 16, DB = D / 32, NW = 4, QB = 32 * NW;
-  using Dma = TileDma<D, 32, NW>;
+// dQ, and d1 and d2: NW waves over 32-key tiles, both maps in a wave (they share dP). S
+// waves share 32 queries, each with every S-th key tile, and add up at the end: blocks
+// of few queries, for launches that leave CUs idle.
+//
+// 24 matrix products and 32 exponentials a lane for 32 x 32 pairs; the accumulators of dP
+// start at -d1, so that a map's factor is there without a subtraction. Every LDS read is a
+// group of products ahead of its use (991 -> 955 us at 4 x 4096 tokens, 32 heads of 128,
+// causal: 864 TFLOP/s of its 6 D flops a pair). The clock falls to 1.85 GHz with the matrix
+// pipes 45 % busy: power bounds it. Running dP and the first map's scores a tile ahead,
+// beside the elementwise work, measured 2 % slower (18 % with heads of 64).
+template <int D, bool CAUSAL, int NW, int S>
+__global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
+  constexpr int KS = D / 16, DB = D / 32, G = NW / S, QB = 32 * G, KT = 32 * S;
+  using Dma = TileDma<D, KT, NW>;
+  using DmaG = TileDma<D, QB, NW>;
   constexpr int TB = Dma::TB, VB = 2 * TB, GB = 4 * TB;  // K slots, V slots, the dO rows
   __shared__ __attribute__((aligned(1024))) char lds[GB + QB * D * 2];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
+  const int grp = w % G, part = w / G;
   int qt, hd, sq;
   diff_decode(a, a.heads, CAUSAL, QB, qt, hd, sq);
   const int end = seq_end(a, sq);
   const long tok0 = (long)sq * a.N, ld = a.W;
-  const int kh = hd / (a.heads / a.kv);
-  const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
-  const bf16_t* Kg = a.qkv + tok0 * ld + a.M + (long)kh * D;
-  const bf16_t* Vg = Kg + (long)a.kv * D;
-  const bf16_t* Gg = a.d_o + tok0 * a.M + (long)hd * D;
-  const bf16_t* Og = a.o + tok0 * a.M + (long)hd * D;
-  const bf16_t* O2g = a.o2 + tok0 * a.M + (long)hd * D;
-  const int q0 = qt * QB, qw = q0 + 32 * w + lq;
+  const int q0 = qt * QB, qw = q0 + 32 * grp + lq;
   const bool live = qw < end;
   const long srow = (long)hd * a.T + tok0 + qw, smap = (long)a.heads * a.T;
-  bf16_t* dst = a.d_qkv + (tok0 + qw) * ld + (long)hd * D;
+  const float lam = a.lambda[hd];
 
   floatx16 dq[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = zero16();
-  if (q0 >= end) {  // padding only
-    if (qw < a.N) {
-#pragma unroll
-      for (int db = 0; db < DB; ++db) store_cols(dst + 32 * db, dq[db], h2, 0.0f);
-      if (h2 == 0) a.delta[srow] = a.delta[srow + smap] = 0.0f;
-    }
-    return;
-  }
-  const int kend = CAUSAL ? min(end, q0 + QB) : end;
-  const int nk = (kend + 31) / 32;
-  const int nkw = CAUSAL ? min(nk, (q0 + 32 * w + 31) / 32 + 1) : nk;
-  const long kstep = 32 * ld;
-  const Dma dma(lds_base(lds), w, lane, ld);
-  {
-    const Dma dmag(lds_base(lds), w, lane, a.M);
-#pragma unroll
-    for (int i = 0; i < NW; ++i)
-      dmag.load(Gg + (long)(q0 + 32 * i) * a.M, end - q0 - 32 * i, GB + i * TB);
-  }
-  dma.load(Kg, kend, 0);
-  dma.load(Vg, kend, VB);
-  const float lam = a.lambda[hd];
-  bf16x8 qf[KS];
   float d1 = 0.0f, d2 = 0.0f;
+  if (q0 < end) {  // (else padding only)
+    const int kh = hd / (a.heads / a.kv);
+    const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
+    const bf16_t* Kg = a.qkv + tok0 * ld + a.M + (long)kh * D;
+    const bf16_t* Vg = Kg + (long)a.kv * D;
+    const long go = tok0 * a.M + (long)hd * D;
+    const int kend = CAUSAL ? min(end, q0 + QB) : end;
+    const int nk = (kend + KT - 1) / KT;
+    const long kstep = KT * ld;
+    const Dma dma(lds_base(lds), w, lane, ld);
+    DmaG(lds_base(lds), w, lane, a.M).load(a.d_o + go + (long)q0 * a.M, end - q0, GB);
+    dma.load(Kg, kend, 0);
+    dma.load(Vg, kend, VB);
+    bf16x8 qf[KS];
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    const int c = 16 * ks + 8 * h2;
-    qf[ks] = live ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + c) : zero8();
-    const bf16x8 gv = live ? *reinterpret_cast<const bf16x8*>(Gg + (long)qw * a.M + c) : zero8();
-    const bf16x8 ov = live ? *reinterpret_cast<const bf16x8*>(Og + (long)qw * a.M + c) : zero8();
-    const bf16x8 pv = live ? *reinterpret_cast<const bf16x8*>(O2g + (long)qw * a.M + c) : zero8();
+    for (int ks = 0; ks < KS; ++ks) {
+      const long c = go + (long)qw * a.M + 16 * ks + 8 * h2;
+      qf[ks] = live ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * ks + 8 * h2) : zero8();
+      const bf16x8 gv = live ? *reinterpret_cast<const bf16x8*>(a.d_o + c) : zero8();
+      const bf16x8 ov = live ? *reinterpret_cast<const bf16x8*>(a.o + c) : zero8();
+      const bf16x8 pv = live ? *reinterpret_cast<const bf16x8*>(a.o2 + c) : zero8();
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      d1 += (float)gv[t] * (float)ov[t];
-      d2 += (float)gv[t] * (float)pv[t];
+      for (int t = 0; t < 8; ++t) {
+        d1 += (float)gv[t] * (float)ov[t];
+        d2 += (float)gv[t] * (float)pv[t];
+      }
+    }
+    d1 = pair_sum(d1);
+    d2 = pair_sum(d2);
+    d1 += lam * d2;
+    const float l1 = live ? a.lse[srow] * kLog2e : 0.0f, l2 = live ? a.lse[srow + smap] * kLog2e : 0.0f;
+    int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
+    // read groups, each read one ahead of its products: 0 .. KS - 1, the K, V and dO rows
+    // at k step i; then DB groups of K transposed, 16 keys by 64 columns each
+    constexpr int NG = KS + DB, RS = 2;
+    bf16x8 fr[RS][3];
+    auto read_group = [&](const char* tk, const char* tv, int i) {
+      if (i < KS) {
+        fr[i % RS][0] = frag_row_x<D>(tk, rbase, 0, i);
+        fr[i % RS][1] = frag_row_x<D>(tv, rbase, 0, i);
+        fr[i % RS][2] = frag_row_x<D>(lds + GB, rbase, 32 * grp, i);
+      } else if (i < NG) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          fr[i % RS][u] = frag_tr_x<D>(tk, tb0, tb1, 16 * ((i - KS) / (DB / 2)),
+                                      32 * (2 * ((i - KS) % (DB / 2)) + u));
+      }
+    };
+    auto step = [&](const int t, auto stc) {
+      constexpr int st = decltype(stc)::value;
+      opaque(rbase, tb0, tb1);
+      wait_vm<0>();   // K(t) and V(t): loaded a step ago
+      lds_barrier();  // and every wave's reads of the slots refilled now are done
+      const char* tk = lds + st * TB + part * (32 * 2 * D);
+      const char* tv = tk + VB;
+      Kg += kstep;
+      Vg += kstep;
+      dma.load(Kg, kend - KT * (t + 1), (st ^ 1) * TB);
+      dma.load(Vg, kend - KT * (t + 1), VB + (st ^ 1) * TB);
+      const int kb0 = KT * t + 32 * part;
+      // (causal: nothing for a wave whose queries all precede these keys)
+      if (kb0 >= kend || (CAUSAL && kb0 > q0 + 32 * grp + 31)) return;
+      floatx16 s[2], dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] = -d1;  // dP - d1
+      read_group(tk, tv, 0);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        read_group(tk, tv, i + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        floatx16& x = s[i >= KS / 2];
+        x = mfma(fr[i % RS][0], qf[i], i % (KS / 2) == 0 ? zero16() : x);
+        dp = mfma(fr[i % RS][1], fr[i % RS][2], dp);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (kb0 + 32 > end || (CAUSAL && kb0 + 31 > q0 + 32 * grp)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = kb0 + 8 * (r >> 2) + 4 * h2 + (r & 3);
+          if (key >= end || (CAUSAL && key > qw)) s[0][r] = s[1][r] = -INFINITY;
+        }
+      }
+      unsigned pw[2][8];  // dS^T of each map in this lane, rounded to bf16 for the product
+      const float dd = d1 - d2;
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        float e[2], f[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          e[j] = exp2_fast(fmaf(s[0][r + j], a.c2, -l1)) * dp[r + j];
+          f[j] = exp2_fast(fmaf(s[1][r + j], a.c2, -l2)) * (dp[r + j] + dd);
+        }
+        pw[0][r >> 1] = pack_bf16x2(e[0], e[1]);
+        pw[1][r >> 1] = pack_bf16x2(f[0], f[1]);  // (times -lambda at the end)
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < DB; ++j) {
+        read_group(tk, tv, KS + j + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const int g = j / (DB / 2);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int db = 2 * (j % (DB / 2)) + u;
+          const unsigned* p = pw[db >= DB / 2 ? 1 : 0] + 4 * g;
+          dq[db] = mfma(fr[(KS + j) % RS][u],
+                        __builtin_bit_cast(bf16x8, u32x4{p[0], p[1], p[2], p[3]}), dq[db]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    for (int t = 0; t < nk; t += 2) {
+      step(t, Stage<0>{});
+      if (t + 1 < nk) step(t + 1, Stage<1>{});
+    }
+    if constexpr (S > 1) {  // parts S - 1 .. 1 hand their sums to part 0's waves, in that order
+      wait_vm<0>();         // (the loads past the last tile write zeros)
+      float4* x = reinterpret_cast<float4*>(lds) + (long)grp * DB * 4 * 64 + lane;
+#pragma unroll
+      for (int n = S - 1; n > 0; --n) {
+        lds_barrier();
+        if (part == n) {
+#pragma unroll
+          for (int i = 0; i < 4 * DB; ++i) {
+            const floatx16& v = dq[i / 4];
+            const int r = 4 * (i % 4);
+            x[i * 64] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
+          }
+        }
+        lds_barrier();
+        if (part == 0) {
+#pragma unroll
+          for (int i = 0; i < 4 * DB; ++i) {
+            const float4 v = x[i * 64];
+            const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) dq[i / 4][4 * (i % 4) + j] += e[j];
+          }
+        }
+      }
     }
   }
-  d1 = pair_sum(d1);
-  d2 = pair_sum(d2);
-  d1 += lam * d2;
-  if (qw < a.N && h2 == 0) {
+  if (qw >= a.N || part > 0) return;
+  if (h2 == 0) {
     a.delta[srow] = d1;
     a.delta[srow + smap] = d2;
   }
-  const float l1 = live ? a.lse[srow] * kLog2e : 0.0f, l2 = live ? a.lse[srow + smap] * kLog2e : 0.0f;
-  int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
-
-  auto step = [&](const int t, auto stc) {
-    constexpr int st = decltype(stc)::value;
-    opaque(rbase, tb0, tb1);
-    wait_vm<0>();
-    lds_barrier();
-    const char* tk = lds + st * TB;
-    const char* tv = lds + VB + st * TB;
-    Kg += kstep;
-    Vg += kstep;
-    dma.load(Kg, kend - 32 * (t + 1), (st ^ 1) * TB);
-    dma.load(Vg, kend - 32 * (t + 1), VB + (st ^ 1) * TB);
-    if (t >= nkw) return;
-    floatx16 s1, s2, dp;
+  bf16_t* dst = a.d_qkv + (tok0 + qw) * ld + (long)hd * D;
 #pragma unroll
-    for (int i = 0; i < KS / 2; ++i) {
-      s1 = mfma(frag_row_x<D>(tk, rbase, 0, i), qf[i], i == 0 ? zero16() : s1);
-      s2 = mfma(frag_row_x<D>(tk, rbase, 0, KS / 2 + i), qf[KS / 2 + i], i == 0 ? zero16() : s2);
-    }
-#pragma unroll
-    for (int i = 0; i < KS; ++i)
-      dp = mfma(frag_row_x<D>(tv, rbase, 0, i), frag_row_x<D>(lds + GB, rbase, 32 * w, i),
-                i == 0 ? zero16() : dp);
-    const int kb0 = 32 * t;
-    if (kb0 + 32 > end || (CAUSAL && kb0 + 31 > q0 + 32 * w)) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int key = kb0 + 8 * (r >> 2) + 4 * h2 + (r & 3);
-        if (key >= end || (CAUSAL && key > qw)) s1[r] = s2[r] = -INFINITY;
-      }
-    }
-    unsigned pw[2][8];  // dS^T of each map in this lane, rounded to bf16 for the product
-#pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      float e[2], f[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        e[j] = exp2_fast(fmaf(s1[r + j], a.c2, -l1)) * (dp[r + j] - d1);
-        f[j] = exp2_fast(fmaf(s2[r + j], a.c2, -l2)) * (dp[r + j] - d2);
-      }
-      pw[0][r >> 1] = pack_bf16x2(e[0], e[1]);
-      pw[1][r >> 1] = pack_bf16x2(f[0], f[1]);  // (times -lambda at the end)
-    }
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        const unsigned* p = pw[db >= DB / 2 ? 1 : 0] + 4 * g;
-        dq[db] = mfma(frag_tr_x<D>(tk, tb0, tb1, 16 * g, 32 * db),
-                      __builtin_bit_cast(bf16x8, u32x4{p[0], p[1], p[2], p[3]}), dq[db]);
-      }
-  };
-  for (int t = 0; t < nk; t += 2) {
-    step(t, Stage<0>{});
-    if (t + 1 < nk) step(t + 1, Stage<1>{});
-  }
-  if (qw < a.N) {
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      if (!live) dq[db] = zero16();
-      store_cols(dst + 32 * db, dq[db], h2, db >= DB / 2 ? -lam * a.rs : a.rs);
-    }
+  for (int db = 0; db < DB; ++db) {
+    if (!live) dq[db] = zero16();
+    store_cols(dst + 32 * db, dq[db], h2, db >= DB / 2 ? -lam * a.rs : a.rs);
   }
 }
 
-// dK and dV: blocks of 4 waves of 32 keys over the 32-query tiles of every query head of
-// the group
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffArgs a) {
-  constexpr int KS = D / 16, DB = D / 32, NW = 4, KB = 32 * NW;
-  using Dma = TileDma<D, 32, NW>;
-  constexpr int TQ = Dma::TB;          // one 32-row tile
+// dlambda_h = -sum of d2 over all rows, by a block
+__device__ __forceinline__ void sum_d_lambda(const DiffArgs& a, int hd, float* part) {
+  const float* d2 = a.delta + ((long)a.heads + hd) * a.T;
+  float s8[8] = {};
+  const int n = blockDim.x;
+  int t = threadIdx.x;
+  for (; t + 7 * n < a.T; t += 8 * n) {  // (eight loads in flight)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s8[i] += d2[t + i * n];
+  }
+  for (; t < a.T; t += n) s8[0] += d2[t];
+  float s = ((s8[0] + s8[1]) + (s8[2] + s8[3])) + ((s8[4] + s8[5]) + (s8[6] + s8[7]));
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) s += __shfl_xor(s, x);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = 0.0f;
+    for (int i = 0; i < (int)blockDim.x / 64; ++i) s += part[i];
+    a.d_lambda[hd] = (a.accumulate ? a.d_lambda[hd] : 0.0f) - s;
+  }
+}
+
+// Steps of QT queries that see key tile kt of KB rows. A (key tile, key head, sequence) is
+// cut into units of `a.unit` steps, the group's heads one after the other (0: uncut).
+template <bool CAUSAL, int KB, int QT>
+__host__ __device__ __forceinline__ int key_steps(int N, int kt) {
+  return (N - (CAUSAL ? kt * KB : 0) + QT - 1) / QT;
+}
+
+// Unit u of a key head of a sequence: its key tile, the tile's units, and its place among
+// them; or (u < 0) the units before tile kt. A lane a tile, as a loop over the tiles with a
+// division each took microseconds.
+struct UnitAt {
+  int kt, units, chunk;
+};
+template <bool CAUSAL, int KB, int QT>
+__device__ __forceinline__ UnitAt find_unit(const DiffArgs& a, int u, int kt) {
+  const int group = a.heads / a.kv, nt = (a.N + KB - 1) / KB, lane = threadIdx.x & 63;
+  int before = 0;
+  for (int k0 = 0;; k0 += 64) {
+    const int k = k0 + lane;
+    const int n = k < nt ? (group * key_steps<CAUSAL, KB, QT>(a.N, k) + a.unit - 1) / a.unit : 0;
+    int upto = n;  // the units of tiles k0 .. k
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int v = __shfl_up(upto, d);
+      if (lane >= d) upto += v;
+    }
+    const unsigned long long here = __ballot(u >= 0 ? before + upto > u : k == kt);
+    if (here != 0) {
+      const int f = __ffsll(here) - 1;
+      const int units = __builtin_amdgcn_readlane(n, f);
+      const int first = before + __builtin_amdgcn_readlane(upto, f) - units;
+      return {k0 + f, units, u >= 0 ? u - first : first};
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+}
+
+// dK and dV: waves of 32 keys over the 32-query tiles of every query head of the group, or
+// over a unit of them, whose sums diff_join_kernel adds. With S > 1, S of the NW waves share 32 keys, each with every S-th query tile, and add up at the end. The
+// last `heads` blocks sum dlambda.
+template <int D, bool CAUSAL, int NW, int S>
+__global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
+  constexpr int KS = D / 16, DB = D / 32, G = NW / S, KB = 32 * G, QT = 32 * S;
+  using Dma = TileDma<D, QT, NW>;
+  using DmaV = TileDma<D, KB, NW>;
+  constexpr int TQ = Dma::TB;          // one query tile
   constexpr int VT = 4 * TQ;           // two slots of Q and dO, then the block's V rows,
-  constexpr int ST = VT + KB * D * 2;  // then two slots of 32 x (lse 1, lse 2, d1, d2)
-  __shared__ __attribute__((aligned(1024))) char lds[ST + 2 * 512];
+  constexpr int ST = VT + KB * D * 2;  // then two slots of 32 S x (lse 1, lse 2, -d1, d2 - d1)
+  constexpr int SB = 512 * S;
+  __shared__ __attribute__((aligned(1024))) char lds[ST + 2 * SB];
+  static_assert(S == 1 || G * 8 * DB * 1024 <= ST + 2 * SB, "a part's sums fit");
+  const int per = a.kv * a.nseq, nblocks = (int)gridDim.x - a.heads;
+  if ((int)blockIdx.x >= nblocks) {
+    sum_d_lambda(a, blockIdx.x - nblocks, reinterpret_cast<float*>(lds));
+    return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
-  int kt, kh, sq;
-  diff_decode(a, a.kv, false, KB, kt, kh, sq);
+  const int grp = w % G, part = w / G;
+  const int rest = (int)(blockIdx.x % per), kh = rest % a.kv, sq = rest / a.kv;
+  const int group = a.heads / a.kv;
+  int kt = (int)(blockIdx.x / per), units = 1, chunk = 0;
+  if (a.unit > 0) {
+    const UnitAt at = find_unit<CAUSAL, KB, QT>(a, kt, 0);
+    kt = at.kt;
+    units = at.units;
+    chunk = at.chunk;
+  }
   const int end = seq_end(a, sq);
   const long tok0 = (long)sq * a.N, ld = a.W;
-  const int group = a.heads / a.kv;
-  const int k0 = kt * KB, kw = k0 + 32 * w + lq;
+  const int k0 = kt * KB, kw = k0 + 32 * grp + lq;
   const bool live = kw < end;
   const long kcol = a.M + (long)kh * D, vcol = kcol + (long)a.kv * D;
-  bf16_t* dst = a.d_qkv + (tok0 + kw) * ld;
   floatx16 dv[DB], dk[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
@@ -445,93 +572,114 @@ __global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffArgs a) {
   if (k0 < end) {
     const bf16_t* rows = a.qkv + tok0 * ld;
     const Dma dma(lds_base(lds), w, lane, ld), dmag(lds_base(lds), w, lane, a.M);
-#pragma unroll
-    for (int i = 0; i < NW; ++i)
-      dma.load(rows + vcol + (long)(k0 + 32 * i) * ld, end - k0 - 32 * i, VT + i * TQ);
+    DmaV(lds_base(lds), w, lane, ld).load(rows + vcol + (long)k0 * ld, end - k0, VT);
     bf16x8 kf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
       kf[ks] = live ? *reinterpret_cast<const bf16x8*>(rows + kcol + kw * ld + 16 * ks + 8 * h2) : zero8();
-    // query steps of 32: causal keys k0.. are seen by queries >= k0 only
+    // query steps of QT: causal keys k0.. are seen by queries >= k0 only
     const int qs0 = CAUSAL ? k0 : 0;
-    const int nqs = (end - qs0 + 31) / 32;
+    const int steps = key_steps<CAUSAL, KB, QT>(a.N, kt), valid = (end - qs0 + QT - 1) / QT;
+    const int lo = chunk * a.unit, hi = a.unit > 0 ? min(lo + a.unit, group * steps) : group * steps;
     int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
 
-    for (int gh = 0; gh < group; ++gh) {
+    bool more_heads = false;
+    for (int gh = lo / steps; gh * steps < hi; ++gh) {
+      const int it0 = max(lo - gh * steps, 0), it1 = min(hi - gh * steps, valid);
+      if (it0 >= it1) continue;
       const int hd = kh * group + gh;
       const float lam = a.lambda[hd];
-      const bf16_t* Qt = rows + (long)hd * D + qs0 * ld;
-      const bf16_t* Gt = a.d_o + (tok0 + qs0) * a.M + (long)hd * D;
-      // the statistics of a step: 128 threads, one value each
-      float rstat = 0.0f;
-      const int which = (tid >> 5) & 3;
-      const float* sp = (which < 2 ? a.lse : a.delta) +
-                        ((long)(which & 1) * a.heads + hd) * a.T + tok0 + (tid & 31);
+      const int qf0 = qs0 + QT * it0;
+      const bf16_t* Qt = rows + (long)hd * D + qf0 * ld;
+      const bf16_t* Gt = a.d_o + (tok0 + qf0) * a.M + (long)hd * D;
+      // the statistics of a step: lse or delta of a row, both maps', a thread
+      float2 rstat = make_float2(0.0f, 0.0f);
+      const bool isd = (tid & 32) != 0;
+      const int srow = 32 * (tid >> 6) + lq;
+      const float* sp = (isd ? a.delta : a.lse) + (long)hd * a.T + tok0 + srow;
+      const long smap = (long)a.heads * a.T;
       auto load_stat = [&](int qb) {
-        if (tid < 128) rstat = qb + (tid & 31) < end ? sp[qb] * (which < 2 ? kLog2e : 1.0f) : 0.0f;
+        if (tid < 64 * S) {
+          const bool in = qb + srow < end;
+          const float x = in ? sp[qb] : 0.0f, y = in ? sp[qb + smap] : 0.0f;
+          rstat = isd ? make_float2(-x, y - x) : make_float2(x * kLog2e, y * kLog2e);
+        }
       };
       auto store_stat = [&](int slot) {
-        if (tid < 128) reinterpret_cast<float*>(lds + ST + 512 * slot)[tid] = rstat;
+        if (tid < 64 * S) {
+          float* s = reinterpret_cast<float*>(lds + ST + SB * slot) + 128 * (tid >> 6) + (isd ? 64 : 0) + lq;
+          s[0] = rstat.x;
+          s[32] = rstat.y;
+        }
       };
-      if (gh > 0) {  // the last head's loads have landed and its reads are done
+      if (more_heads) {  // (the last head's loads have landed and its reads are done)
         wait_vm<0>();
         lds_barrier();
       }
-      dma.load(Qt, end - qs0, 0);
-      dmag.load(Gt, end - qs0, TQ);
-      load_stat(qs0);
+      more_heads = true;
+      dma.load(Qt, end - qf0, 0);
+      dmag.load(Gt, end - qf0, TQ);
+      load_stat(qf0);
       store_stat(0);
 
+      constexpr int H = KS / 2;
       auto step = [&](const int it, auto stc) {
         constexpr int st = decltype(stc)::value;
         opaque(rbase, tb0, tb1);
-        const int qb = qs0 + 32 * it;
+        const int qt0 = qs0 + QT * it, qb = qt0 + 32 * part;
         wait_vm<0>();   // this tile's loads
         lds_barrier();  // and every wave's reads of the other slot are done
-        const char* tq = lds + st * 2 * TQ;
-        const char* tg = tq + TQ;
-        const float* stat = reinterpret_cast<const float*>(lds + ST + 512 * st);
-        Qt += 32 * ld;
-        Gt += 32 * a.M;
-        dma.load(Qt, end - qb - 32, (st ^ 1) * 2 * TQ);
-        dmag.load(Gt, end - qb - 32, (st ^ 1) * 2 * TQ + TQ);
-        if (it + 1 < nqs) load_stat(qb + 32);
-        if (!CAUSAL || qb + 31 >= k0 + 32 * w) {
+        const char* tq = lds + st * 2 * TQ + part * (32 * 2 * D);
+        const float* stat = reinterpret_cast<const float*>(lds + ST + SB * st) + 128 * part + 4 * h2;
+        Qt += QT * ld;
+        Gt += QT * a.M;
+        const int more = it + 1 < it1 ? end - qt0 - QT : 0;
+        dma.load(Qt, more, (st ^ 1) * 2 * TQ);
+        dmag.load(Gt, more, (st ^ 1) * 2 * TQ + TQ);
+        if (it + 1 < it1) load_stat(qt0 + QT);
+        if (qb < end && (!CAUSAL || qb + 31 >= k0 + 32 * grp)) {
+          const bool edge = qb + 32 > end || (CAUSAL && k0 + 32 * grp + 31 > qb);
+          auto mask = [&](floatx16& s) {
+            if (edge) {
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const int q = qb + 8 * (r >> 2) + 4 * h2 + (r & 3);
+                if (q >= end || (CAUSAL && kw > q)) s[r] = -INFINITY;
+              }
+            }
+          };
+          auto row4 = [&](int k, int J) { return *reinterpret_cast<const float4*>(stat + 32 * k + 8 * J); };
           floatx16 s1, s2, dp;
+          unsigned pp[8], pd[2][8];  // P_1 - lambda P_2 and dS of each map, bf16 pairs
+          const char* tg = tq + TQ;
+#pragma unroll
+          for (int J = 0; J < 4; ++J) {  // dP - d1
+            const float4 v = row4(2, J);
+            dp[4 * J] = v.x; dp[4 * J + 1] = v.y; dp[4 * J + 2] = v.z; dp[4 * J + 3] = v.w;
+          }
+#pragma unroll
+          for (int i = 0; i < H; ++i) {
+            s1 = mfma(frag_row_x<D>(tq, rbase, 0, i), kf[i], i == 0 ? zero16() : s1);
+            s2 = mfma(frag_row_x<D>(tq, rbase, 0, H + i), kf[H + i], i == 0 ? zero16() : s2);
+          }
 #pragma unroll
           for (int i = 0; i < KS; ++i)
-            dp = mfma(frag_row_x<D>(tg, rbase, 0, i), frag_row_x<D>(lds + VT, rbase, 32 * w, i),
-                      i == 0 ? zero16() : dp);
-#pragma unroll
-          for (int i = 0; i < KS / 2; ++i) {
-            s1 = mfma(frag_row_x<D>(tq, rbase, 0, i), kf[i], i == 0 ? zero16() : s1);
-            s2 = mfma(frag_row_x<D>(tq, rbase, 0, KS / 2 + i), kf[KS / 2 + i], i == 0 ? zero16() : s2);
-          }
-          if (qb + 32 > end || (CAUSAL && k0 + 32 * w + 31 > qb)) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int q = qb + 8 * (r >> 2) + 4 * h2 + (r & 3);
-              if (q >= end || (CAUSAL && kw > q)) s1[r] = s2[r] = -INFINITY;
-            }
-          }
-          unsigned pp[8], pd[2][8];  // P_1 - lambda P_2 and dS of each map, bf16 pairs
+            dp = mfma(frag_row_x<D>(tg, rbase, 0, i), frag_row_x<D>(lds + VT, rbase, 32 * grp, i), dp);
+          mask(s1);
+          mask(s2);
 #pragma unroll
           for (int J = 0; J < 4; ++J) {
-            float st4[4][4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float4 v = *reinterpret_cast<const float4*>(stat + 32 * k + 8 * J + 4 * h2);
-              st4[k][0] = v.x; st4[k][1] = v.y; st4[k][2] = v.z; st4[k][3] = v.w;
-            }
+            const float4 t = row4(0, J), v = row4(1, J), u = row4(3, J);
+            const float l1[4] = {t.x, t.y, t.z, t.w}, l2[4] = {v.x, v.y, v.z, v.w}, dd[4] = {u.x, u.y, u.z, u.w};
             float p[4], e[4], f[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const int r = 4 * J + j;
-              const float p1 = exp2_fast(fmaf(s1[r], a.c2, -st4[0][j]));
-              const float p2 = lam * exp2_fast(fmaf(s2[r], a.c2, -st4[1][j]));
+              const float p1 = exp2_fast(fmaf(s1[r], a.c2, -l1[j]));
+              const float p2 = lam * exp2_fast(fmaf(s2[r], a.c2, -l2[j]));
               p[j] = p1 - p2;
-              e[j] = p1 * (dp[r] - st4[2][j]);
-              f[j] = p2 * (st4[3][j] - dp[r]);
+              e[j] = p1 * dp[r];
+              f[j] = p2 * (dd[j] - dp[r]);
             }
 #pragma unroll
             for (int j = 0; j < 4; j += 2) {
@@ -546,21 +694,59 @@ __global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffArgs a) {
             for (int db = 0; db < DB; ++db) {
               const unsigned* d = pd[db >= DB / 2 ? 1 : 0] + 4 * g;
               dv[db] = mfma(frag_tr_x<D>(tg, tb0, tb1, 16 * g, 32 * db),
-                            __builtin_bit_cast(bf16x8, u32x4{pp[4 * g], pp[4 * g + 1], pp[4 * g + 2], pp[4 * g + 3]}),
-                            dv[db]);
+                            __builtin_bit_cast(bf16x8, u32x4{pp[4 * g], pp[4 * g + 1], pp[4 * g + 2], pp[4 * g + 3]}), dv[db]);
               dk[db] = mfma(frag_tr_x<D>(tq, tb0, tb1, 16 * g, 32 * db),
                             __builtin_bit_cast(bf16x8, u32x4{d[0], d[1], d[2], d[3]}), dk[db]);
             }
         }
-        if (it + 1 < nqs) store_stat(st ^ 1);
+        if (it + 1 < it1) store_stat(st ^ 1);
       };
-      for (int it = 0; it < nqs; it += 2) {
+      for (int it = it0; it < it1; it += 2) {
         step(it, Stage<0>{});
-        if (it + 1 < nqs) step(it + 1, Stage<1>{});
+        if (it + 1 < it1) step(it + 1, Stage<1>{});
       }
     }
   }
-  if (kw < a.N) {  // (rows past the end: their accumulators hold only masked zeros)
+  if constexpr (S > 1) {  // parts S - 1 .. 1 hand their sums to part 0's waves, in that order
+    wait_vm<0>();         // (the loads past the last tile write zeros)
+    float4* x = reinterpret_cast<float4*>(lds) + (long)grp * 8 * DB * 64 + lane;
+#pragma unroll
+    for (int n = S - 1; n > 0; --n) {
+      lds_barrier();
+      if (part == n) {
+#pragma unroll
+        for (int i = 0; i < 8 * DB; ++i) {
+          const floatx16& v = i < 4 * DB ? dk[i / 4] : dv[i / 4 - DB];
+          const int r = 4 * (i % 4);
+          x[i * 64] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
+        }
+      }
+      lds_barrier();
+      if (part == 0) {
+#pragma unroll
+        for (int i = 0; i < 8 * DB; ++i) {
+          floatx16& s = i < 4 * DB ? dk[i / 4] : dv[i / 4 - DB];
+          const float4 v = x[i * 64];
+          const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[4 * (i % 4) + j] += e[j];
+        }
+      }
+    }
+    if (part > 0) return;
+  }
+  if (units > 1) {
+    if (k0 >= end) return;
+    float4* x = reinterpret_cast<float4*>(a.part) +
+                ((long)rest * a.units + blockIdx.x / per) * (8 * DB * 64 * G) + tid;
+#pragma unroll
+    for (int i = 0; i < 8 * DB; ++i) {
+      const floatx16& v = i < 4 * DB ? dk[i / 4] : dv[i / 4 - DB];
+      const int r = 4 * (i % 4);
+      x[i * 64 * G] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
+    }
+  } else if (kw < a.N) {  // (rows past the end: their accumulators hold only masked zeros)
+    bf16_t* dst = a.d_qkv + (tok0 + kw) * ld;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       if (!live) dk[db] = dv[db] = zero16();
@@ -570,21 +756,34 @@ __global__ __launch_bounds__(256, 2) void diff_dkdv_kernel(DiffArgs a) {
   }
 }
 
-// dlambda_h = -sum of d2 over all rows: a block a head
-__global__ __launch_bounds__(1024) void diff_dlambda_kernel(DiffArgs a) {
-  __shared__ float part[16];
-  const float* d2 = a.delta + ((long)a.heads + blockIdx.x) * a.T;
-  float s = 0.0f;
-  for (int t = threadIdx.x; t < a.T; t += 1024) s += d2[t];
+// dK and dV of key tiles that were cut into units, their sums added in unit order: a block
+// a key tile of 32 G and 32 columns of K or V, with the lanes as they were
+template <int D, bool CAUSAL, int G, int S>
+__global__ __launch_bounds__(64 * G) void diff_join_kernel(DiffArgs a) {
+  constexpr int DB = D / 32, KB = 32 * G, QT = 32 * S;
+  const int per = a.kv * a.nseq, tid = threadIdx.x, lane = tid & 63;
+  const int rest = (int)(blockIdx.x % per), kh = rest % a.kv, sq = rest / a.kv;
+  const int u = (int)(blockIdx.x / per), col = u % (2 * DB), kt = u / (2 * DB);
+  const UnitAt at = find_unit<CAUSAL, KB, QT>(a, -1, kt);
+  const int first = at.chunk, units = at.units;
+  if (units == 1) return;
+  const int end = seq_end(a, sq), k0 = kt * KB, kw = k0 + 32 * (tid >> 6) + (lane & 31);
+  floatx16 s = zero16();
+  if (kw < end) {
+    constexpr int U = 8 * DB * 64 * G;  // float4s of a unit
+    const float4* x = reinterpret_cast<const float4*>(a.part) + ((long)rest * a.units + first) * U +
+                      4 * col * 64 * G + tid;
+    for (int n = 0; n < units; ++n, x += U) {
 #pragma unroll
-  for (int x = 32; x > 0; x >>= 1) s += __shfl_xor(s, x);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    s = 0.0f;
-    for (int i = 0; i < 16; ++i) s += part[i];
-    a.d_lambda[blockIdx.x] = (a.accumulate ? a.d_lambda[blockIdx.x] : 0.0f) - s;
+      for (int J = 0; J < 4; ++J) {
+        const float4 v = x[J * 64 * G];
+        s[4 * J] += v.x; s[4 * J + 1] += v.y; s[4 * J + 2] += v.z; s[4 * J + 3] += v.w;
+      }
+    }
   }
+  if (kw >= a.N) return;
+  const long c = a.M + (long)(col < DB ? kh : a.kv + kh) * D + 32 * (col % DB);
+  store_cols(a.d_qkv + ((long)sq * a.N + kw) * a.W + c, s, lane >> 5, col < DB ? a.rs : 1.0f);
 }
 
 DiffArgs diff_args(const DiffShape& m, int T) {
@@ -600,18 +799,6 @@ DiffArgs diff_args(const DiffShape& m, int T) {
   a.rs = 1.0f / sqrtf((float)(m.D / 2));
   return a;
 }
-
-#define FLOWMOE_DIFF_LAUNCH(KERNEL, blocks, threads)                                        \
-  do {                                                                                       \
-    const dim3 g((unsigned)(blocks)), b(threads);                                            \
-    if (m.D == 128) {                                                                        \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true>), g, b, 0, st, a);                 \
-      else hipLaunchKernelGGL((KERNEL<128, false>), g, b, 0, st, a);                         \
-    } else {                                                                                 \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true>), g, b, 0, st, a);                  \
-      else hipLaunchKernelGGL((KERNEL<64, false>), g, b, 0, st, a);                          \
-    }                                                                                        \
-  } while (0)
 
 long tiles(const DiffArgs& a, int heads, int rows) {
   return (long)((a.N + rows - 1) / rows) * heads * a.nseq;
@@ -661,9 +848,106 @@ void launch_fwd_variant(int v, const DiffShape& m, const DiffArgs& a, hipStream_
   else launch_fwd<D, 8, 1>(m, a, st);
 }
 
+template <int D, int NW, int S>
+void launch_dq(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
+  const dim3 g((unsigned)tiles(a, a.heads, 32 * NW / S)), b(64 * NW);
+  if (m.causal) hipLaunchKernelGGL((diff_dq_kernel<D, true, NW, S>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((diff_dq_kernel<D, false, NW, S>), g, b, 0, st, a);
+}
+
+// dQ blocks by the launch: 0: one wave of 32 queries (sequences of at most 32); four waves
+// that share 1: 32 queries, 2: 64, 3: 128. us of the whole backward with 1, 2, 3: 2 x 512, 8
+// heads of 64, causal 34, 36, 42; 1 x 2048, heads of 128, causal, 4 heads 71, 75, 100; 16 on 4
+// heads 176, 139, 158; 32 heads 301, 208, 209; 16 x 500, 16 on 8 heads of 64 119, 95, 91; 4 x
+// 4096, 32 heads of 128, causal 3610, 2460, 2270. 700 x 16, 4 heads of 64, variants 0, 3: 42,
+// 50.
+int dq_variant(const DiffShape& m, const DiffArgs& a) {
+  if (m.N <= 32) return 0;
+  const long b32 = tiles(a, a.heads, 32);
+  return b32 <= 256 ? 1 : b32 <= 2048 ? 2 : 3;
+}
+
+template <int D>
+void launch_dq_variant(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
+  const int v = dq_variant(m, a);
+  if (v == 0) launch_dq<D, 1, 1>(m, a, st);
+  else if (v == 1) launch_dq<D, 4, 4>(m, a, st);
+  else if (v == 2) launch_dq<D, 4, 2>(m, a, st);
+  else launch_dq<D, 4, 1>(m, a, st);
+}
+
+// dK and dV by the launch: blocks of 32 G keys and 32 S queries a step. A block's walk over
+// the queries (a step is about 1 us for a wave alone on its SIMD) is the time of a small
+// call, so its waves share the queries there; large ones are better served by tiles that
+// more keys share. Query tiles of 64 and 128 rows of heads of 128 leave a CU one
+// block, so those keep {4, 1} earlier and are cut into units instead. us of {1, 4}, {2, 2},
+// {4, 1}: heads of 64: 2 x 512, 8 heads, causal 19, 23, 32; 4 x 1024, 8 heads 59, 53, 78;
+// 16 x 500, 16 heads (8) 95, 86, 92; 4 x 4096, 24 heads, causal 1170, 1042, 1012; heads of
+// 128: 1 x 2048, 4 heads, causal 72, 79, 74; 8 x 256, 8 heads 38, 28, 35; 20 x 200, 8 heads
+// (4) 78, 68, 61; 1 x 2048, 16 heads (4), causal 173, 153, 134.
+struct KeyTile {
+  int G, S;
+};
+KeyTile key_tile(const DiffShape& m, const DiffArgs& a) {
+  if (m.N <= 32) return {1, 1};
+  if (tiles(a, a.heads, 32) <= 256) return {1, 4};
+  if (m.D == 64) return tiles(a, a.kv, 128) < 1024 ? KeyTile{2, 2} : KeyTile{4, 1};
+  // 128 keys by 32 queries: up to three such steps for each of 512 resident blocks
+  const long n = (m.N + 31) / 32, steps = tiles(a, a.heads, 128) * (m.causal ? (n + 1) / 2 : n);
+  return steps <= 3 * 512 ? KeyTile{2, 2} : KeyTile{4, 1};
+}
+
+// Units of dK and dV: sets a.unit and a.units. Cut where the longest block has more than
+// twice the steps that every one of 768 would have (512 are resident): few key heads with
+// large groups, long causal sequences. 2 x 2031 tokens, 16 heads on 4 of 128, causal, uncut
+// 396 us, units of 1/512, 1/768 and 1/1024 of the steps 228, 201 and 205 (the whole
+// backward); 1 x 4096, 8 on 2 heads 789, 236, 211, 217. Units below 8 steps lose more to
+// their partial sums (1 x 2048, 4 heads: 88 for 4 steps, 71 for 8).
+void cut_units(const DiffShape& m, DiffArgs& a) {
+  const KeyTile k = key_tile(m, a);
+  const int group = m.heads / m.kv, KB = 32 * k.G, QT = 32 * k.S, nt = (m.N + KB - 1) / KB;
+  const long per = (long)m.kv * a.nseq;
+  auto steps = [&](int kt) { return (long)group * ((m.N - (m.causal ? KB * kt : 0) + QT - 1) / QT); };
+  a.unit = a.units = 0;
+  long all = 0;
+  for (int kt = 0; kt < nt; ++kt) all += steps(kt);
+  const long unit = std::max<long>(all * per / 768, 8);
+  if (steps(0) <= 2 * unit) return;
+  a.unit = (int)unit;
+  for (int kt = 0; kt < nt; ++kt) a.units += (int)((steps(kt) + unit - 1) / unit);
+}
+
+template <int D, int G, int S>
+hipError_t launch_dkdv(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
+  const long n = a.unit > 0 ? (long)a.units * a.kv * a.nseq : tiles(a, a.kv, 32 * G);
+  const hipError_t e = traced(FLOWMOE_K_DIFF_BWD_DKDV, st, [&] {
+    const dim3 g((unsigned)(n + a.heads)), b(64 * G * S);
+    if (m.causal) hipLaunchKernelGGL((diff_dkdv_kernel<D, true, G * S, S>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((diff_dkdv_kernel<D, false, G * S, S>), g, b, 0, st, a);
+  });
+  if (e != hipSuccess || a.unit == 0) return e;
+  return traced(FLOWMOE_K_DIFF_JOIN, st, [&] {
+    const dim3 g((unsigned)(tiles(a, a.kv, 32 * G) * (2 * D / 32))), b(64 * G);
+    if (m.causal) hipLaunchKernelGGL((diff_join_kernel<D, true, G, S>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((diff_join_kernel<D, false, G, S>), g, b, 0, st, a);
+  });
+}
+
+template <int D>
+hipError_t launch_dkdv_variant(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
+  const KeyTile k = key_tile(m, a);
+  if (k.G == 4) return launch_dkdv<D, 4, 1>(m, a, st);
+  if (k.G == 2) return launch_dkdv<D, 2, 2>(m, a, st);
+  return k.S == 4 ? launch_dkdv<D, 1, 4>(m, a, st) : launch_dkdv<D, 1, 1>(m, a, st);
+}
+
 }  // namespace
 
-size_t diff_attn_ws_bytes(const DiffShape&, int) { return 0; }
+size_t diff_attn_ws_bytes(const DiffShape& m, int T) {
+  DiffArgs a = diff_args(m, T);
+  cut_units(m, a);
+  return align256((size_t)a.units * m.kv * a.nseq * 32 * key_tile(m, a).G * 2 * m.D * sizeof(float));
+}
 
 hipError_t launch_diff_attn_fwd(const DiffShape& m, int T, const void* qkv, const float* lambda,
                                 const int32_t* lens, void* out, void* out2, float* lse,
@@ -692,7 +976,6 @@ hipError_t launch_diff_attn_bwd(const DiffShape& m, int T, const void* qkv, cons
                                 const int32_t* lens, const void* o, const void* o2,
                                 const float* lse, const void* d_o, void* d_qkv, float* delta,
                                 float* d_lambda, int accumulate, void* ws, hipStream_t st) {
-  (void)ws;
   DiffArgs a = diff_args(m, T);
   a.qkv = static_cast<const bf16_t*>(qkv);
   a.lambda = lambda;
@@ -705,18 +988,17 @@ hipError_t launch_diff_attn_bwd(const DiffShape& m, int T, const void* qkv, cons
   a.delta = delta;
   a.d_lambda = d_lambda;
   a.accumulate = accumulate;
-  hipError_t e = hipSuccess;
+  a.part = static_cast<float*>(ws);
   if (T > 0) {
-    e = traced(FLOWMOE_K_DIFF_BWD_DQ, st,
-               [&] { FLOWMOE_DIFF_LAUNCH(diff_dq_kernel, tiles(a, a.heads, 128), 256); });
-    if (e != hipSuccess) return e;
-    e = traced(FLOWMOE_K_DIFF_BWD_DKDV, st,
-               [&] { FLOWMOE_DIFF_LAUNCH(diff_dkdv_kernel, tiles(a, a.kv, 128), 256); });
+    const hipError_t e = traced(FLOWMOE_K_DIFF_BWD_DQ, st, [&] {
+      if (m.D == 128) launch_dq_variant<128>(m, a, st);
+      else launch_dq_variant<64>(m, a, st);
+    });
     if (e != hipSuccess) return e;
   }
-  return traced(FLOWMOE_K_DIFF_JOIN, st, [&] {
-    hipLaunchKernelGGL(diff_dlambda_kernel, dim3(a.heads), dim3(1024), 0, st, a);
-  });
+  // (without tokens: dlambda alone)
+  cut_units(m, a);
+  return m.D == 128 ? launch_dkdv_variant<128>(m, a, st) : launch_dkdv_variant<64>(m, a, st);
 }
 
 }  // namespace flowmoe

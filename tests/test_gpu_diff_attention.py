@@ -103,6 +103,18 @@ CASES = [
     (2, 520, 24, 8, 64, True, None),
     # lengths outside 0 .. seq_len are cut
     (3, 70, 2, 1, 64, True, [-5, 1000, 70]),
+    # blocks of the large launches, and of the backward's units: many heads, few key heads,
+    # long sequences (few steps of a unit, a short last one, units past a valid length)
+    (9, 1030, 16, 4, 128, True, [1030, 1, 0, 897, 1024, 129, 1029, 500, 64]),
+    (8, 1030, 16, 16, 64, False, [1030, 1000, 96, 897, 0, 31, 1029, 500]),
+    (1, 2100, 8, 1, 128, True, [2090]),
+    (1, 2100, 2, 1, 64, True, None),
+    (2, 700, 12, 4, 64, False, [700, 450]),
+    (2, 700, 12, 2, 128, False, None),
+    (3, 600, 3, 3, 128, True, [600, 2, 333]),
+    # sequences of one tile
+    (300, 20, 3, 3, 64, True, None),
+    (200, 32, 4, 2, 128, False, [n % 33 for n in range(200)]),
     # around the tiles: one, two and three of 64 or 32 rows, a row short, whole, a row over
     *[(2, n, 1, 1, d, c, None) for n in (31, 32, 33, 63, 64, 65, 129) for d in (64, 128)
       for c in (False, True)],

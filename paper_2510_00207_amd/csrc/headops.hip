@@ -8,6 +8,13 @@
 namespace flowmoe {
 namespace {
 
+// Non-temporal stores, for calls that move at least 256 MB: their lines would evict, from
+// the Infinity Cache, input that is still to be read. us, cached and non-temporal, with new
+// inputs each pass: 537 MB of rotary positions 110, 108; 402 MB of the norm's backward 81,
+// 80; 268 MB of its forward 51, 49; 50 MB of positions 10.3, 11.3. (A copy of 1 GB reaches
+// 5.05 TB/s here, which is 106, 80 and 53 us for the three large ones.)
+bool stream_past_caches(long bytes) { return bytes >= (256L << 20); }
+
 // ---------------------------------------------------------------------------
 // rotary positions
 // ---------------------------------------------------------------------------
@@ -37,113 +44,102 @@ __device__ __forceinline__ double pair_turns(const RopeArgs& a, int i) {
   return f * a.scale;
 }
 
-constexpr int kRopeTokens = 4;  // tokens of a block
-
-// 8 elements at any element's address (half of rot_dim need be no multiple of a vector;
-// global memory takes 16-byte accesses there)
-template <typename T>
-struct __attribute__((packed, aligned(sizeof(T)))) Any8 {
-  u32x4v_t v[sizeof(T) / 2];
+// A block's place: n threads hold the vectors (8 columns) of a head, `per` heads are held
+// at once, of `tps` tokens; a block has `tokens` tokens.
+struct RopeTile {
+  int n, per, tps, tokens;
 };
-__device__ __forceinline__ void load8_any(const bf16_t* p, float v[8]) {
-  raw8_f32(Raw8b{reinterpret_cast<const Any8<bf16_t>*>(p)->v[0]}, v);
-}
-__device__ __forceinline__ void load8_any(const float* p, float v[8]) {
-  const Any8<float>* q = reinterpret_cast<const Any8<float>*>(p);
-  raw8_f32(Raw8f{q->v[0], q->v[1]}, v);
-}
-__device__ __forceinline__ void store8_any(bf16_t* p, const float v[8]) {
-  reinterpret_cast<Any8<bf16_t>*>(p)->v[0] =
-      u32x4v_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-               pack_bf16x2(v[6], v[7])};
-}
-__device__ __forceinline__ void store8_any(float* p, const float v[8]) {
-  Any8<float>* q = reinterpret_cast<Any8<float>*>(p);
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    q->v[i] = u32x4v_t{__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
-                       __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
+__host__ __device__ __forceinline__ RopeTile rope_tile(int D, int heads) {
+  RopeTile r;
+  r.n = D / 8;
+  r.per = 256 / r.n;
+  r.tps = heads < r.per ? r.per / heads : 1;
+  r.tokens = r.tps > 4 ? r.tps : 4;
+  return r;
 }
 
-// A block's threads first make the cosines and sines of its tokens, once for all heads,
-// then walk the heads in pieces. HALF: 8 pairs, 8 columns of each half of rot_dim, and
-// then the copied columns by eights; the last piece of either may be short. Pairs: 8
-// columns, of which those past rot_dim turn by nothing.
-template <typename T, bool HALF>
+// The cosines and sines of a block's tokens come first, once for all heads. Then a thread
+// holds the same 8 columns of one head after another. With pairs (2 i, 2 i + 1) a column's
+// partner is its neighbour; with halves (HALF) it is half a rotation away, anywhere in
+// another thread's vector, and taken from LDS: element i of thread k lies at i * 256 + k
+// there, and the cosines likewise, so that a wave's reads, which all have one distance,
+// touch every bank once. 16384 tokens of 64 heads of 128, bf16: 537 MB in 108 us, 5.0 TB/s,
+// which is what a large copy reaches; with 122 columns turned the same (409 us with
+// 16-byte accesses to either half where it starts, a thread both).
+template <typename T, bool HALF, bool NT>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  extern __shared__ float2 table[];  // kRopeTokens x (rot / 2, rounded up to 4)
-  const int half = a.rot / 2, tw = (half + 3) & ~3, t0 = blockIdx.x * kRopeTokens,
-            nt = min(kRopeTokens, a.T - t0);
-  for (int i = threadIdx.x; i < tw; i += 256) {
-    const double f = pair_turns(a, i);
-    for (int t = 0; t < nt; ++t) {
-      const int p = a.pos ? a.pos[t0 + t] : (t0 + t) % a.seq_len;
-      const double turns = (double)p * f;
-      float s, c;
-      sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
-      table[t * tw + i] = i < half ? make_float2(c * a.mscale, s * a.mscale * a.sign)
-                                   : make_float2(1.0f, 0.0f);
-    }
+  extern __shared__ float2 table[];  // tokens x 8 x (pairs / 8, rounded up)
+  __shared__ float stage[HALF ? 2 : 1][HALF ? 8 * 256 : 1];
+  const RopeTile r = rope_tile(a.D, a.heads);
+  const int half = a.rot / 2, tw = (half + 7) / 8, t0 = blockIdx.x * r.tokens,
+            nt = min(r.tokens, a.T - t0), tid = threadIdx.x;
+  for (int k = tid; k < half * nt; k += 256) {
+    const int i = k % half, t = k / half;
+    const int p = a.pos ? a.pos[t0 + t] : (t0 + t) % a.seq_len;
+    const double turns = (double)p * pair_turns(a, i);
+    float s, c;
+    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+    table[(t * 8 + i % 8) * tw + i / 8] = make_float2(c * a.mscale, s * a.mscale * a.sign);
   }
   __syncthreads();
-  // a head's pieces: np of turned columns, the others copied
-  const int np = HALF ? (half + 7) / 8 : (a.rot + 7) / 8;
-  const int rest = HALF ? a.rot : 8 * np;  // the first column that is only copied
-  const int n = np + (a.copy ? (a.D - rest + 7) / 8 : 0);
-  for (int k = threadIdx.x; k < n * a.heads * nt; k += 256) {
-    const int c = k % n, r = k / n, hd = r % a.heads, t = r / a.heads;
-    const long at = (long)(t0 + t) * a.ld + (long)hd * a.D;
-    const T* x = static_cast<const T*>(a.x) + at;
-    T* y = static_cast<T*>(a.y) + at;
-    float u[8], p[8];
-    if (c >= np) {
-      const int e = rest + 8 * (c - np);
-      if (e + 8 <= a.D) {
-        load8_any(x + e, u);
-        store8_any(y + e, u);
-      } else {
-        for (int i = e; i < a.D; ++i) y[i] = x[i];
-      }
-      continue;
+  const int c = tid % r.n, h = tid / r.n;
+  const int h0 = r.tps > 1 ? h % a.heads : h, tk = r.tps > 1 ? h / a.heads : 0;
+  // (threads past the heads, and with y = x those of columns that stay as they are)
+  const bool mine = h < r.per && tk < r.tps && (a.copy || 8 * c < a.rot);
+  int from[8];  // where the partners lie
+  if constexpr (HALF) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int e = 8 * c + i, q = e < half ? e + half : e - half;
+      from[i] = e < a.rot ? (q % 8) * 256 + tid - c + q / 8 : i * 256 + tid;
     }
-    const float2* cs = table + t * tw + c * (HALF ? 8 : 4);
-    if constexpr (HALF) {
-      if (8 * c + 8 <= half) {
-        float v[8], q[8];
-        load8(x + 8 * c, u);
-        load8_any(x + half + 8 * c, v);
+  }
+  int step = 0;
+  for (int tb = 0; tb < nt; tb += r.tps) {
+    const int t = tb + tk;
+    const bool live = mine && t < nt;
+    float2 cs[8];  // by which the thread's columns and their partners are multiplied
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          p[i] = u[i] * cs[i].x - v[i] * cs[i].y;
-          q[i] = u[i] * cs[i].y + v[i] * cs[i].x;
-        }
-        store8(y + 8 * c, p);
-        store8_any(y + half + 8 * c, q);
+    for (int i = 0; i < 8; ++i) {
+      const int e = 8 * c + i, pair = HALF ? (e < half ? e : e - half) : e / 2;
+      const bool turn = live && e < a.rot;
+      cs[i] = turn ? table[(t * 8 + pair % 8) * tw + pair / 8] : make_float2(1.0f, 0.0f);
+      if (HALF ? e < half : i % 2 == 0) cs[i].y = -cs[i].y;
+    }
+    for (int g = 0; g < a.heads; g += r.tps > 1 ? a.heads : r.per, ++step) {
+      const bool in = live && g + h0 < a.heads;
+      const long at = (long)(t0 + t) * a.ld + (long)(g + h0) * a.D + 8 * c;
+      float u[8] = {}, p[8];
+      if (in) load8(static_cast<const T*>(a.x) + at, u);
+      if constexpr (HALF) {
+        float* s = stage[step & 1];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i * 256 + tid] = u[i];
+        __syncthreads();  // (and the reads of the other stage, a step ago, are done)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = u[i] * cs[i].x + s[from[i]] * cs[i].y;
       } else {
-        for (int i = 8 * c; i < half; ++i, ++cs) {
-          const float v = Elem<T>::load(x + i), w = Elem<T>::load(x + half + i);
-          Elem<T>::store(y + i, v * cs->x - w * cs->y);
-          Elem<T>::store(y + half + i, v * cs->y + w * cs->x);
-        }
-      }
-    } else {
-      load8(x + 8 * c, u);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        p[2 * i] = u[2 * i] * cs[i].x - u[2 * i + 1] * cs[i].y;
-        p[2 * i + 1] = u[2 * i] * cs[i].y + u[2 * i + 1] * cs[i].x;
+        for (int i = 0; i < 8; ++i) p[i] = u[i] * cs[i].x + u[i ^ 1] * cs[i].y;
       }
-      store8(y + 8 * c, p);
+      if (in) store8_t<NT>(static_cast<T*>(a.y) + at, p);
     }
   }
 }
 
 template <typename T>
 void run_rope(const RopeArgs& a, bool half_layout, hipStream_t st) {
-  const dim3 g((unsigned)((a.T + kRopeTokens - 1) / kRopeTokens)), b(256);
-  const size_t lds = (size_t)kRopeTokens * ((a.rot / 2 + 3) & ~3) * sizeof(float2);
-  if (half_layout) hipLaunchKernelGGL((rope_kernel<T, true>), g, b, lds, st, a);
-  else hipLaunchKernelGGL((rope_kernel<T, false>), g, b, lds, st, a);
+  const RopeTile r = rope_tile(a.D, a.heads);
+  const dim3 g((unsigned)((a.T + (long)r.tokens - 1) / r.tokens)), b(256);
+  const size_t lds = (size_t)r.tokens * 8 * ((a.rot / 2 + 7) / 8) * sizeof(float2);
+  const bool nt = stream_past_caches(2L * a.T * a.heads * a.D * (long)sizeof(T));
+  if (half_layout) {
+    if (nt) hipLaunchKernelGGL((rope_kernel<T, true, true>), g, b, lds, st, a);
+    else hipLaunchKernelGGL((rope_kernel<T, true, false>), g, b, lds, st, a);
+  } else {
+    if (nt) hipLaunchKernelGGL((rope_kernel<T, false, true>), g, b, lds, st, a);
+    else hipLaunchKernelGGL((rope_kernel<T, false, false>), g, b, lds, st, a);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -166,8 +162,10 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// L lanes (a power of two) hold a head's D <= 8 L elements, 8 each
-template <typename T, int L>
+// L lanes (a power of two) hold a head's D <= 8 L elements, 8 each; a block's groups walk
+// the rows. 16384 tokens of 32 heads of 128, bf16: 268 MB in 49 us, 5.5 TB/s, the rate of a
+// large copy.
+template <typename T, int L, bool NT>
 __global__ __launch_bounds__(256) void head_norm_kernel(NormArgs a) {
   const int c = 8 * (threadIdx.x % L);
   const bool in = c < a.D;
@@ -184,13 +182,14 @@ __global__ __launch_bounds__(256) void head_norm_kernel(NormArgs a) {
     s = rsqrtf(group_sum<L>(s) * rd + a.eps);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= s * g[i];
-    if (in) store8(static_cast<T*>(a.y) + r * a.D + c, v);
+    if (in) store8_t<NT>(static_cast<T*>(a.y) + r * a.D + c, v);
   }
 }
 
 // dx = r (u - x r^2 mean(u x)), u = scale gain dy; dgain's sums over the block's rows go
-// to `part`, in a fixed order
-template <typename T, int L>
+// to `part`, in a fixed order. As above 402 MB in 80 us, 5.0 TB/s, with the join's 5 us; 512,
+// 1024 and 2048 blocks 111, 82 and 91.
+template <typename T, int L, bool NT>
 __global__ __launch_bounds__(256) void head_norm_bwd_kernel(NormArgs a) {
   __shared__ float sums[256 * 8];
   const int c = 8 * (threadIdx.x % L);
@@ -218,7 +217,7 @@ __global__ __launch_bounds__(256) void head_norm_bwd_kernel(NormArgs a) {
       dg[i] += d[i] * (v[i] * s);
       v[i] = s * (d[i] * g[i] - v[i] * p);
     }
-    if (in) store8(static_cast<T*>(a.y) + r * a.D + c, v);
+    if (in) store8_t<NT>(static_cast<T*>(a.y) + r * a.D + c, v);
   }
   if (a.part == nullptr) return;
 #pragma unroll
@@ -254,13 +253,17 @@ int norm_blocks(long rows, int D) {
   return (int)(need < 1024 ? need : 1024);
 }
 
-#define FLOWMOE_NORM_LAUNCH(KERNEL, T)                                                    \
-  switch (norm_lanes(a.D)) {                                                               \
-    case 4: hipLaunchKernelGGL((KERNEL<T, 4>), g, b, 0, st, a); break;                     \
-    case 8: hipLaunchKernelGGL((KERNEL<T, 8>), g, b, 0, st, a); break;                     \
-    case 16: hipLaunchKernelGGL((KERNEL<T, 16>), g, b, 0, st, a); break;                   \
-    case 32: hipLaunchKernelGGL((KERNEL<T, 32>), g, b, 0, st, a); break;                   \
-    default: hipLaunchKernelGGL((KERNEL<T, 64>), g, b, 0, st, a); break;                   \
+#define FLOWMOE_NORM_CASE(KERNEL, T, L)                                          \
+  if (nt) hipLaunchKernelGGL((KERNEL<T, L, true>), g, b, 0, st, a);              \
+  else hipLaunchKernelGGL((KERNEL<T, L, false>), g, b, 0, st, a);                \
+  break
+#define FLOWMOE_NORM_LAUNCH(KERNEL, T)                                           \
+  switch (norm_lanes(a.D)) {                                                     \
+    case 4: FLOWMOE_NORM_CASE(KERNEL, T, 4);                                     \
+    case 8: FLOWMOE_NORM_CASE(KERNEL, T, 8);                                     \
+    case 16: FLOWMOE_NORM_CASE(KERNEL, T, 16);                                   \
+    case 32: FLOWMOE_NORM_CASE(KERNEL, T, 32);                                   \
+    default: FLOWMOE_NORM_CASE(KERNEL, T, 64);                                   \
   }
 
 }  // namespace
@@ -268,7 +271,8 @@ int norm_blocks(long rows, int D) {
 hipError_t launch_rope(const RopeShape& m, int dtype, int T, long ld, bool back, const void* x,
                        const int32_t* pos, void* y, hipStream_t st) {
   if (T == 0) return hipSuccess;
-  if ((T + kRopeTokens - 1) / kRopeTokens > kMaxBlocks) return hipErrorInvalidConfiguration;
+  const int tokens = rope_tile(m.D, m.heads).tokens;
+  if ((T + (long)tokens - 1) / tokens > kMaxBlocks) return hipErrorInvalidConfiguration;
   RopeArgs a = {};
   a.x = x;
   a.y = y;
@@ -311,6 +315,7 @@ hipError_t launch_head_norm_fwd(const NormShape& m, int dtype, int T, const void
   a.eps = m.eps;
   a.scale = m.scale;
   const dim3 g(norm_blocks(a.rows, a.D)), b(256);
+  const bool nt = stream_past_caches(2 * a.rows * a.D * (long)esize(dtype));
   return traced(FLOWMOE_K_HEAD_NORM, st, [&] {
     if (dtype == FLOWMOE_BF16) FLOWMOE_NORM_LAUNCH(head_norm_kernel, bf16_t)
     else FLOWMOE_NORM_LAUNCH(head_norm_kernel, float)
@@ -333,6 +338,7 @@ hipError_t launch_head_norm_bwd(const NormShape& m, int dtype, int T, const void
   const int n = norm_blocks(a.rows, a.D);
   if (T > 0) {
     const dim3 g(n), b(256);
+    const bool nt = stream_past_caches(3 * a.rows * a.D * (long)esize(dtype));
     const hipError_t e = traced(FLOWMOE_K_HEAD_NORM_BWD, st, [&] {
       if (dtype == FLOWMOE_BF16) FLOWMOE_NORM_LAUNCH(head_norm_bwd_kernel, bf16_t)
       else FLOWMOE_NORM_LAUNCH(head_norm_bwd_kernel, float)

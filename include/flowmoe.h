@@ -574,6 +574,66 @@ flowmoe_status_t flowmoe_diff_attention_bwd(const flowmoe_shape_t* shape,
                                             float* d_lambda, int32_t accumulate, void* ws,
                                             size_t ws_bytes, hipStream_t stream);
 
+/* ---- the block's attention with the three ------------------------------------- */
+
+/* Buffers of flowmoe_diff_mha_fwd / _bwd, W = M + 2 * kv_heads * head_dim. */
+typedef struct {
+  /* parameters and inputs */
+  const void* in;           /* T x M: the block input I */
+  const void* w_qkv;        /* M x W: [W^Q | W^K | W^V] side by side */
+  const void* w_o;          /* M x M */
+  const float* lambda;      /* heads */
+  const float* gain;        /* head_dim, nullable (ones) */
+  const int32_t* positions; /* T, nullable (flowmoe_rope_fwd) */
+  const int32_t* lens;      /* T / seq_len, nullable (flowmoe_diff_attention_fwd) */
+  /* forward (all but out kept for the backward) */
+  void* qkv;                /* T x W: Q and K turned */
+  void* attn;               /* T x M */
+  void* attn2;              /* T x M */
+  float* lse;               /* 2 x heads x T */
+  void* normed;             /* T x M */
+  void* out;                /* T x M: I' */
+  /* backward */
+  const void* d_out;        /* T x M */
+  void* d_attn;             /* T x M */
+  void* d_qkv;              /* T x W */
+  float* delta;             /* 2 x heads x T */
+  void* d_in;               /* T x M */
+  float* dw_qkv;            /* M x W */
+  float* dw_o;              /* M x M */
+  float* d_lambda;          /* heads */
+  float* dgain;             /* head_dim, nullable */
+  /* scratch of the backward: flowmoe_diff_mha_ws_bytes bytes */
+  void* ws;
+  size_t ws_bytes;
+} flowmoe_diff_mha_bufs_t;
+
+/* In the place of flowmoe_mha_fwd: qkv = in [W^Q | W^K | W^V], Q and K turned by
+ * their positions (rope: heads = 2 * (heads + kv_heads) of head_dim / 2 columns, each
+ * map's queries and keys for themselves, seq_len as diff's; null: not turned), the
+ * differential attention, the head norm (norm: diff's heads and head_dim), out =
+ * normed W^O. bf16 only. */
+flowmoe_status_t flowmoe_diff_mha_fwd(const flowmoe_shape_t* shape,
+                                      const flowmoe_diff_shape_t* diff,
+                                      const flowmoe_rope_shape_t* rope,
+                                      const flowmoe_norm_shape_t* norm,
+                                      const flowmoe_diff_mha_bufs_t* bufs, hipStream_t stream);
+
+/* Bytes of scratch flowmoe_diff_mha_bwd needs (0 for an invalid shape). */
+size_t flowmoe_diff_mha_ws_bytes(const flowmoe_shape_t* shape, const flowmoe_diff_shape_t* diff,
+                                 const flowmoe_norm_shape_t* norm);
+
+/* Its backward: d_attn = the norm's gradient of d_out W^O^T, the attention backward
+ * (d_qkv, delta, d_lambda), Q's and K's columns of d_qkv turned back, d_in = d_qkv [W^Q |
+ * W^K | W^V]^T, dw_o = normed^T d_out, dw_qkv = in^T d_qkv. With accumulate != 0, dw_qkv,
+ * dw_o, d_lambda and dgain are added to, else overwritten. */
+flowmoe_status_t flowmoe_diff_mha_bwd(const flowmoe_shape_t* shape,
+                                      const flowmoe_diff_shape_t* diff,
+                                      const flowmoe_rope_shape_t* rope,
+                                      const flowmoe_norm_shape_t* norm,
+                                      const flowmoe_diff_mha_bufs_t* bufs, int32_t accumulate,
+                                      hipStream_t stream);
+
 /* ---- the R-chunk two-stream layer (Sec. 3.2, Eqs. 3-6) -------------------- */
 
 /* Buffers of a whole layer over R chunks of shape->T tokens each. Per-token

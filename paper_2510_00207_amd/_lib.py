@@ -74,6 +74,17 @@ class LayerBufs(ctypes.Structure):
     _fields_ = [(n, _VP) for n in _LAYER_FIELDS] + [("ws_bytes", ctypes.c_size_t)]
 
 
+_DIFF_MHA_FIELDS = [
+    "in", "w_qkv", "w_o", "lambda", "gain", "positions", "lens",
+    "qkv", "attn", "attn2", "lse", "normed", "out",
+    "d_out", "d_attn", "d_qkv", "delta", "d_in", "dw_qkv", "dw_o", "d_lambda", "dgain", "ws",
+]
+
+
+class DiffMhaBufs(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in _DIFF_MHA_FIELDS] + [("ws_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -94,6 +105,7 @@ def load():
     SP = ctypes.POINTER(Shape)
     MP = ctypes.POINTER(MhaShape)
     RP, NP, DP = (ctypes.POINTER(c) for c in (RopeShape, NormShape, DiffShape))
+    BP = ctypes.POINTER(DiffMhaBufs)
     sig = {
         "flowmoe_version": ([], ctypes.c_char_p),
         "flowmoe_last_error": ([], ctypes.c_char_p),
@@ -128,6 +140,9 @@ def load():
         "flowmoe_diff_attention_fwd": ([SP, DP] + [P] * 7, I32),
         "flowmoe_diff_attention_ws_bytes": ([SP, DP], SZ),
         "flowmoe_diff_attention_bwd": ([SP, DP] + [P] * 10 + [I32, P, SZ, P], I32),
+        "flowmoe_diff_mha_fwd": ([SP, DP, RP, NP, BP, P], I32),
+        "flowmoe_diff_mha_ws_bytes": ([SP, DP, NP], SZ),
+        "flowmoe_diff_mha_bwd": ([SP, DP, RP, NP, BP, I32, P], I32),
         "flowmoe_layer_fwd": ([SP, I32, ctypes.POINTER(LayerBufs), P, P, P], I32),
         "flowmoe_layer_bwd": ([SP, I32, ctypes.POINTER(LayerBufs), P, P, P], I32),
     }
@@ -355,6 +370,39 @@ def flowmoe_diff_attention_bwd(shape, diff, qkv, lam, lens, attn, attn2, lse, d_
                                              ptr(d_attn), ptr(d_qkv), ptr(delta), ptr(d_lambda),
                                              int(accumulate), ptr(ws), int(ws_bytes),
                                              _stream(stream)))
+
+
+def diff_mha_bufs(**tensors) -> DiffMhaBufs:
+    """DiffMhaBufs from keyword tensors (names of the C struct fields; ``in`` and ``lambda``,
+    which Python keeps for itself, as ``inp`` and ``lam``)."""
+    b = DiffMhaBufs()
+    for name, t in tensors.items():
+        name = {"inp": "in", "lam": "lambda"}.get(name, name)
+        if name == "ws_bytes":
+            b.ws_bytes = int(t)
+        elif name not in _DIFF_MHA_FIELDS:
+            raise KeyError(name)
+        else:
+            setattr(b, name, ptr(t))
+    return b
+
+
+def flowmoe_diff_mha_fwd(shape, diff, rope, norm, bufs, stream=None):
+    _check(load().flowmoe_diff_mha_fwd(ctypes.byref(shape), ctypes.byref(diff),
+                                       None if rope is None else ctypes.byref(rope),
+                                       ctypes.byref(norm), ctypes.byref(bufs), _stream(stream)))
+
+
+def flowmoe_diff_mha_ws_bytes(shape, diff, norm) -> int:
+    return load().flowmoe_diff_mha_ws_bytes(ctypes.byref(shape), ctypes.byref(diff),
+                                            ctypes.byref(norm))
+
+
+def flowmoe_diff_mha_bwd(shape, diff, rope, norm, bufs, accumulate, stream=None):
+    _check(load().flowmoe_diff_mha_bwd(ctypes.byref(shape), ctypes.byref(diff),
+                                       None if rope is None else ctypes.byref(rope),
+                                       ctypes.byref(norm), ctypes.byref(bufs), int(accumulate),
+                                       _stream(stream)))
 
 
 # ---- kernel tracing --------------------------------------------------------------

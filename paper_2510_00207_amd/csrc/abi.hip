@@ -966,6 +966,122 @@ flowmoe_status_t flowmoe_diff_attention_bwd(const flowmoe_shape_t* shape,
 
 namespace {
 
+// the three shapes of flowmoe_diff_mha_*, as one block's
+flowmoe_status_t check_diff_mha(const flowmoe_shape_t* shape, const flowmoe_diff_shape_t* diff,
+                                const flowmoe_rope_shape_t* rope, const flowmoe_norm_shape_t* norm,
+                                DiffShape* m, RopeShape* r, NormShape* n) {
+  flowmoe_status_t st = check_diff(shape, diff, m);
+  if (st != FLOWMOE_OK) return st;
+  st = check_norm(shape, norm, n);
+  if (st != FLOWMOE_OK) return st;
+  if (n->heads != m->heads || n->D != m->D)
+    return fail(FLOWMOE_ERR_INVALID, "norm's heads * head_dim = %d * %d are not diff's %d * %d",
+                n->heads, n->D, m->heads, m->D);
+  const long W = shape->M + 2L * m->kv * m->D;
+  if (W > (1 << 26)) return fail(FLOWMOE_ERR_UNSUPPORTED, "tensor too large");
+  if (rope == nullptr) return FLOWMOE_OK;
+  flowmoe_shape_t row = *shape;
+  row.M = (int32_t)W;
+  st = check_rope(&row, rope, r);
+  if (st != FLOWMOE_OK) return st;
+  if (r->D != m->D / 2 || r->heads != 2 * (m->heads + m->kv))
+    return fail(FLOWMOE_ERR_INVALID,
+                "rope's heads * head_dim = %d * %d are not Q's and K's 2 * (%d + %d) * %d", r->heads,
+                r->D, m->heads, m->kv, m->D / 2);
+  if (r->seq_len != m->N)
+    return fail(FLOWMOE_ERR_INVALID, "rope's seq_len = %d is not diff's %d", r->seq_len, m->N);
+  return FLOWMOE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+flowmoe_status_t flowmoe_diff_mha_fwd(const flowmoe_shape_t* shape,
+                                      const flowmoe_diff_shape_t* diff,
+                                      const flowmoe_rope_shape_t* rope,
+                                      const flowmoe_norm_shape_t* norm,
+                                      const flowmoe_diff_mha_bufs_t* b, hipStream_t stream) {
+  DiffShape m;
+  RopeShape r;
+  NormShape n;
+  flowmoe_status_t st = check_diff_mha(shape, diff, rope, norm, &m, &r, &n);
+  if (st != FLOWMOE_OK) return st;
+  if (b == nullptr) return fail(FLOWMOE_ERR_INVALID, "bufs is null");
+  if (shape->T == 0) return ok();
+  REQUIRE_T(b->in, "bufs->in");
+  REQUIRE_T(b->w_qkv, "bufs->w_qkv");
+  REQUIRE_T(b->w_o, "bufs->w_o");
+  REQUIRE_F(b->lambda, "bufs->lambda");
+  CHECK_A4(b->gain, "bufs->gain");
+  CHECK_A4(b->positions, "bufs->positions");
+  CHECK_A4(b->lens, "bufs->lens");
+  REQUIRE_T(b->qkv, "bufs->qkv");
+  REQUIRE_T(b->attn, "bufs->attn");
+  REQUIRE_T(b->attn2, "bufs->attn2");
+  REQUIRE_F(b->lse, "bufs->lse");
+  REQUIRE_T(b->normed, "bufs->normed");
+  REQUIRE_T(b->out, "bufs->out");
+  return hip_status(launch_diff_mha_fwd(m, rope ? &r : nullptr, n, shape->T, *b, stream),
+                    "flowmoe_diff_mha_fwd");
+}
+
+size_t flowmoe_diff_mha_ws_bytes(const flowmoe_shape_t* shape, const flowmoe_diff_shape_t* diff,
+                                 const flowmoe_norm_shape_t* norm) {
+  DiffShape m;
+  NormShape n;
+  if (check_diff_mha(shape, diff, nullptr, norm, &m, nullptr, &n) != FLOWMOE_OK) return 0;
+  return diff_mha_ws_bytes(m, n, shape->T);
+}
+
+flowmoe_status_t flowmoe_diff_mha_bwd(const flowmoe_shape_t* shape,
+                                      const flowmoe_diff_shape_t* diff,
+                                      const flowmoe_rope_shape_t* rope,
+                                      const flowmoe_norm_shape_t* norm,
+                                      const flowmoe_diff_mha_bufs_t* b, int32_t accumulate,
+                                      hipStream_t stream) {
+  DiffShape m;
+  RopeShape r;
+  NormShape n;
+  flowmoe_status_t st = check_diff_mha(shape, diff, rope, norm, &m, &r, &n);
+  if (st != FLOWMOE_OK) return st;
+  if (b == nullptr) return fail(FLOWMOE_ERR_INVALID, "bufs is null");
+  REQUIRE_T(b->dw_qkv, "bufs->dw_qkv");
+  REQUIRE_T(b->dw_o, "bufs->dw_o");
+  REQUIRE_F(b->d_lambda, "bufs->d_lambda");
+  CHECK_A4(b->dgain, "bufs->dgain");
+  CHECK_A4(b->gain, "bufs->gain");
+  CHECK_A4(b->positions, "bufs->positions");
+  CHECK_A4(b->lens, "bufs->lens");
+  if (shape->T > 0) {
+    REQUIRE_T(b->in, "bufs->in");
+    REQUIRE_T(b->w_qkv, "bufs->w_qkv");
+    REQUIRE_T(b->w_o, "bufs->w_o");
+    REQUIRE_F(b->lambda, "bufs->lambda");
+    REQUIRE_T(b->qkv, "bufs->qkv");
+    REQUIRE_T(b->attn, "bufs->attn");
+    REQUIRE_T(b->attn2, "bufs->attn2");
+    REQUIRE_F(b->lse, "bufs->lse");
+    REQUIRE_T(b->normed, "bufs->normed");
+    REQUIRE_T(b->d_out, "bufs->d_out");
+    REQUIRE_T(b->d_attn, "bufs->d_attn");
+    REQUIRE_T(b->d_qkv, "bufs->d_qkv");
+    REQUIRE_F(b->delta, "bufs->delta");
+    REQUIRE_T(b->d_in, "bufs->d_in");
+  }
+  const size_t need = diff_mha_ws_bytes(m, n, shape->T);
+  st = check_ws(b->ws, b->ws_bytes, need, "flowmoe_diff_mha_bwd");
+  if (st != FLOWMOE_OK) return st;
+  if (need > 0) REQUIRE_T(b->ws, "bufs->ws");
+  return hip_status(launch_diff_mha_bwd(m, rope ? &r : nullptr, n, shape->T, *b, accumulate != 0,
+                                        stream),
+                    "flowmoe_diff_mha_bwd");
+}
+
+}  // extern "C"
+
+namespace {
+
 struct Chunk {
   const char *x, *dy;
   float *logits, *w, *dw, *dl;

@@ -448,6 +448,13 @@ hipError_t launch_head_norm_bwd(const NormShape& m, int dtype, int T, const void
                                 const float* gain, const void* dy, void* dx, float* dgain,
                                 int accumulate, void* ws, hipStream_t st);
 
+// The block's attention with these (rope null: not turned)
+size_t diff_mha_ws_bytes(const DiffShape& m, const NormShape& n, int T);
+hipError_t launch_diff_mha_fwd(const DiffShape& m, const RopeShape* r, const NormShape& n, int T,
+                               const flowmoe_diff_mha_bufs_t& b, hipStream_t st);
+hipError_t launch_diff_mha_bwd(const DiffShape& m, const RopeShape* r, const NormShape& n, int T,
+                               const flowmoe_diff_mha_bufs_t& b, int accumulate, hipStream_t st);
+
 // Kernel tracing (flowmoe_trace_start): record a begin/end event around a
 // launch when the kind is selected. Defined in abi.hip.
 hipError_t trace_mark(int kind, bool end, hipStream_t st);

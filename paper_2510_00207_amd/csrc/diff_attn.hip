@@ -1001,4 +1001,62 @@ hipError_t launch_diff_attn_bwd(const DiffShape& m, int T, const void* qkv, cons
   return m.D == 128 ? launch_dkdv_variant<128>(m, a, st) : launch_dkdv_variant<64>(m, a, st);
 }
 
+// ---------------------------------------------------------------------------
+// the block's attention: projections, positions, differential attention, head norm
+// ---------------------------------------------------------------------------
+namespace {
+// partial sums of a weight gradient (M x N) whose rows are split
+size_t wgrad_part_bytes(int M, int N, long rows) {
+  const int s = dense_wgrad_splits(M, N, rows);
+  return s > 1 ? (size_t)s * M * N * sizeof(float) : 0;
+}
+}  // namespace
+
+size_t diff_mha_ws_bytes(const DiffShape& m, const NormShape& n, int T) {
+  const int M = m.heads * m.D, W = M + 2 * m.kv * m.D;
+  return align256(std::max(std::max(diff_attn_ws_bytes(m, T), head_norm_ws_bytes(T, n.heads, n.D)),
+                           std::max(wgrad_part_bytes(M, W, T), wgrad_part_bytes(M, M, T))));
+}
+
+hipError_t launch_diff_mha_fwd(const DiffShape& m, const RopeShape* r, const NormShape& n, int T,
+                               const flowmoe_diff_mha_bufs_t& b, hipStream_t st) {
+  if (T == 0) return hipSuccess;
+  const int M = m.heads * m.D, W = M + 2 * m.kv * m.D;
+  hipError_t e = launch_dense_gemm(FLOWMOE_K_ATTN_QKV, T, b.in, M, M, b.w_qkv, W, false, W, b.qkv, W, st);
+  if (e == hipSuccess && r != nullptr)
+    e = launch_rope(*r, FLOWMOE_BF16, T, W, false, b.qkv, b.positions, b.qkv, st);
+  if (e == hipSuccess)
+    e = launch_diff_attn_fwd(m, T, b.qkv, b.lambda, b.lens, b.attn, b.attn2, b.lse, st);
+  if (e == hipSuccess) e = launch_head_norm_fwd(n, FLOWMOE_BF16, T, b.attn, b.gain, b.normed, st);
+  if (e != hipSuccess) return e;
+  return launch_dense_gemm(FLOWMOE_K_ATTN_OUT, T, b.normed, M, M, b.w_o, M, false, M, b.out, M, st);
+}
+
+hipError_t launch_diff_mha_bwd(const DiffShape& m, const RopeShape* r, const NormShape& n, int T,
+                               const flowmoe_diff_mha_bufs_t& b, int accumulate, hipStream_t st) {
+  const int M = m.heads * m.D, W = M + 2 * m.kv * m.D;
+  hipError_t e = hipSuccess;
+  // the gradient of the norm's output, B[k][n] = W^O[n][k]; the norm's backward in its place
+  if (T > 0)
+    e = launch_dense_gemm(FLOWMOE_K_ATTN_DGRAD, T, b.d_out, M, M, b.w_o, M, true, M, b.d_attn, M, st);
+  if (e == hipSuccess)
+    e = launch_head_norm_bwd(n, FLOWMOE_BF16, T, b.attn, b.gain, b.d_attn, b.d_attn, b.dgain,
+                             accumulate, b.ws, st);
+  if (e == hipSuccess)
+    e = launch_diff_attn_bwd(m, T, b.qkv, b.lambda, b.lens, b.attn, b.attn2, b.lse, b.d_attn, b.d_qkv,
+                             b.delta, b.d_lambda, accumulate, b.ws, st);
+  if (e == hipSuccess && r != nullptr)
+    e = launch_rope(*r, FLOWMOE_BF16, T, W, true, b.d_qkv, b.positions, b.d_qkv, st);
+  if (e == hipSuccess && T > 0)
+    e = launch_dense_gemm(FLOWMOE_K_ATTN_DGRAD, T, b.d_qkv, W, W, b.w_qkv, W, true, M, b.d_in, M, st);
+  float* part = static_cast<float*>(b.ws);
+  if (e == hipSuccess)
+    e = launch_dense_wgrad(FLOWMOE_K_ATTN_WGRAD, T, 1, b.normed, M, 0, M, b.d_out, M, 0, M, b.dw_o, M,
+                           accumulate, wgrad_part_bytes(M, M, T) ? part : nullptr, st);
+  if (e == hipSuccess)
+    e = launch_dense_wgrad(FLOWMOE_K_ATTN_WGRAD, T, 1, b.in, M, 0, M, b.d_qkv, W, 0, W, b.dw_qkv, W,
+                           accumulate, wgrad_part_bytes(M, W, T) ? part : nullptr, st);
+  return e;
+}
+
 }  // namespace flowmoe

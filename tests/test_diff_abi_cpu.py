@@ -163,3 +163,59 @@ def test_no_tokens(flowmoe_lib):
     L.flowmoe_diff_attention_fwd(s, d, *[None] * 6, stream=0)
     refused(L.ERR_INVALID, "d_lambda is null", lambda: L.flowmoe_diff_attention_bwd(
         s, d, *[None] * 10, 0, stream=0))
+
+
+def mha_bufs(**kw):
+    b = {n: FAKE for n in L._DIFF_MHA_FIELDS}
+    b.update(ws_bytes=BIG, **kw)
+    return L.diff_mha_bufs(**b)
+
+
+def test_diff_mha_refusals(flowmoe_lib):
+    s, d, n = shape(), L.make_diff_shape(16, 4, 2, 64, True), L.make_norm_shape(4, 64)
+    r = L.make_rope_shape(12, 32, 32, 16)
+    both = lambda *a: [lambda: L.flowmoe_diff_mha_fwd(*a, stream=0),
+                       lambda: L.flowmoe_diff_mha_bwd(*a, 0, stream=0)]
+    for rr, text in ((L.make_rope_shape(8, 32, 32, 16), "Q's and K's"),
+                     (L.make_rope_shape(6, 64, 32, 16), "Q's and K's"),
+                     (L.make_rope_shape(12, 32, 32, 64), "seq_len"),
+                     (L.make_rope_shape(12, 32, 34, 16), "rot_dim")):
+        for call in both(s, d, rr, n, mha_bufs()):
+            refused(L.ERR_INVALID, text, call)
+    for nn, text in ((L.make_norm_shape(2, 128), "norm's heads"), (L.make_norm_shape(4, 64, eps=-1.0), "eps")):
+        for call in both(s, d, r, nn, mha_bufs()):
+            refused(L.ERR_INVALID, text, call)
+    for call in both(shape(dtype=L.F32), d, r, n, mha_bufs()):
+        refused(L.ERR_UNSUPPORTED, "BF16", call)
+    nullable = ("gain", "positions", "lens", "dgain", "ws")
+    fwd = ("in", "w_qkv", "w_o", "lambda", "qkv", "attn", "attn2", "lse", "normed", "out")
+    names = [x for x in L._DIFF_MHA_FIELDS if x not in nullable]
+    for x in names:
+        calls_ = both(s, d, r, n, mha_bufs(**{x: None}))
+        if x in fwd:
+            refused(L.ERR_INVALID, f"bufs->{x} is null", calls_[0])
+        if x != "out":
+            refused(L.ERR_INVALID, f"bufs->{x} is null", calls_[1])
+    for x in ("gain", "positions", "lens"):
+        for call in both(s, d, r, n, mha_bufs(**{x: FAKE + 2})):
+            refused(L.ERR_INVALID, f"bufs->{x} is not 4-byte aligned", call)
+    need = L.flowmoe_diff_mha_ws_bytes(s, d, n)
+    assert need >= max(L.flowmoe_diff_attention_ws_bytes(s, d), L.flowmoe_head_norm_ws_bytes(s, n))
+    b = mha_bufs()
+    b.ws_bytes = need - 1
+    refused(L.ERR_WORKSPACE, "flowmoe_diff_mha_bwd", lambda: L.flowmoe_diff_mha_bwd(s, d, r, n, b, 0,
+                                                                                    stream=0))
+    with pytest.raises(KeyError):
+        L.diff_mha_bufs(w1=None)
+    # no tokens: the forward has nothing to do, the backward's sums stay to be written
+    L.flowmoe_diff_mha_fwd(shape(T=0), d, r, n, L.diff_mha_bufs(), stream=0)
+    refused(L.ERR_INVALID, "dw_qkv is null", lambda: L.flowmoe_diff_mha_bwd(
+        shape(T=0), d, r, n, L.diff_mha_bufs(), 0, stream=0))
+
+
+def test_more_tokens_than_a_grid_holds_refused(flowmoe_lib):
+    """Four tokens to a block of 256 threads: from 2^26 of them on HIP would cut a grid off."""
+    with pytest.raises(L.FlowMoEError) as ei:
+        L.flowmoe_rope_fwd(shape(T=1 << 26, M=2048), L.make_rope_shape(32, 64, 64, 16), FAKE, None, FAKE,
+                           stream=0)
+    assert ei.value.status == L.ERR_HIP and "invalid configuration" in str(ei.value)

@@ -99,16 +99,17 @@ struct FwdTile {
   static constexpr int G = NW / (2 * S), QB = 32 * G;  // groups of 32 queries, queries
   static constexpr int KB = S == 1 && NW == 8 ? 2 : 1, KT = 32 * KB * S;  // keys of a wave / 32, of a tile
 };
-template <int D, bool CAUSAL, int NW, int S>
+template <int D, bool CAUSAL, int NW, int S, bool ONE>
 __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffArgs a) {
   using Tile = FwdTile<NW, S>;
+  constexpr int SL = ONE ? 1 : 2;  // slots: ONE for sequences of one tile (more blocks to a CU)
   constexpr int KS = D / 32, DB = D / 32, QB = Tile::QB, KT = Tile::KT;  // KS: k steps of one map
   using Dma = TileDma<D, KT, NW>;
   constexpr int TB = Dma::TB;
-  // K slots 0, 1, then V slots 0, 1; at the end the outputs (float) of half the waves
-  __shared__ __attribute__((aligned(1024))) char lds[4 * TB];
+  // K slots, then V slots; at the end the outputs (float) of half the waves
+  __shared__ __attribute__((aligned(1024))) char lds[2 * SL * TB];
   __shared__ float2 stat[S > 1 ? NW / 2 * 64 : 1];  // and their references and sums
-  static_assert(4 * TB >= NW / 2 * 32 * D * 4, "the outputs fit the tiles' place");
+  static_assert(2 * SL * TB >= NW / 2 * 32 * D * 4, "the outputs fit the tiles' place");
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
   const int map = w & 1, grp = (w >> 1) % Tile::G, part = (w >> 1) / Tile::G;
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
     const Dma dma(lds_base(lds), w, lane, ld);
     const long kstep = KT * ld;
     dma.load(Kg, kend, 0);
-    dma.load(Vg, kend, 2 * TB);
+    dma.load(Vg, kend, SL * TB);
     bf16x8 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
@@ -147,11 +148,13 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
       wait_vm<0>();   // K(t) and V(t): loaded a step ago
       lds_barrier();  // and every wave's reads of the slots refilled now are done
       const char* tk = lds + st * TB;
-      const char* tv = lds + (2 + st) * TB;
-      Kg += kstep;  // K(t + 1), V(t + 1)
-      Vg += kstep;
-      dma.load(Kg, kend - KT * (t + 1), (st ^ 1) * TB);
-      dma.load(Vg, kend - KT * (t + 1), (2 + (st ^ 1)) * TB);
+      const char* tv = lds + (SL + st) * TB;
+      if constexpr (!ONE) {
+        Kg += kstep;  // K(t + 1), V(t + 1)
+        Vg += kstep;
+        dma.load(Kg, kend - KT * (t + 1), (st ^ 1) * TB);
+        dma.load(Vg, kend - KT * (t + 1), (SL + (st ^ 1)) * TB);
+      }
 #pragma unroll
       for (int j = 0; j < Tile::KB; ++j) {
         const int kb = Tile::KB * part + j, kb0 = KT * t + 32 * kb;
@@ -205,9 +208,13 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
         l += pair_sum(rsum);
       }
     };
-    for (int t = 0; t < nk; t += 2) {
-      step(t, Stage<0>{});
-      if (t + 1 < nk) step(t + 1, Stage<1>{});
+    if constexpr (ONE) {
+      step(0, Stage<0>{});
+    } else {
+      for (int t = 0; t < nk; t += 2) {
+        step(t, Stage<0>{});
+        if (t + 1 < nk) step(t + 1, Stage<1>{});
+      }
     }
     // waves that share rows hand them over, lane by lane: half the key parts to the
     // other half until one is left, then the second map to the first
@@ -289,12 +296,13 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
 // causal: 864 TFLOP/s of its 6 D flops a pair). The clock falls to 1.85 GHz with the matrix
 // pipes 45 % busy: power bounds it. Running dP and the first map's scores a tile ahead,
 // beside the elementwise work, measured 2 % slower (18 % with heads of 64).
-template <int D, bool CAUSAL, int NW, int S>
+template <int D, bool CAUSAL, int NW, int S, bool ONE>
 __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
+  constexpr int SL = ONE ? 1 : 2;  // slots: ONE for sequences of one tile
   constexpr int KS = D / 16, DB = D / 32, G = NW / S, QB = 32 * G, KT = 32 * S;
   using Dma = TileDma<D, KT, NW>;
   using DmaG = TileDma<D, QB, NW>;
-  constexpr int TB = Dma::TB, VB = 2 * TB, GB = 4 * TB;  // K slots, V slots, the dO rows
+  constexpr int TB = Dma::TB, VB = SL * TB, GB = 2 * VB;  // K slots, V slots, the dO rows
   __shared__ __attribute__((aligned(1024))) char lds[GB + QB * D * 2];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
@@ -367,10 +375,12 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
       lds_barrier();  // and every wave's reads of the slots refilled now are done
       const char* tk = lds + st * TB + part * (32 * 2 * D);
       const char* tv = tk + VB;
-      Kg += kstep;
-      Vg += kstep;
-      dma.load(Kg, kend - KT * (t + 1), (st ^ 1) * TB);
-      dma.load(Vg, kend - KT * (t + 1), VB + (st ^ 1) * TB);
+      if constexpr (!ONE) {
+        Kg += kstep;
+        Vg += kstep;
+        dma.load(Kg, kend - KT * (t + 1), (st ^ 1) * TB);
+        dma.load(Vg, kend - KT * (t + 1), VB + (st ^ 1) * TB);
+      }
       const int kb0 = KT * t + 32 * part;
       // (causal: nothing for a wave whose queries all precede these keys)
       if (kb0 >= kend || (CAUSAL && kb0 > q0 + 32 * grp + 31)) return;
@@ -423,9 +433,13 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    for (int t = 0; t < nk; t += 2) {
-      step(t, Stage<0>{});
-      if (t + 1 < nk) step(t + 1, Stage<1>{});
+    if constexpr (ONE) {
+      step(0, Stage<0>{});
+    } else {
+      for (int t = 0; t < nk; t += 2) {
+        step(t, Stage<0>{});
+        if (t + 1 < nk) step(t + 1, Stage<1>{});
+      }
     }
     if constexpr (S > 1) {  // parts S - 1 .. 1 hand their sums to part 0's waves, in that order
       wait_vm<0>();         // (the loads past the last tile write zeros)
@@ -530,17 +544,18 @@ __device__ __forceinline__ UnitAt find_unit(const DiffArgs& a, int u, int kt) {
 // dK and dV: waves of 32 keys over the 32-query tiles of every query head of the group, or
 // over a unit of them, whose sums diff_join_kernel adds. With S > 1, S of the NW waves share 32 keys, each with every S-th query tile, and add up at the end. The
 // last `heads` blocks sum dlambda.
-template <int D, bool CAUSAL, int NW, int S>
+template <int D, bool CAUSAL, int NW, int S, bool ONE>
 __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
+  constexpr int SL = ONE ? 1 : 2;  // slots: ONE for sequences of one tile
   constexpr int KS = D / 16, DB = D / 32, G = NW / S, KB = 32 * G, QT = 32 * S;
   using Dma = TileDma<D, QT, NW>;
   using DmaV = TileDma<D, KB, NW>;
   constexpr int TQ = Dma::TB;          // one query tile
-  constexpr int VT = 4 * TQ;           // two slots of Q and dO, then the block's V rows,
-  constexpr int ST = VT + KB * D * 2;  // then two slots of 32 S x (lse 1, lse 2, -d1, d2 - d1)
+  constexpr int VT = 2 * SL * TQ;      // slots of Q and dO, then the block's V rows,
+  constexpr int ST = VT + KB * D * 2;  // then slots of 32 S x (lse 1, lse 2, -d1, d2 - d1)
   constexpr int SB = 512 * S;
-  __shared__ __attribute__((aligned(1024))) char lds[ST + 2 * SB];
-  static_assert(S == 1 || G * 8 * DB * 1024 <= ST + 2 * SB, "a part's sums fit");
+  __shared__ __attribute__((aligned(1024))) char lds[ST + SL * SB];
+  static_assert(S == 1 || G * 8 * DB * 1024 <= ST + SL * SB, "a part's sums fit");
   const int per = a.kv * a.nseq, nblocks = (int)gridDim.x - a.heads;
   if ((int)blockIdx.x >= nblocks) {
     sum_d_lambda(a, blockIdx.x - nblocks, reinterpret_cast<float*>(lds));
@@ -631,12 +646,14 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
         lds_barrier();  // and every wave's reads of the other slot are done
         const char* tq = lds + st * 2 * TQ + part * (32 * 2 * D);
         const float* stat = reinterpret_cast<const float*>(lds + ST + SB * st) + 128 * part + 4 * h2;
-        Qt += QT * ld;
-        Gt += QT * a.M;
-        const int more = it + 1 < it1 ? end - qt0 - QT : 0;
-        dma.load(Qt, more, (st ^ 1) * 2 * TQ);
-        dmag.load(Gt, more, (st ^ 1) * 2 * TQ + TQ);
-        if (it + 1 < it1) load_stat(qt0 + QT);
+        if constexpr (!ONE) {
+          Qt += QT * ld;
+          Gt += QT * a.M;
+          const int more = it + 1 < it1 ? end - qt0 - QT : 0;
+          dma.load(Qt, more, (st ^ 1) * 2 * TQ);
+          dmag.load(Gt, more, (st ^ 1) * 2 * TQ + TQ);
+          if (it + 1 < it1) load_stat(qt0 + QT);
+        }
         if (qb < end && (!CAUSAL || qb + 31 >= k0 + 32 * grp)) {
           const bool edge = qb + 32 > end || (CAUSAL && k0 + 32 * grp + 31 > qb);
           auto mask = [&](floatx16& s) {
@@ -699,11 +716,15 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
                             __builtin_bit_cast(bf16x8, u32x4{d[0], d[1], d[2], d[3]}), dk[db]);
             }
         }
-        if (it + 1 < it1) store_stat(st ^ 1);
+        if (!ONE && it + 1 < it1) store_stat(st ^ 1);
       };
-      for (int it = it0; it < it1; it += 2) {
-        step(it, Stage<0>{});
-        if (it + 1 < it1) step(it + 1, Stage<1>{});
+      if constexpr (ONE) {
+        step(it0, Stage<0>{});
+      } else {
+        for (int it = it0; it < it1; it += 2) {
+          step(it, Stage<0>{});
+          if (it + 1 < it1) step(it + 1, Stage<1>{});
+        }
       }
     }
   }
@@ -804,29 +825,33 @@ long tiles(const DiffArgs& a, int heads, int rows) {
   return (long)((a.N + rows - 1) / rows) * heads * a.nseq;
 }
 
-template <int D, int NW, int S>
+template <int D, int NW, int S, bool ONE = false>
 void launch_fwd(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   const dim3 g((unsigned)tiles(a, a.heads, FwdTile<NW, S>::QB)), b(64 * NW);
-  if (m.causal) hipLaunchKernelGGL((diff_fwd_kernel<D, true, NW, S>), g, b, 0, st, a);
-  else hipLaunchKernelGGL((diff_fwd_kernel<D, false, NW, S>), g, b, 0, st, a);
+  if (m.causal) hipLaunchKernelGGL((diff_fwd_kernel<D, true, NW, S, ONE>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((diff_fwd_kernel<D, false, NW, S, ONE>), g, b, 0, st, a);
 }
 
 // Forward blocks by the launch: 0: 32 queries, 8 waves, four parts of the keys; 1: 32
-// queries, 4 waves, two parts; 2: 64 queries, 4 waves; 3: 128 queries, 8 waves.
+// queries, 4 waves, two parts; 2: 64 queries, 4 waves; 3: 128 queries, 8 waves; 4: below.
 // Few queries leave CUs idle and a block's walk over the keys is the time of the call, so
 // its waves share the keys; many are better served by blocks that read K and V less
 // often. us of variants 0, 1, 2, 3: 1 sequence of 2048, heads of 128, causal, 4 heads 23,
 // 26, 43, 55; 8 heads 30, 28, 44, 55; 16 heads 58, 44, 47, 56; 32 heads 116, 81, 67, 73;
 // 4 x 4096, 32 heads 1719, 1648, 904, 885; 8 x 2048, 16 heads, bidirectional 803, 736,
-// 424, 413; 50 x 300 -, 155, 78, 90; 32 x 512, 32 heads -, 443, 241, 246.
+// 424, 413; 50 x 300 -, 155, 78, 90; 32 x 512, 32 heads -, 443, 241, 246. Heads of 64 leave
+// room for more blocks of variant 1: 1 x 4485, 8 heads, variant 1 53, 2 86. 4: sequences of
+// one tile, 32 queries by 2 waves: 407 x 1, 8 heads of 128 10, variant 2 19; 452 x 10, 16
+// heads 25, 38.
 int fwd_variant(const DiffShape& m, const DiffArgs& a) {
   const long b32 = tiles(a, a.heads, 32), b128 = tiles(a, a.heads, 128);
+  if (m.N <= 32) return 4;
   if (b32 <= 256) return 0;
-  if (b32 <= 1024) return 1;
+  if (b32 <= (m.D == 64 ? 2048 : 1024)) return 1;
   return m.N >= 1024 && (b128 >= 1024 || !m.causal) ? 3 : 2;
 }
 long fwd_blocks(const DiffArgs& a, int v) {
-  return tiles(a, a.heads, v < 2 ? 32 : v == 2 ? 64 : 128);
+  return tiles(a, a.heads, v == 2 ? 64 : v == 3 ? 128 : 32);
 }
 
 // Tiles of a head side by side? Bidirectional ones have equal work and lose nothing by
@@ -845,18 +870,19 @@ void launch_fwd_variant(int v, const DiffShape& m, const DiffArgs& a, hipStream_
   if (v == 0) launch_fwd<D, 8, 4>(m, a, st);
   else if (v == 1) launch_fwd<D, 4, 2>(m, a, st);
   else if (v == 2) launch_fwd<D, 4, 1>(m, a, st);
-  else launch_fwd<D, 8, 1>(m, a, st);
+  else if (v == 3) launch_fwd<D, 8, 1>(m, a, st);
+  else launch_fwd<D, 2, 1, true>(m, a, st);
 }
 
-template <int D, int NW, int S>
+template <int D, int NW, int S, bool ONE = false>
 void launch_dq(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   const dim3 g((unsigned)tiles(a, a.heads, 32 * NW / S)), b(64 * NW);
-  if (m.causal) hipLaunchKernelGGL((diff_dq_kernel<D, true, NW, S>), g, b, 0, st, a);
-  else hipLaunchKernelGGL((diff_dq_kernel<D, false, NW, S>), g, b, 0, st, a);
+  if (m.causal) hipLaunchKernelGGL((diff_dq_kernel<D, true, NW, S, ONE>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((diff_dq_kernel<D, false, NW, S, ONE>), g, b, 0, st, a);
 }
 
-// dQ blocks by the launch: 0: one wave of 32 queries (sequences of at most 32); four waves
-// that share 1: 32 queries, 2: 64, 3: 128. us of the whole backward with 1, 2, 3: 2 x 512, 8
+// dQ blocks by the launch: 0: one wave of 32 queries (sequences of at most 32); 4: two of
+// 64 (at most 64); four waves that share 1: 32 queries, 2: 64, 3: 128. us of the whole backward with 1, 2, 3: 2 x 512, 8
 // heads of 64, causal 34, 36, 42; 1 x 2048, heads of 128, causal, 4 heads 71, 75, 100; 16 on 4
 // heads 176, 139, 158; 32 heads 301, 208, 209; 16 x 500, 16 on 8 heads of 64 119, 95, 91; 4 x
 // 4096, 32 heads of 128, causal 3610, 2460, 2270. 700 x 16, 4 heads of 64, variants 0, 3: 42,
@@ -864,13 +890,14 @@ void launch_dq(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
 int dq_variant(const DiffShape& m, const DiffArgs& a) {
   if (m.N <= 32) return 0;
   const long b32 = tiles(a, a.heads, 32);
-  return b32 <= 256 ? 1 : b32 <= 2048 ? 2 : 3;
+  return b32 <= 256 ? 1 : m.N <= 64 ? 4 : b32 <= 2048 ? 2 : 3;
 }
 
 template <int D>
 void launch_dq_variant(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   const int v = dq_variant(m, a);
-  if (v == 0) launch_dq<D, 1, 1>(m, a, st);
+  if (v == 0) launch_dq<D, 1, 1, true>(m, a, st);
+  else if (v == 4) launch_dq<D, 2, 1>(m, a, st);
   else if (v == 1) launch_dq<D, 4, 4>(m, a, st);
   else if (v == 2) launch_dq<D, 4, 2>(m, a, st);
   else launch_dq<D, 4, 1>(m, a, st);
@@ -879,7 +906,7 @@ void launch_dq_variant(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
 // dK and dV by the launch: blocks of 32 G keys and 32 S queries a step. A block's walk over
 // the queries (a step is about 1 us for a wave alone on its SIMD) is the time of a small
 // call, so its waves share the queries there; large ones are better served by tiles that
-// more keys share. Query tiles of 64 and 128 rows of heads of 128 leave a CU one
+// more keys share. Sequences of at most 32 and 64 take blocks of one and two waves. Query tiles of 64 and 128 rows of heads of 128 leave a CU one
 // block, so those keep {4, 1} earlier and are cut into units instead. us of {1, 4}, {2, 2},
 // {4, 1}: heads of 64: 2 x 512, 8 heads, causal 19, 23, 32; 4 x 1024, 8 heads 59, 53, 78;
 // 16 x 500, 16 heads (8) 95, 86, 92; 4 x 4096, 24 heads, causal 1170, 1042, 1012; heads of
@@ -891,6 +918,7 @@ struct KeyTile {
 KeyTile key_tile(const DiffShape& m, const DiffArgs& a) {
   if (m.N <= 32) return {1, 1};
   if (tiles(a, a.heads, 32) <= 256) return {1, 4};
+  if (m.N <= 64) return {2, 1};
   if (m.D == 64) return tiles(a, a.kv, 128) < 1024 ? KeyTile{2, 2} : KeyTile{4, 1};
   // 128 keys by 32 queries: up to three such steps for each of 512 resident blocks
   const long n = (m.N + 31) / 32, steps = tiles(a, a.heads, 128) * (m.causal ? (n + 1) / 2 : n);
@@ -898,11 +926,12 @@ KeyTile key_tile(const DiffShape& m, const DiffArgs& a) {
 }
 
 // Units of dK and dV: sets a.unit and a.units. Cut where the longest block has more than
-// twice the steps that every one of 768 would have (512 are resident): few key heads with
-// large groups, long causal sequences. 2 x 2031 tokens, 16 heads on 4 of 128, causal, uncut
-// 396 us, units of 1/512, 1/768 and 1/1024 of the steps 228, 201 and 205 (the whole
-// backward); 1 x 4096, 8 on 2 heads 789, 236, 211, 217. Units below 8 steps lose more to
-// their partial sums (1 x 2048, 4 heads: 88 for 4 steps, 71 for 8).
+// twice the steps that every one of 768 would have (512 are resident; of {1, 4} 256): few
+// key heads with large groups, long causal sequences. 2 x 2031 tokens, 16 heads on 4 of
+// 128, causal, uncut 396 us, units of 1/512, 1/768 and 1/1024 of the steps 228, 201 and 205
+// (the whole backward); 1 x 4096, 8 on 2 heads 789, 236, 211, 217. {1, 4}: 2 x 443, 2 heads
+// on 1 of 128, units of 8 steps (uncut) and 2: 42, 32; 3 x 500, 3 heads on 1, causal 52, 37;
+// 1 x 3000, 1 head of 64, 8 and 3: 47, 56.
 void cut_units(const DiffShape& m, DiffArgs& a) {
   const KeyTile k = key_tile(m, a);
   const int group = m.heads / m.kv, KB = 32 * k.G, QT = 32 * k.S, nt = (m.N + KB - 1) / KB;
@@ -911,19 +940,19 @@ void cut_units(const DiffShape& m, DiffArgs& a) {
   a.unit = a.units = 0;
   long all = 0;
   for (int kt = 0; kt < nt; ++kt) all += steps(kt);
-  const long unit = std::max<long>(all * per / 768, 8);
+  const long unit = k.S == 4 ? std::max<long>(all * per / 256, 2) : std::max<long>(all * per / 768, 8);
   if (steps(0) <= 2 * unit) return;
   a.unit = (int)unit;
   for (int kt = 0; kt < nt; ++kt) a.units += (int)((steps(kt) + unit - 1) / unit);
 }
 
-template <int D, int G, int S>
+template <int D, int G, int S, bool ONE = false>
 hipError_t launch_dkdv(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   const long n = a.unit > 0 ? (long)a.units * a.kv * a.nseq : tiles(a, a.kv, 32 * G);
   const hipError_t e = traced(FLOWMOE_K_DIFF_BWD_DKDV, st, [&] {
     const dim3 g((unsigned)(n + a.heads)), b(64 * G * S);
-    if (m.causal) hipLaunchKernelGGL((diff_dkdv_kernel<D, true, G * S, S>), g, b, 0, st, a);
-    else hipLaunchKernelGGL((diff_dkdv_kernel<D, false, G * S, S>), g, b, 0, st, a);
+    if (m.causal) hipLaunchKernelGGL((diff_dkdv_kernel<D, true, G * S, S, ONE>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((diff_dkdv_kernel<D, false, G * S, S, ONE>), g, b, 0, st, a);
   });
   if (e != hipSuccess || a.unit == 0) return e;
   return traced(FLOWMOE_K_DIFF_JOIN, st, [&] {
@@ -937,8 +966,8 @@ template <int D>
 hipError_t launch_dkdv_variant(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   const KeyTile k = key_tile(m, a);
   if (k.G == 4) return launch_dkdv<D, 4, 1>(m, a, st);
-  if (k.G == 2) return launch_dkdv<D, 2, 2>(m, a, st);
-  return k.S == 4 ? launch_dkdv<D, 1, 4>(m, a, st) : launch_dkdv<D, 1, 1>(m, a, st);
+  if (k.G == 2) return k.S == 2 ? launch_dkdv<D, 2, 2>(m, a, st) : launch_dkdv<D, 2, 1>(m, a, st);
+  return k.S == 4 ? launch_dkdv<D, 1, 4>(m, a, st) : launch_dkdv<D, 1, 1, true>(m, a, st);
 }
 
 }  // namespace

@@ -143,7 +143,7 @@ def test_null_and_misaligned_refused(flowmoe_lib):
 
 
 def test_workspaces_checked(flowmoe_lib):
-    s, n = shape(), L.make_norm_shape(4, 64)
+    s, n = shape(T=1024), L.make_norm_shape(4, 64)
     need = L.flowmoe_head_norm_ws_bytes(s, n)
     assert need >= 64 * 4
     for ws, have in ((FAKE, need - 1), (None, need)):
@@ -199,8 +199,9 @@ def test_diff_mha_refusals(flowmoe_lib):
     for x in ("gain", "positions", "lens"):
         for call in both(s, d, r, n, mha_bufs(**{x: FAKE + 2})):
             refused(L.ERR_INVALID, f"bufs->{x} is not 4-byte aligned", call)
+    s = shape(T=1024)
     need = L.flowmoe_diff_mha_ws_bytes(s, d, n)
-    assert need >= max(L.flowmoe_diff_attention_ws_bytes(s, d), L.flowmoe_head_norm_ws_bytes(s, n))
+    assert need >= 64 * 4 and need >= max(L.flowmoe_diff_attention_ws_bytes(s, d), L.flowmoe_head_norm_ws_bytes(s, n))
     b = mha_bufs()
     b.ws_bytes = need - 1
     refused(L.ERR_WORKSPACE, "flowmoe_diff_mha_bwd", lambda: L.flowmoe_diff_mha_bwd(s, d, r, n, b, 0,

@@ -112,7 +112,9 @@ CASES = [
     (2, 700, 12, 4, 64, False, [700, 450]),
     (2, 700, 12, 2, 128, False, None),
     (3, 600, 3, 3, 128, True, [600, 2, 333]),
-    # sequences of one tile
+    # sequences of two tiles and of one
+    (90, 37, 6, 3, 128, True, None),
+    (80, 64, 8, 4, 64, False, [n % 65 for n in range(80)]),
     (300, 20, 3, 3, 64, True, None),
     (200, 32, 4, 2, 128, False, [n % 33 for n in range(200)]),
     # around the tiles: one, two and three of 64 or 32 rows, a row short, whole, a row over

@@ -49,12 +49,15 @@ __device__ __forceinline__ double pair_turns(const RopeArgs& a, int i) {
 struct RopeTile {
   int n, per, tps, tokens;
 };
-__host__ __device__ __forceinline__ RopeTile rope_tile(int D, int heads) {
+__host__ __device__ __forceinline__ RopeTile rope_tile(int D, int heads, int T) {
   RopeTile r;
   r.n = D / 8;
   r.per = 256 / r.n;
   r.tps = heads < r.per ? r.per / heads : 1;
-  r.tokens = r.tps > 4 ? r.tps : 4;
+  // (tokens of a block one after the other: one a block while they are few; us of 1 and 4: 64
+  // tokens 4.5, 6.7; 1024 of 32 heads of 64 6.2, 7.2; 2048 8.8, 8.4; 1500 of 64 of 128 13.9, 10.6)
+  const int few = T <= 1024 ? 1 : 4;
+  r.tokens = r.tps > few ? r.tps : few;
   return r;
 }
 
@@ -70,7 +73,7 @@ template <typename T, bool HALF, bool NT>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   extern __shared__ float2 table[];  // tokens x 8 x (pairs / 8, rounded up)
   __shared__ float stage[HALF ? 2 : 1][HALF ? 8 * 256 : 1];
-  const RopeTile r = rope_tile(a.D, a.heads);
+  const RopeTile r = rope_tile(a.D, a.heads, a.T);
   const int half = a.rot / 2, tw = (half + 7) / 8, t0 = blockIdx.x * r.tokens,
             nt = min(r.tokens, a.T - t0), tid = threadIdx.x;
   for (int k = tid; k < half * nt; k += 256) {
@@ -129,7 +132,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 
 template <typename T>
 void run_rope(const RopeArgs& a, bool half_layout, hipStream_t st) {
-  const RopeTile r = rope_tile(a.D, a.heads);
+  const RopeTile r = rope_tile(a.D, a.heads, a.T);
   const dim3 g((unsigned)((a.T + (long)r.tokens - 1) / r.tokens)), b(256);
   const size_t lds = (size_t)r.tokens * 8 * ((a.rot / 2 + 7) / 8) * sizeof(float2);
   const bool nt = stream_past_caches(2L * a.T * a.heads * a.D * (long)sizeof(T));
@@ -280,7 +283,7 @@ int norm_bwd_blocks(long rows, int D) {
 hipError_t launch_rope(const RopeShape& m, int dtype, int T, long ld, bool back, const void* x,
                        const int32_t* pos, void* y, hipStream_t st) {
   if (T == 0) return hipSuccess;
-  const int tokens = rope_tile(m.D, m.heads).tokens;
+  const int tokens = rope_tile(m.D, m.heads, T).tokens;
   if ((T + (long)tokens - 1) / tokens > kMaxBlocks) return hipErrorInvalidConfiguration;
   RopeArgs a = {};
   a.x = x;

@@ -476,6 +476,7 @@ typedef struct {
  *             read and written; the others of y are left as they are. y may be x
  *             (in place); else they must not overlap.
  *   positions T int32, nullable (then t % seq_len); any value
+ * From 2^26 tokens on (of rows that fill a block) FLOWMOE_ERR_HIP, as dispatch.
  * Q and K of qkv (T x 3M') turn in one call: M = 3 M', heads = 2 M' / head_dim. */
 flowmoe_status_t flowmoe_rope_fwd(const flowmoe_shape_t* shape, const flowmoe_rope_shape_t* rope,
                                   const void* x, const int32_t* positions, void* y,
@@ -491,11 +492,11 @@ flowmoe_status_t flowmoe_rope_bwd(const flowmoe_shape_t* shape, const flowmoe_ro
 typedef struct {
   int32_t heads;    /* M = heads * head_dim */
   int32_t head_dim; /* a multiple of 8, 8..512 */
-  float eps;        /* > 0 */
+  float eps;        /* > 0, a normal float */
   float scale;      /* a constant factor (differential attention: 1 - lambda_init) */
 } flowmoe_norm_shape_t;
 
-/* RMS norm of each head's columns of a row:
+/* RMS norm of each head's columns of a row, squares summed in float:
  *   y = scale * gain * x / sqrt(mean(x^2) + eps).
  *   x, y  T x M layer dtype (y may be x); only shape->T, M and dtype are used
  *   gain  head_dim float, nullable (ones), shared by the heads */
@@ -526,7 +527,9 @@ flowmoe_status_t flowmoe_head_norm_bwd(const flowmoe_shape_t* shape,
  * key/value heads are shared by heads / kv_heads query heads each (query head h
  * reads key head h / (heads / kv_heads)). qkv rows hold W = M + 2 * kv_heads *
  * head_dim elements, [Q | K | V]. bf16 only; 16-byte aligned; only shape->T, M
- * and dtype are used. */
+ * (at most 2^21) and dtype are used. heads times the sequences' tiles of 32 tokens
+ * stay below 2^23. A call's blocks depend on its sizes: the same rows in a larger
+ * batch may be summed in another order. */
 typedef struct {
   int32_t seq_len;  /* tokens per sequence; shape->T is a whole number of sequences */
   int32_t heads;

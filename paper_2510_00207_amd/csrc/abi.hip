@@ -1,5 +1,6 @@
 // C ABI front end of libflowmoe: argument validation, status codes, workspace
 // queries, and the R-chunk two-stream layer schedule (Sec. 3.2, Eqs. 3-6).
+#include <float.h>
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -787,8 +788,8 @@ flowmoe_status_t check_norm(const flowmoe_shape_t* s, const flowmoe_norm_shape_t
   if (n->heads < 1 || (long)n->heads * n->head_dim != s->M)
     return fail(FLOWMOE_ERR_INVALID, "heads * head_dim = %d * %d is not M = %d", n->heads,
                 n->head_dim, s->M);
-  if (!(n->eps > 0.0f) || !isfinite(n->eps))
-    return fail(FLOWMOE_ERR_INVALID, "eps = %g must be finite and > 0", n->eps);
+  if (!(n->eps >= FLT_MIN) || !isfinite(n->eps))
+    return fail(FLOWMOE_ERR_INVALID, "eps = %g must be a finite normal float > 0", n->eps);
   if (!isfinite(n->scale)) return fail(FLOWMOE_ERR_INVALID, "scale is not finite");
   *out = NormShape{n->heads, n->head_dim, n->eps, n->scale};
   return FLOWMOE_OK;
@@ -816,7 +817,7 @@ flowmoe_status_t check_diff(const flowmoe_shape_t* s, const flowmoe_diff_shape_t
   if (m->causal != 0 && m->causal != 1)
     return fail(FLOWMOE_ERR_INVALID, "causal = %d is not 0 or 1", m->causal);
   // (a tile's rows are reached by 32-bit byte offsets; a grid holds 2^32 threads)
-  if ((long)s->T * 3 * s->M > (1L << 40) || s->T > (1 << 30) || s->M > (1 << 22))
+  if ((long)s->T * 3 * s->M > (1L << 40) || s->T > (1 << 30) || s->M > (1 << 21))
     return fail(FLOWMOE_ERR_UNSUPPORTED, "tensor too large");
   if (((m->seq_len + 31L) / 32) * m->heads * (s->T / m->seq_len) >= (1L << 32) / 512)
     return fail(FLOWMOE_ERR_UNSUPPORTED, "too many attention tiles");

@@ -441,8 +441,8 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
         if (t + 1 < nk) step(t + 1, Stage<1>{});
       }
     }
+    wait_vm<0>();           // (the loads past the last tile write zeros)
     if constexpr (S > 1) {  // parts S - 1 .. 1 hand their sums to part 0's waves, in that order
-      wait_vm<0>();         // (the loads past the last tile write zeros)
       float4* x = reinterpret_cast<float4*>(lds) + (long)grp * DB * 4 * 64 + lane;
 #pragma unroll
       for (int n = S - 1; n > 0; --n) {
@@ -728,8 +728,8 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
       }
     }
   }
+  wait_vm<0>();           // (the loads past the last tile write zeros)
   if constexpr (S > 1) {  // parts S - 1 .. 1 hand their sums to part 0's waves, in that order
-    wait_vm<0>();         // (the loads past the last tile write zeros)
     float4* x = reinterpret_cast<float4*>(lds) + (long)grp * 8 * DB * 64 + lane;
 #pragma unroll
     for (int n = S - 1; n > 0; --n) {
@@ -938,6 +938,7 @@ void cut_units(const DiffShape& m, DiffArgs& a) {
   const long per = (long)m.kv * a.nseq;
   auto steps = [&](int kt) { return (long)group * ((m.N - (m.causal ? KB * kt : 0) + QT - 1) / QT); };
   a.unit = a.units = 0;
+  if (per == 0) return;
   long all = 0;
   for (int kt = 0; kt < nt; ++kt) all += steps(kt);
   const long unit = k.S == 4 ? std::max<long>(all * per / 256, 2) : std::max<long>(all * per / 768, 8);

@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int e = 8 * c + i, q = e < half ? e + half : e - half;
-      from[i] = e < a.rot ? (q % 8) * 256 + tid - c + q / 8 : i * 256 + tid;
+      from[i] = h < r.per && e < a.rot ? (q % 8) * 256 + tid - c + q / 8 : i * 256 + tid;
     }
   }
   int step = 0;

@@ -83,6 +83,7 @@ def test_rope_refusals(flowmoe_lib, kw, status, text):
     (L.make_norm_shape(0, 64), L.ERR_INVALID, "heads * head_dim"),
     (L.make_norm_shape(64, 4), L.ERR_INVALID, "head_dim"),
     (L.make_norm_shape(4, 64, eps=0.0), L.ERR_INVALID, "eps"),
+    (L.make_norm_shape(4, 64, eps=1e-40), L.ERR_INVALID, "eps"),
     (L.make_norm_shape(4, 64, eps=float("nan")), L.ERR_INVALID, "eps"),
     (L.make_norm_shape(4, 64, scale=float("inf")), L.ERR_INVALID, "scale"),
     (L.make_diff_shape(16, 4, 2, 32, True), L.ERR_UNSUPPORTED, "head_dim"),
@@ -105,6 +106,9 @@ def test_sizes_refused(flowmoe_lib):
     d = L.make_diff_shape(16, 4, 2, 64, True)
     refused(L.ERR_UNSUPPORTED, "BF16", lambda: L.flowmoe_diff_attention_fwd(
         shape(dtype=L.F32), d, FAKE, FAKE, None, FAKE, None, None, stream=0))
+    wide = L.make_diff_shape(16, 1 << 16, 1, 64, True)
+    refused(L.ERR_UNSUPPORTED, "too large", lambda: L.flowmoe_diff_attention_fwd(
+        shape(T=16, M=1 << 22), wide, FAKE, FAKE, None, FAKE, None, None, stream=0))
     # 2^23 tiles of 512 threads are more than a grid holds
     many = L.make_diff_shape(1, 1, 1, 64, True)
     refused(L.ERR_UNSUPPORTED, "too many", lambda: L.flowmoe_diff_attention_fwd(

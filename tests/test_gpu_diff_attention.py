@@ -209,6 +209,21 @@ def test_d_lambda_accumulates_and_results_repeat():
     assert torch.equal(again["d_lambda"], first["d_lambda"] + first["d_lambda"])
 
 
+def test_no_tokens():
+    """No sequence of any length: nothing but dlambda's sum of nothing."""
+    need_gpu()
+    s = L.make_shape(0, 256, 8, 1, 1, 0, L.BF16)
+    for seq, hd in ((1, 64), (4096, 64), (4096, 128)):
+        m = L.make_diff_shape(seq, 256 // hd, 1, hd, True)
+        assert L.flowmoe_diff_attention_ws_bytes(s, m) == 0
+        L.flowmoe_diff_attention_fwd(s, m, *[None] * 6)
+        dl = torch.full((256 // hd,), 3.0, device=dev())
+        L.flowmoe_diff_attention_bwd(s, m, *[None] * 9, dl, True)
+        assert bool((dl == 3.0).all())
+        L.flowmoe_diff_attention_bwd(s, m, *[None] * 9, dl, False)
+        assert not bool(dl.any())
+
+
 def test_two_streams_at_once():
     need_gpu()
     cs = [Call(2, 300, 4, 2, 64, c, *make(2, 300, 4, 2, 64, 10 + c), [300, 211]) for c in (0, 1)]

@@ -141,6 +141,20 @@ def test_steps_and_products(nseq, seq, heads, kv, hd, causal, lens, rot, layout)
         assert torch.equal(o2[n], o[n]), n
 
 
+def test_no_tokens():
+    need_gpu()
+    s, d, n = (L.make_shape(0, 256, 8, 1, 1, 0, L.BF16), L.make_diff_shape(64, 4, 2, 64, True),
+               L.make_norm_shape(4, 64))
+    z = dict(dw_qkv=torch.ones(256, 512, device=dev()), dw_o=torch.ones(256, 256, device=dev()),
+             d_lambda=torch.ones(4, device=dev()), dgain=torch.ones(64, device=dev()))
+    b = L.diff_mha_bufs(**z)
+    L.flowmoe_diff_mha_fwd(s, d, None, n, b)
+    L.flowmoe_diff_mha_bwd(s, d, None, n, b, True)
+    assert all(bool((v == 1).all()) for v in z.values())
+    L.flowmoe_diff_mha_bwd(s, d, None, n, b, False)
+    assert not any(bool(v.any()) for v in z.values())
+
+
 def test_captured_and_replayed():
     """A captured step, replayed on new inputs between eager steps of the same block."""
     need_gpu()

@@ -49,6 +49,11 @@ ROPE_CASES = [
     (4, 24, 3, 8, 6, "pairs", "f32", {}, "row"),
     (257, 8, 1, 8, 8, "pairs", "bf16", {}, "far"),
     (300, 5128, 65, 72, 16, "half", "bf16", {}, "row"),
+    # heads that do not divide a block's threads, more heads than it holds
+    (1030, 2400, 30, 80, 80, "half", "bf16", {}, "row"),
+    (1100, 480, 6, 80, 42, "half", "f32", BANDS, "far"),
+    (70, 2640, 11, 240, 240, "half", "bf16", {}, "row"),
+    (2, 512, 1, 512, 510, "half", "bf16", {}, "row"),
 ]
 
 

@@ -542,8 +542,14 @@ __device__ __forceinline__ UnitAt find_unit(const DiffArgs& a, int u, int kt) {
 }
 
 // dK and dV: waves of 32 keys over the 32-query tiles of every query head of the group, or
-// over a unit of them, whose sums diff_join_kernel adds. With S > 1, S of the NW waves share 32 keys, each with every S-th query tile, and add up at the end. The
-// last `heads` blocks sum dlambda.
+// over a unit of them, whose sums diff_join_kernel adds. With S > 1, S of the NW waves
+// share 32 keys, each with every S-th query tile, and add up at the end. The last `heads`
+// blocks sum dlambda.
+//
+// 32 matrix products and 32 exponentials a lane for 32 x 32 pairs; both accumulators (128
+// registers at D = 128) and the K fragments leave none to read ahead of the products: with
+// read groups as in dQ 1570 us, the plain order 1350 (4 x 4096 tokens, 32 heads of 128,
+// causal: 815 TFLOP/s of its 8 D flops a pair, the clock at 2.0 GHz).
 template <int D, bool CAUSAL, int NW, int S, bool ONE>
 __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
   constexpr int SL = ONE ? 1 : 2;  // slots: ONE for sequences of one tile
@@ -552,7 +558,7 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
   using DmaV = TileDma<D, KB, NW>;
   constexpr int TQ = Dma::TB;          // one query tile
   constexpr int VT = 2 * SL * TQ;      // slots of Q and dO, then the block's V rows,
-  constexpr int ST = VT + KB * D * 2;  // then slots of 32 S x (lse 1, lse 2, -d1, d2 - d1)
+  constexpr int ST = VT + KB * D * 2;  // then slots of 32 S x 4 row statistics
   constexpr int SB = 512 * S;
   __shared__ __attribute__((aligned(1024))) char lds[ST + SL * SB];
   static_assert(S == 1 || G * 8 * DB * 1024 <= ST + SL * SB, "a part's sums fit");
@@ -603,11 +609,14 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
       const int it0 = max(lo - gh * steps, 0), it1 = min(hi - gh * steps, valid);
       if (it0 >= it1) continue;
       const int hd = kh * group + gh;
-      const float lam = a.lambda[hd];
+      // |lambda| goes into the second map's exponent (lambda = 0: -inf, and P_2 is 0), its sign
+      // into the sums
+      const float lam = a.lambda[hd], sgn = lam < 0.0f ? -1.0f : 1.0f, llam = log2f(fabsf(lam));
       const int qf0 = qs0 + QT * it0;
       const bf16_t* Qt = rows + (long)hd * D + qf0 * ld;
       const bf16_t* Gt = a.d_o + (tok0 + qf0) * a.M + (long)hd * D;
-      // the statistics of a step: lse or delta of a row, both maps', a thread
+      // the statistics of a step's rows, two a thread: lse of map 1, of map 2 less log2 |lambda|
+      // (base 2); -d1, +-(d2 - d1)
       float2 rstat = make_float2(0.0f, 0.0f);
       const bool isd = (tid & 32) != 0;
       const int srow = 32 * (tid >> 6) + lq;
@@ -617,7 +626,7 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
         if (tid < 64 * S) {
           const bool in = qb + srow < end;
           const float x = in ? sp[qb] : 0.0f, y = in ? sp[qb + smap] : 0.0f;
-          rstat = isd ? make_float2(-x, y - x) : make_float2(x * kLog2e, y * kLog2e);
+          rstat = isd ? make_float2(-x, sgn * (y - x)) : make_float2(x * kLog2e, y * kLog2e - llam);
         }
       };
       auto store_stat = [&](int slot) {
@@ -654,7 +663,9 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
           dmag.load(Gt, more, (st ^ 1) * 2 * TQ + TQ);
           if (it + 1 < it1) load_stat(qt0 + QT);
         }
-        if (qb < end && (!CAUSAL || qb + 31 >= k0 + 32 * grp)) {
+        // (a condition less in the loop of causal blocks that share nothing: it cost a spill of
+        // a K fragment, whose reload waits for the loads under way, 8 % of the time)
+        if (((S == 1 && CAUSAL) || qb < end) && (!CAUSAL || qb + 31 >= k0 + 32 * grp)) {
           const bool edge = qb + 32 > end || (CAUSAL && k0 + 32 * grp + 31 > qb);
           auto mask = [&](floatx16& s) {
             if (edge) {
@@ -693,10 +704,10 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
             for (int j = 0; j < 4; ++j) {
               const int r = 4 * J + j;
               const float p1 = exp2_fast(fmaf(s1[r], a.c2, -l1[j]));
-              const float p2 = lam * exp2_fast(fmaf(s2[r], a.c2, -l2[j]));
-              p[j] = p1 - p2;
+              const float p2 = exp2_fast(fmaf(s2[r], a.c2, -l2[j]));
+              p[j] = fmaf(-sgn, p2, p1);
               e[j] = p1 * dp[r];
-              f[j] = p2 * (dd[j] - dp[r]);
+              f[j] = p2 * fmaf(-sgn, dp[r], dd[j]);
             }
 #pragma unroll
             for (int j = 0; j < 4; j += 2) {

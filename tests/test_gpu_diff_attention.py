@@ -181,6 +181,20 @@ def test_large_scores(hd):
     assert bool(torch.isfinite(o["d_qkv"]).all()) and bool(torch.isfinite(o["d_lambda"]).all())
 
 
+@pytest.mark.parametrize("nseq,seq,heads,kv,hd,causal", [
+    (2, 130, 4, 1, 64, True), (1, 200, 4, 4, 128, False), (40, 32, 4, 2, 128, True),
+    (9, 400, 8, 4, 128, True)])
+def test_lambda_of_any_sign(nseq, seq, heads, kv, hd, causal):
+    """Zero, negative and large lambda, also among the heads that share a key head."""
+    need_gpu()
+    qkv, lam, d_attn = make(nseq, seq, heads, kv, hd, 7)
+    lam[:4] = torch.tensor([0.0, -0.7, 3.0, -1e-3], device=dev())
+    c = Call(nseq, seq, heads, kv, hd, causal, qkv, lam, d_attn)
+    c.fwd()
+    c.bwd()
+    check(c, (seq, heads, kv, hd, causal))
+
+
 def test_forward_alone():
     """Without attn2 and lse (no backward follows): the same attn."""
     need_gpu()

@@ -48,8 +48,10 @@ struct DiffArgs {
   int T, N, heads, kv, nseq;
   int accumulate;        // add to d_lambda
   long M, W;             // columns of a row of A, of qkv
-  float* part;           // sums of units (dK, dV)
+  float *part, *qpart;   // sums of units: dK and dV, dQ
   int unit, units;       // steps of a unit (0: uncut), units of a key head of a sequence
+  int qunit, qunits;     // the same of dQ and a query head
+  int kblocks;           // blocks of the join of dK and dV
   int shared, pair;      // order of the blocks (diff_decode)
   float c2;              // log2(e) / sqrt(d)
   float rs;              // 1 / sqrt(d)
@@ -106,10 +108,10 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
   constexpr int KS = D / 32, DB = D / 32, QB = Tile::QB, KT = Tile::KT;  // KS: k steps of one map
   using Dma = TileDma<D, KT, NW>;
   constexpr int TB = Dma::TB;
-  // K slots, then V slots; at the end the outputs (float) of half the waves
+  // K slots, then V slots; at the end the waves' outputs (float)
   __shared__ __attribute__((aligned(1024))) char lds[2 * SL * TB];
-  __shared__ float2 stat[S > 1 ? NW / 2 * 64 : 1];  // and their references and sums
-  static_assert(2 * SL * TB >= NW / 2 * 32 * D * 4, "the outputs fit the tiles' place");
+  __shared__ float2 stat[S > 1 ? NW * 64 : 1];  // and their references and sums
+  static_assert(2 * SL * TB >= (S > 1 ? NW : NW / 2) * 32 * D * 4, "the outputs fit the tiles' place");
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
   const int map = w & 1, grp = (w >> 1) % Tile::G, part = (w >> 1) / Tile::G;
@@ -216,74 +218,170 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
         if (t + 1 < nk) step(t + 1, Stage<1>{});
       }
     }
-    // waves that share rows hand them over, lane by lane: half the key parts to the
-    // other half until one is left, then the second map to the first
-    auto slot = [&](int owner) { return reinterpret_cast<float4*>(lds) + (long)owner * DB * 4 * 64 + lane; };
-    auto put = [&](float4* x) {
+    // The waves of a part own the 32-column blocks db = part (mod S) of their rows: each hands
+    // the others theirs, lane by lane, and adds up its own; then the second map's hand
+    // theirs to the first's (in slots that the first exchange left free)
+    auto slot = [&](int mp, int p, int db) {
+      const int owner = S > 1 ? (grp * 2 + mp) * S + p : grp;
+      return reinterpret_cast<float4*>(lds) + (long)(owner * DB + db) * 256 + lane;
+    };
+    auto put = [&](float4* x, const floatx16& v) {
 #pragma unroll
-      for (int i = 0; i < 4 * DB; ++i) {
-        const floatx16& v = o[i / 4];
-        const int r = 4 * (i % 4);
-        x[i * 64] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
-      }
+      for (int J = 0; J < 4; ++J) x[J * 64] = make_float4(v[4 * J], v[4 * J + 1], v[4 * J + 2], v[4 * J + 3]);
     };
     wait_vm<0>();  // (the loads past the last tile write zeros)
     lds_barrier();
+    if constexpr (S > 1) {
 #pragma unroll
-    for (int n = S / 2; n > 0; n /= 2) {
-      const int owner = ((part & (n - 1)) * Tile::G + grp) * 2 + map;  // of n x 2 G
-      if (part >= n && part < 2 * n) {
-        put(slot(owner));
-        stat[owner * 64 + lane] = make_float2(m, l);
-      }
+      for (int db = 0; db < DB; ++db)
+        if (db % S != part) put(slot(map, part, db), o[db]);
+      stat[w * 64 + lane] = make_float2(m, l);
       lds_barrier();
-      if (part < n) {
-        const float2 other = stat[owner * 64 + lane];
-        const float mn = fmaxf(m, other.x);  // (part 0 has key 0: finite where the row is live)
-        const float ref = mn == -INFINITY ? 0.0f : mn;
-        const float f = exp2_fast(m - ref), g = exp2_fast(other.x - ref);
-        l = l * f + other.y * g;
-        m = mn;
-        const float4* x = slot(owner);
+      float f[S], mn = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 4 * DB; ++i) {
-          const float4 v = x[i * 64];
-          const float e[4] = {v.x, v.y, v.z, v.w};
+      for (int p = 0; p < S; ++p) mn = fmaxf(mn, stat[(((p * Tile::G + grp) << 1) | map) * 64 + lane].x);
+      const float ref = mn == -INFINITY ? 0.0f : mn;  // (part 0 has key 0: finite where the row is live)
+      l = 0.0f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int r = 4 * (i % 4) + j;
-            o[i / 4][r] = o[i / 4][r] * f + e[j] * g;
+      for (int p = 0; p < S; ++p) {
+        const float2 x = stat[(((p * Tile::G + grp) << 1) | map) * 64 + lane];
+        f[p] = exp2_fast(x.x - ref);
+        l += x.y * f[p];
+      }
+      const float fo = exp2_fast(m - ref);
+      m = mn;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        if (db % S != part) continue;
+        floatx16 s = o[db] * fo;
+#pragma unroll
+        for (int p = 0; p < S; ++p) {
+          if (p == part) continue;
+          const float4* x = slot(map, p, db);
+#pragma unroll
+          for (int J = 0; J < 4; ++J) {
+            const float4 v = x[J * 64];
+            s[4 * J] += v.x * f[p]; s[4 * J + 1] += v.y * f[p];
+            s[4 * J + 2] += v.z * f[p]; s[4 * J + 3] += v.w * f[p];
           }
         }
+        o[db] = s;
       }
-      lds_barrier();
     }
     const float inv = qw < end ? 1.0f / l : 0.0f;
     const float lam = qw < end ? a.lambda[hd] : 0.0f;
 #pragma unroll
-    for (int db = 0; db < DB; ++db) o[db] *= inv;
-    if (part == 0 && map == 1) put(slot(grp));
+    for (int db = 0; db < DB; ++db) {
+      if (S > 1 && db % S != part) continue;
+      o[db] *= inv;
+      if (map == 1) put(slot(1, part, db), o[db]);
+    }
     lds_barrier();
-    if (part == 0 && map == 0) {
-      const float4* x = slot(grp);
+    if (map == 0) {
 #pragma unroll
-      for (int i = 0; i < 4 * DB; ++i) {
-        const float4 v = x[i * 64];
-        const float e[4] = {v.x, v.y, v.z, v.w};
+      for (int db = 0; db < DB; ++db) {
+        if (S > 1 && db % S != part) continue;
+        const float4* x = slot(1, part, db);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[i / 4][4 * (i % 4) + j] -= lam * e[j];
+        for (int J = 0; J < 4; ++J) {
+          const float4 v = x[J * 64];
+          o[db][4 * J] -= lam * v.x; o[db][4 * J + 1] -= lam * v.y;
+          o[db][4 * J + 2] -= lam * v.z; o[db][4 * J + 3] -= lam * v.w;
+        }
       }
     }
   }
-  if (qw >= a.N || part > 0) return;
+  if (qw >= a.N) return;
   bf16_t* out = map == 0 ? a.out : a.out2;
   if (out != nullptr) {
     bf16_t* Og = out + (tok0 + qw) * a.M + (long)hd * D;
 #pragma unroll
-    for (int db = 0; db < DB; ++db) store_cols(Og + 32 * db, o[db], h2, 1.0f);
+    for (int db = 0; db < DB; ++db)
+      if (S == 1 || db % S == part) store_cols(Og + 32 * db, o[db], h2, 1.0f);
   }
-  if (h2 == 0 && a.lse != nullptr)
+  if (h2 == 0 && part == 0 && a.lse != nullptr)
     a.lse[((long)map * a.heads + hd) * a.T + tok0 + qw] = qw < end ? (m + log2f(l)) * kLn2 : 0.0f;
+}
+
+// S waves (the parts of a group) that hold sums of the same NB 32-row blocks: each hands
+// the others theirs, lane by lane, and adds up its own, those with index = part (mod S),
+// in the order of the parts. Every wave's reads of LDS are done. (One part after the
+// other handing all to the first took 3.3 us of a dQ block of four waves at D = 128.)
+template <int S, int NB>
+__device__ __forceinline__ void add_parts(floatx16 (&v)[NB], char* lds, int grp, int part, int lane) {
+  auto slot = [&](int p, int b) {
+    return reinterpret_cast<float4*>(lds) + (long)((grp * S + p) * NB + b) * 256 + lane;
+  };
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    if (b % S == part) continue;
+    float4* x = slot(part, b);
+#pragma unroll
+    for (int J = 0; J < 4; ++J)
+      x[J * 64] = make_float4(v[b][4 * J], v[b][4 * J + 1], v[b][4 * J + 2], v[b][4 * J + 3]);
+  }
+  lds_barrier();
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    if (b % S != part) continue;
+    floatx16 s = zero16();
+#pragma unroll
+    for (int p = 0; p < S; ++p) {
+      if (p == part) {
+        s += v[b];
+        continue;
+      }
+      const float4* x = slot(p, b);
+#pragma unroll
+      for (int J = 0; J < 4; ++J) {
+        const float4 e = x[J * 64];
+        s[4 * J] += e.x; s[4 * J + 1] += e.y; s[4 * J + 2] += e.z; s[4 * J + 3] += e.w;
+      }
+    }
+    v[b] = s;
+  }
+}
+
+// Steps of QT queries that see key tile kt of KB rows, and steps of KT keys that query
+// tile qt of QB rows sees. A (tile, head, sequence) is cut into units of `a.unit` steps (key
+// tiles; the group's heads one after the other) or `a.qunit` (query tiles); 0: uncut.
+template <bool CAUSAL, int KB, int QT>
+__host__ __device__ __forceinline__ int key_steps(int N, int kt) {
+  return (N - (CAUSAL ? kt * KB : 0) + QT - 1) / QT;
+}
+template <bool CAUSAL, int QB, int KT>
+__host__ __device__ __forceinline__ int query_steps(int N, int qt) {
+  return ((CAUSAL && QB * (qt + 1) < N ? QB * (qt + 1) : N) + KT - 1) / KT;
+}
+
+// Of nt tiles of steps(tile) steps each in units of `unit`: unit u's tile, the tile's units,
+// and its place among them; or (u < 0) the units before tile kt. A lane a tile, as a loop
+// over the tiles with a division each took microseconds.
+struct UnitAt {
+  int kt, units, chunk;
+};
+template <class F>
+__device__ __forceinline__ UnitAt find_unit(int nt, int unit, F&& steps, int u, int kt) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int k0 = 0;; k0 += 64) {
+    const int k = k0 + lane;
+    const int n = k < nt ? (steps(k) + unit - 1) / unit : 0;
+    int upto = n;  // the units of tiles k0 .. k
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int v = __shfl_up(upto, d);
+      if (lane >= d) upto += v;
+    }
+    const unsigned long long here = __ballot(u >= 0 ? before + upto > u : k == kt);
+    if (here != 0) {
+      const int f = __ffsll(here) - 1;
+      const int units = __builtin_amdgcn_readlane(n, f);
+      const int first = before + __builtin_amdgcn_readlane(upto, f) - units;
+      return {k0 + f, units, u >= 0 ? u - first : first};
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
 }
 
 // dQ, and d1 and d2: NW waves over 32-key tiles, both maps in a wave (they share dP). S
@@ -307,8 +405,20 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
   const int grp = w % G, part = w / G;
-  int qt, hd, sq;
-  diff_decode(a, a.heads, CAUSAL, QB, qt, hd, sq);
+  int qt, hd, sq, units = 1, chunk = 0;
+  if (a.qunit > 0) {
+    const int per = a.heads * a.nseq, rest = (int)(blockIdx.x % per);
+    const UnitAt at = find_unit((a.N + QB - 1) / QB, a.qunit,
+                                [&](int k) { return query_steps<CAUSAL, QB, KT>(a.N, k); },
+                                blockIdx.x / per, 0);
+    qt = at.kt;
+    units = at.units;
+    chunk = at.chunk;
+    hd = rest % a.heads;
+    sq = rest / a.heads;
+  } else {
+    diff_decode(a, a.heads, CAUSAL, QB, qt, hd, sq);
+  }
   const int end = seq_end(a, sq);
   const long tok0 = (long)sq * a.N, ld = a.W;
   const int q0 = qt * QB, qw = q0 + 32 * grp + lq;
@@ -327,25 +437,34 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
     const bf16_t* Vg = Kg + (long)a.kv * D;
     const long go = tok0 * a.M + (long)hd * D;
     const int kend = CAUSAL ? min(end, q0 + QB) : end;
-    const int nk = (kend + KT - 1) / KT;
+    const int nk0 = (kend + KT - 1) / KT, t0 = chunk * a.qunit;
+    const int nk = a.qunit > 0 ? min(nk0, t0 + a.qunit) : nk0;
     const long kstep = KT * ld;
     const Dma dma(lds_base(lds), w, lane, ld);
-    DmaG(lds_base(lds), w, lane, a.M).load(a.d_o + go + (long)q0 * a.M, end - q0, GB);
-    dma.load(Kg, kend, 0);
-    dma.load(Vg, kend, VB);
     bf16x8 qf[KS];
+    {
+      bf16x8 gv[KS], ov[KS], pv[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const long c = go + (long)qw * a.M + 16 * ks + 8 * h2;
-      qf[ks] = live ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * ks + 8 * h2) : zero8();
-      const bf16x8 gv = live ? *reinterpret_cast<const bf16x8*>(a.d_o + c) : zero8();
-      const bf16x8 ov = live ? *reinterpret_cast<const bf16x8*>(a.o + c) : zero8();
-      const bf16x8 pv = live ? *reinterpret_cast<const bf16x8*>(a.o2 + c) : zero8();
-#pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        d1 += (float)gv[t] * (float)ov[t];
-        d2 += (float)gv[t] * (float)pv[t];
+      for (int ks = 0; ks < KS; ++ks) {
+        const long c = go + (long)qw * a.M + 16 * ks + 8 * h2;
+        gv[ks] = live ? *reinterpret_cast<const bf16x8*>(a.d_o + c) : zero8();
+        ov[ks] = live ? *reinterpret_cast<const bf16x8*>(a.o + c) : zero8();
+        pv[ks] = live ? *reinterpret_cast<const bf16x8*>(a.o2 + c) : zero8();
+        qf[ks] = live ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * ks + 8 * h2) : zero8();
       }
+      // (after the rows above, which would else wait for the tiles too: loads return in order)
+      DmaG(lds_base(lds), w, lane, a.M).load(a.d_o + go + (long)q0 * a.M, end - q0, GB);
+      Kg += t0 * kstep;
+      Vg += t0 * kstep;
+      dma.load(Kg, kend - KT * t0, 0);
+      dma.load(Vg, kend - KT * t0, VB);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          d1 += (float)gv[ks][t] * (float)ov[ks][t];
+          d2 += (float)gv[ks][t] * (float)pv[ks][t];
+        }
     }
     d1 = pair_sum(d1);
     d2 = pair_sum(d2);
@@ -436,46 +555,42 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
     if constexpr (ONE) {
       step(0, Stage<0>{});
     } else {
-      for (int t = 0; t < nk; t += 2) {
+      for (int t = t0; t < nk; t += 2) {
         step(t, Stage<0>{});
         if (t + 1 < nk) step(t + 1, Stage<1>{});
       }
     }
     wait_vm<0>();           // (the loads past the last tile write zeros)
-    if constexpr (S > 1) {  // parts S - 1 .. 1 hand their sums to part 0's waves, in that order
-      float4* x = reinterpret_cast<float4*>(lds) + (long)grp * DB * 4 * 64 + lane;
-#pragma unroll
-      for (int n = S - 1; n > 0; --n) {
-        lds_barrier();
-        if (part == n) {
-#pragma unroll
-          for (int i = 0; i < 4 * DB; ++i) {
-            const floatx16& v = dq[i / 4];
-            const int r = 4 * (i % 4);
-            x[i * 64] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
-          }
-        }
-        lds_barrier();
-        if (part == 0) {
-#pragma unroll
-          for (int i = 0; i < 4 * DB; ++i) {
-            const float4 v = x[i * 64];
-            const float e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) dq[i / 4][4 * (i % 4) + j] += e[j];
-          }
-        }
-      }
+    if constexpr (S > 1) {
+      lds_barrier();
+      add_parts<S>(dq, lds, grp, part, lane);
     }
   }
-  if (qw >= a.N || part > 0) return;
-  if (h2 == 0) {
+  const bool lead = part == 0 && h2 == 0;
+  if (units > 1) {
+    if (q0 < end) {
+      float4* x = reinterpret_cast<float4*>(a.qpart) +
+                  ((long)(blockIdx.x % (a.heads * a.nseq)) * a.qunits + blockIdx.x / (a.heads * a.nseq)) *
+                      (4 * DB * 64 * G) + 64 * grp + lane;
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i) {
+        const floatx16& v = dq[i / 4];
+        const int r = 4 * (i % 4);
+        if (i / 4 % S == part) x[i * 64 * G] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
+      }
+    }
+    if (chunk > 0) return;  // (the first unit writes the rows' d1 and d2)
+  }
+  if (qw >= a.N) return;
+  if (lead) {
     a.delta[srow] = d1;
     a.delta[srow + smap] = d2;
   }
+  if (units > 1) return;
   bf16_t* dst = a.d_qkv + (tok0 + qw) * ld + (long)hd * D;
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
+    if (db % S != part) continue;
     if (!live) dq[db] = zero16();
     store_cols(dst + 32 * db, dq[db], h2, db >= DB / 2 ? -lam * a.rs : a.rs);
   }
@@ -504,43 +619,6 @@ __device__ __forceinline__ void sum_d_lambda(const DiffArgs& a, int hd, float* p
   }
 }
 
-// Steps of QT queries that see key tile kt of KB rows. A (key tile, key head, sequence) is
-// cut into units of `a.unit` steps, the group's heads one after the other (0: uncut).
-template <bool CAUSAL, int KB, int QT>
-__host__ __device__ __forceinline__ int key_steps(int N, int kt) {
-  return (N - (CAUSAL ? kt * KB : 0) + QT - 1) / QT;
-}
-
-// Unit u of a key head of a sequence: its key tile, the tile's units, and its place among
-// them; or (u < 0) the units before tile kt. A lane a tile, as a loop over the tiles with a
-// division each took microseconds.
-struct UnitAt {
-  int kt, units, chunk;
-};
-template <bool CAUSAL, int KB, int QT>
-__device__ __forceinline__ UnitAt find_unit(const DiffArgs& a, int u, int kt) {
-  const int group = a.heads / a.kv, nt = (a.N + KB - 1) / KB, lane = threadIdx.x & 63;
-  int before = 0;
-  for (int k0 = 0;; k0 += 64) {
-    const int k = k0 + lane;
-    const int n = k < nt ? (group * key_steps<CAUSAL, KB, QT>(a.N, k) + a.unit - 1) / a.unit : 0;
-    int upto = n;  // the units of tiles k0 .. k
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int v = __shfl_up(upto, d);
-      if (lane >= d) upto += v;
-    }
-    const unsigned long long here = __ballot(u >= 0 ? before + upto > u : k == kt);
-    if (here != 0) {
-      const int f = __ffsll(here) - 1;
-      const int units = __builtin_amdgcn_readlane(n, f);
-      const int first = before + __builtin_amdgcn_readlane(upto, f) - units;
-      return {k0 + f, units, u >= 0 ? u - first : first};
-    }
-    before += __builtin_amdgcn_readlane(upto, 63);
-  }
-}
-
 // dK and dV: waves of 32 keys over the 32-query tiles of every query head of the group, or
 // over a unit of them, whose sums diff_join_kernel adds. With S > 1, S of the NW waves
 // share 32 keys, each with every S-th query tile, and add up at the end. The last `heads`
@@ -561,7 +639,7 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
   constexpr int ST = VT + KB * D * 2;  // then slots of 32 S x 4 row statistics
   constexpr int SB = 512 * S;
   __shared__ __attribute__((aligned(1024))) char lds[ST + SL * SB];
-  static_assert(S == 1 || G * 8 * DB * 1024 <= ST + SL * SB, "a part's sums fit");
+  static_assert(S == 1 || NW * DB * 4096 <= ST + SL * SB, "the parts' sums fit");
   const int per = a.kv * a.nseq, nblocks = (int)gridDim.x - a.heads;
   if ((int)blockIdx.x >= nblocks) {
     sum_d_lambda(a, blockIdx.x - nblocks, reinterpret_cast<float*>(lds));
@@ -574,7 +652,8 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
   const int group = a.heads / a.kv;
   int kt = (int)(blockIdx.x / per), units = 1, chunk = 0;
   if (a.unit > 0) {
-    const UnitAt at = find_unit<CAUSAL, KB, QT>(a, kt, 0);
+    const UnitAt at = find_unit((a.N + KB - 1) / KB, a.unit,
+                                [&](int k) { return group * key_steps<CAUSAL, KB, QT>(a.N, k); }, kt, 0);
     kt = at.kt;
     units = at.units;
     chunk = at.chunk;
@@ -740,47 +819,27 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
     }
   }
   wait_vm<0>();           // (the loads past the last tile write zeros)
-  if constexpr (S > 1) {  // parts S - 1 .. 1 hand their sums to part 0's waves, in that order
-    float4* x = reinterpret_cast<float4*>(lds) + (long)grp * 8 * DB * 64 + lane;
-#pragma unroll
-    for (int n = S - 1; n > 0; --n) {
-      lds_barrier();
-      if (part == n) {
-#pragma unroll
-        for (int i = 0; i < 8 * DB; ++i) {
-          const floatx16& v = i < 4 * DB ? dk[i / 4] : dv[i / 4 - DB];
-          const int r = 4 * (i % 4);
-          x[i * 64] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
-        }
-      }
-      lds_barrier();
-      if (part == 0) {
-#pragma unroll
-        for (int i = 0; i < 8 * DB; ++i) {
-          floatx16& s = i < 4 * DB ? dk[i / 4] : dv[i / 4 - DB];
-          const float4 v = x[i * 64];
-          const float e[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) s[4 * (i % 4) + j] += e[j];
-        }
-      }
-    }
-    if (part > 0) return;
+  if constexpr (S > 1) {
+    lds_barrier();
+    add_parts<S>(dk, lds, grp, part, lane);
+    lds_barrier();
+    add_parts<S>(dv, lds, grp, part, lane);
   }
   if (units > 1) {
     if (k0 >= end) return;
     float4* x = reinterpret_cast<float4*>(a.part) +
-                ((long)rest * a.units + blockIdx.x / per) * (8 * DB * 64 * G) + tid;
+                ((long)rest * a.units + blockIdx.x / per) * (8 * DB * 64 * G) + 64 * grp + lane;
 #pragma unroll
     for (int i = 0; i < 8 * DB; ++i) {
       const floatx16& v = i < 4 * DB ? dk[i / 4] : dv[i / 4 - DB];
       const int r = 4 * (i % 4);
-      x[i * 64 * G] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
+      if (i / 4 % DB % S == part) x[i * 64 * G] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
     }
   } else if (kw < a.N) {  // (rows past the end: their accumulators hold only masked zeros)
     bf16_t* dst = a.d_qkv + (tok0 + kw) * ld;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
+      if (db % S != part) continue;
       if (!live) dk[db] = dv[db] = zero16();
       store_cols(dst + kcol + 32 * db, dk[db], h2, a.rs);
       store_cols(dst + vcol + 32 * db, dv[db], h2, 1.0f);
@@ -789,23 +848,29 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
 }
 
 // dK and dV of key tiles that were cut into units, their sums added in unit order: a block
-// a key tile of 32 G and 32 columns of K or V, with the lanes as they were
+// a key tile of 32 G and 32 columns of K or V, with the lanes as they were. Blocks past
+// a.kblocks: dQ of query tiles that were (S = 4 only).
 template <int D, bool CAUSAL, int G, int S>
 __global__ __launch_bounds__(64 * G) void diff_join_kernel(DiffArgs a) {
   constexpr int DB = D / 32, KB = 32 * G, QT = 32 * S;
-  const int per = a.kv * a.nseq, tid = threadIdx.x, lane = tid & 63;
-  const int rest = (int)(blockIdx.x % per), kh = rest % a.kv, sq = rest / a.kv;
-  const int u = (int)(blockIdx.x / per), col = u % (2 * DB), kt = u / (2 * DB);
-  const UnitAt at = find_unit<CAUSAL, KB, QT>(a, -1, kt);
-  const int first = at.chunk, units = at.units;
-  if (units == 1) return;
-  const int end = seq_end(a, sq), k0 = kt * KB, kw = k0 + 32 * (tid >> 6) + (lane & 31);
+  const bool q = S == 4 && (int)blockIdx.x >= a.kblocks;
+  const int b = (int)blockIdx.x - (q ? a.kblocks : 0), cols = q ? DB : 2 * DB;
+  const int heads = q ? a.heads : a.kv, per = heads * a.nseq, tid = threadIdx.x, lane = tid & 63;
+  const int rest = b % per, hd = rest % heads, sq = rest / heads;
+  const int u = b / per, col = u % cols, tile = u / cols;
+  const int group = a.heads / a.kv, nt = (a.N + KB - 1) / KB;
+  const UnitAt at = q ? find_unit(nt, a.qunit, [&](int k) { return query_steps<CAUSAL, KB, QT>(a.N, k); },
+                                  -1, tile)
+                      : find_unit(nt, a.unit,
+                                  [&](int k) { return group * key_steps<CAUSAL, KB, QT>(a.N, k); }, -1, tile);
+  if (at.units == 1) return;
+  const int end = seq_end(a, sq), r0 = tile * KB, rw = r0 + 32 * (tid >> 6) + (lane & 31);
   floatx16 s = zero16();
-  if (kw < end) {
-    constexpr int U = 8 * DB * 64 * G;  // float4s of a unit
-    const float4* x = reinterpret_cast<const float4*>(a.part) + ((long)rest * a.units + first) * U +
-                      4 * col * 64 * G + tid;
-    for (int n = 0; n < units; ++n, x += U) {
+  if (rw < end) {
+    const int U = 4 * cols * 64 * G;  // float4s of a unit
+    const float4* x = reinterpret_cast<const float4*>(q ? a.qpart : a.part) +
+                      ((long)rest * (q ? a.qunits : a.units) + at.chunk) * U + 4 * col * 64 * G + tid;
+    for (int n = 0; n < at.units; ++n, x += U) {
 #pragma unroll
       for (int J = 0; J < 4; ++J) {
         const float4 v = x[J * 64 * G];
@@ -813,9 +878,14 @@ __global__ __launch_bounds__(64 * G) void diff_join_kernel(DiffArgs a) {
       }
     }
   }
-  if (kw >= a.N) return;
-  const long c = a.M + (long)(col < DB ? kh : a.kv + kh) * D + 32 * (col % DB);
-  store_cols(a.d_qkv + ((long)sq * a.N + kw) * a.W + c, s, lane >> 5, col < DB ? a.rs : 1.0f);
+  if (rw >= a.N) return;
+  bf16_t* row = a.d_qkv + ((long)sq * a.N + rw) * a.W;
+  if (q) {
+    store_cols(row + (long)hd * D + 32 * col, s, lane >> 5, col >= DB / 2 ? -a.lambda[hd] * a.rs : a.rs);
+  } else {
+    const long c = a.M + (long)(col < DB ? hd : a.kv + hd) * D + 32 * (col % DB);
+    store_cols(row + c, s, lane >> 5, col < DB ? a.rs : 1.0f);
+  }
 }
 
 DiffArgs diff_args(const DiffShape& m, int T) {
@@ -887,7 +957,8 @@ void launch_fwd_variant(int v, const DiffShape& m, const DiffArgs& a, hipStream_
 
 template <int D, int NW, int S, bool ONE = false>
 void launch_dq(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
-  const dim3 g((unsigned)tiles(a, a.heads, 32 * NW / S)), b(64 * NW);
+  const long n = a.qunit > 0 ? (long)a.qunits * a.heads * a.nseq : tiles(a, a.heads, 32 * NW / S);
+  const dim3 g((unsigned)n), b(64 * NW);
   if (m.causal) hipLaunchKernelGGL((diff_dq_kernel<D, true, NW, S, ONE>), g, b, 0, st, a);
   else hipLaunchKernelGGL((diff_dq_kernel<D, false, NW, S, ONE>), g, b, 0, st, a);
 }
@@ -957,6 +1028,27 @@ void cut_units(const DiffShape& m, DiffArgs& a) {
   a.unit = (int)unit;
   for (int kt = 0; kt < nt; ++kt) a.units += (int)((steps(kt) + unit - 1) / unit);
 }
+// And of dQ, in its blocks of 32 queries and 128 keys a step (variant 1): a.qunit, a.qunits.
+// The whole backward uncut and cut: 1 x 773, 2 heads of 128 34, 29 us; 1 x 3000, 1 head of 64 46,
+// 40; 1 x 700, 2 heads on 1 23, 21.
+void cut_query_units(const DiffShape& m, DiffArgs& a) {
+  a.qunit = a.qunits = 0;
+  const long per = (long)m.heads * a.nseq;
+  if (per == 0 || dq_variant(m, a) != 1) return;
+  const int nt = (m.N + 31) / 32;
+  auto steps = [&](int qt) {
+    return m.causal ? query_steps<true, 32, 128>(m.N, qt) : query_steps<false, 32, 128>(m.N, qt);
+  };
+  long all = 0;
+  for (int qt = 0; qt < nt; ++qt) all += steps(qt);
+  const long unit = std::max<long>(all * per / 256, 2);
+  if (steps(nt - 1) <= 2 * unit) return;
+  a.qunit = (int)unit;
+  for (int qt = 0; qt < nt; ++qt) a.qunits += (int)((steps(qt) + unit - 1) / unit);
+}
+size_t part_bytes(const DiffShape& m, const DiffArgs& a) {
+  return align256((size_t)a.units * m.kv * a.nseq * 32 * key_tile(m, a).G * 2 * m.D * sizeof(float));
+}
 
 template <int D, int G, int S, bool ONE = false>
 hipError_t launch_dkdv(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
@@ -966,11 +1058,14 @@ hipError_t launch_dkdv(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
     if (m.causal) hipLaunchKernelGGL((diff_dkdv_kernel<D, true, G * S, S, ONE>), g, b, 0, st, a);
     else hipLaunchKernelGGL((diff_dkdv_kernel<D, false, G * S, S, ONE>), g, b, 0, st, a);
   });
-  if (e != hipSuccess || a.unit == 0) return e;
+  if (e != hipSuccess || (a.unit == 0 && a.qunit == 0)) return e;
+  DiffArgs j = a;
+  j.kblocks = a.unit > 0 ? (int)(tiles(a, a.kv, 32 * G) * (2 * D / 32)) : 0;
+  const long nq = a.qunit > 0 ? tiles(a, a.heads, 32) * (D / 32) : 0;
   return traced(FLOWMOE_K_DIFF_JOIN, st, [&] {
-    const dim3 g((unsigned)(tiles(a, a.kv, 32 * G) * (2 * D / 32))), b(64 * G);
-    if (m.causal) hipLaunchKernelGGL((diff_join_kernel<D, true, G, S>), g, b, 0, st, a);
-    else hipLaunchKernelGGL((diff_join_kernel<D, false, G, S>), g, b, 0, st, a);
+    const dim3 g((unsigned)(j.kblocks + nq)), b(64 * G);
+    if (m.causal) hipLaunchKernelGGL((diff_join_kernel<D, true, G, S>), g, b, 0, st, j);
+    else hipLaunchKernelGGL((diff_join_kernel<D, false, G, S>), g, b, 0, st, j);
   });
 }
 
@@ -987,7 +1082,8 @@ hipError_t launch_dkdv_variant(const DiffShape& m, const DiffArgs& a, hipStream_
 size_t diff_attn_ws_bytes(const DiffShape& m, int T) {
   DiffArgs a = diff_args(m, T);
   cut_units(m, a);
-  return align256((size_t)a.units * m.kv * a.nseq * 32 * key_tile(m, a).G * 2 * m.D * sizeof(float));
+  cut_query_units(m, a);
+  return part_bytes(m, a) + align256((size_t)a.qunits * m.heads * a.nseq * 32 * m.D * sizeof(float));
 }
 
 hipError_t launch_diff_attn_fwd(const DiffShape& m, int T, const void* qkv, const float* lambda,
@@ -1029,7 +1125,10 @@ hipError_t launch_diff_attn_bwd(const DiffShape& m, int T, const void* qkv, cons
   a.delta = delta;
   a.d_lambda = d_lambda;
   a.accumulate = accumulate;
+  cut_units(m, a);
+  cut_query_units(m, a);
   a.part = static_cast<float*>(ws);
+  a.qpart = a.qunit > 0 ? reinterpret_cast<float*>(static_cast<char*>(ws) + part_bytes(m, a)) : nullptr;
   if (T > 0) {
     const hipError_t e = traced(FLOWMOE_K_DIFF_BWD_DQ, st, [&] {
       if (m.D == 128) launch_dq_variant<128>(m, a, st);
@@ -1038,7 +1137,6 @@ hipError_t launch_diff_attn_bwd(const DiffShape& m, int T, const void* qkv, cons
     if (e != hipSuccess) return e;
   }
   // (without tokens: dlambda alone)
-  cut_units(m, a);
   return m.D == 128 ? launch_dkdv_variant<128>(m, a, st) : launch_dkdv_variant<64>(m, a, st);
 }
 

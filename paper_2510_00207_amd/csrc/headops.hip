@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256) void head_norm_kernel(NormArgs a) {
 }
 
 // dx = r (u - x r^2 mean(u x)), u = scale gain dy; dgain's sums over the block's rows go
-// to `part`, in a fixed order. As above 402 MB in 80 us, 5.0 TB/s, with the join's 5 us; 512,
+// to `part`, in a fixed order. As above 402 MB in 80 us, 5.0 TB/s, with the join's 4 us; 512,
 // 1024 and 2048 blocks 111, 82 and 91.
 template <typename T, int L, bool NT>
 __global__ __launch_bounds__(256) void head_norm_bwd_kernel(NormArgs a) {
@@ -236,15 +236,23 @@ __global__ __launch_bounds__(256) void head_norm_bwd_kernel(NormArgs a) {
   }
 }
 
-// dgain = (or +=) scale x the sum of n partial rows: a wave a column
-__global__ __launch_bounds__(64) void head_norm_join_kernel(const float* part, int n, int D,
-                                                            float scale, float* dgain,
-                                                            int accumulate) {
+// dgain = (or +=) scale x the sum of n partial rows: a block a column (a wave a column took
+// 7 us for 1024 rows)
+__global__ __launch_bounds__(256) void head_norm_join_kernel(const float* part, int n, int D,
+                                                             float scale, float* dgain,
+                                                             int accumulate) {
+  __shared__ float sums[4];
   const int c = blockIdx.x;
   float s = 0.0f;
-  for (int k = threadIdx.x; k < n; k += 64) s += part[(long)k * D + c];
-  s = scale * group_sum<64>(s);
-  if (threadIdx.x == 0) dgain[c] = accumulate ? dgain[c] + s : s;
+#pragma unroll 4
+  for (int k = threadIdx.x; k < n; k += 256) s += part[(long)k * D + c];
+  s = group_sum<64>(s);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = scale * ((sums[0] + sums[1]) + (sums[2] + sums[3]));
+    dgain[c] = accumulate ? dgain[c] + s : s;
+  }
 }
 
 int norm_lanes(int D) {
@@ -364,7 +372,7 @@ hipError_t launch_head_norm_bwd(const NormShape& m, int dtype, int T, const void
   }
   if (dgain == nullptr || one) return hipSuccess;
   return traced(FLOWMOE_K_HEAD_NORM_BWD, st, [&] {
-    hipLaunchKernelGGL(head_norm_join_kernel, dim3(a.D), dim3(64), 0, st, a.part, n, a.D, a.scale,
+    hipLaunchKernelGGL(head_norm_join_kernel, dim3(a.D), dim3(256), 0, st, a.part, n, a.D, a.scale,
                        dgain, accumulate);
   });
 }

@@ -849,31 +849,32 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
 
 // dK and dV of key tiles that were cut into units, their sums added in unit order: a block
 // a key tile of 32 G and 32 columns of K or V, with the lanes as they were. Blocks past
-// a.kblocks: dQ of query tiles that were (S = 4 only).
+// a.kblocks: dQ of query tiles that were, in the blocks that go with these of dK and dV.
 template <int D, bool CAUSAL, int G, int S>
 __global__ __launch_bounds__(64 * G) void diff_join_kernel(DiffArgs a) {
   constexpr int DB = D / 32, KB = 32 * G, QT = 32 * S;
-  const bool q = S == 4 && (int)blockIdx.x >= a.kblocks;
-  const int b = (int)blockIdx.x - (q ? a.kblocks : 0), cols = q ? DB : 2 * DB;
+  constexpr int GQ = S == 4 ? 1 : 2, SQ = S == 4 ? 4 : 2;
+  const bool q = (int)blockIdx.x >= a.kblocks;
+  const int b = (int)blockIdx.x - (q ? a.kblocks : 0), cols = q ? DB : 2 * DB, g = q ? GQ : G;
   const int heads = q ? a.heads : a.kv, per = heads * a.nseq, tid = threadIdx.x, lane = tid & 63;
+  if (tid >= 64 * g) return;
   const int rest = b % per, hd = rest % heads, sq = rest / heads;
   const int u = b / per, col = u % cols, tile = u / cols;
-  const int group = a.heads / a.kv, nt = (a.N + KB - 1) / KB;
-  const UnitAt at = q ? find_unit(nt, a.qunit, [&](int k) { return query_steps<CAUSAL, KB, QT>(a.N, k); },
-                                  -1, tile)
-                      : find_unit(nt, a.unit,
-                                  [&](int k) { return group * key_steps<CAUSAL, KB, QT>(a.N, k); }, -1, tile);
+  const int group = a.heads / a.kv, nt = (a.N + 32 * g - 1) / (32 * g);
+  const UnitAt at =
+      q ? find_unit(nt, a.qunit, [&](int k) { return query_steps<CAUSAL, 32 * GQ, 32 * SQ>(a.N, k); }, -1, tile)
+        : find_unit(nt, a.unit, [&](int k) { return group * key_steps<CAUSAL, KB, QT>(a.N, k); }, -1, tile);
   if (at.units == 1) return;
-  const int end = seq_end(a, sq), r0 = tile * KB, rw = r0 + 32 * (tid >> 6) + (lane & 31);
+  const int end = seq_end(a, sq), r0 = tile * 32 * g, rw = r0 + 32 * (tid >> 6) + (lane & 31);
   floatx16 s = zero16();
   if (rw < end) {
-    const int U = 4 * cols * 64 * G;  // float4s of a unit
+    const int U = 4 * cols * 64 * g;  // float4s of a unit
     const float4* x = reinterpret_cast<const float4*>(q ? a.qpart : a.part) +
-                      ((long)rest * (q ? a.qunits : a.units) + at.chunk) * U + 4 * col * 64 * G + tid;
+                      ((long)rest * (q ? a.qunits : a.units) + at.chunk) * U + 4 * col * 64 * g + tid;
     for (int n = 0; n < at.units; ++n, x += U) {
 #pragma unroll
       for (int J = 0; J < 4; ++J) {
-        const float4 v = x[J * 64 * G];
+        const float4 v = x[J * 64 * g];
         s[4 * J] += v.x; s[4 * J + 1] += v.y; s[4 * J + 2] += v.z; s[4 * J + 3] += v.w;
       }
     }
@@ -964,11 +965,11 @@ void launch_dq(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
 }
 
 // dQ blocks by the launch: 0: one wave of 32 queries (sequences of at most 32); 4: two of
-// 64 (at most 64); four waves that share 1: 32 queries, 2: 64, 3: 128. us of the whole backward with 1, 2, 3: 2 x 512, 8
-// heads of 64, causal 34, 36, 42; 1 x 2048, heads of 128, causal, 4 heads 71, 75, 100; 16 on 4
-// heads 176, 139, 158; 32 heads 301, 208, 209; 16 x 500, 16 on 8 heads of 64 119, 95, 91; 4 x
-// 4096, 32 heads of 128, causal 3610, 2460, 2270. 700 x 16, 4 heads of 64, variants 0, 3: 42,
-// 50.
+// 64 (at most 64); four waves that share 1: 32 queries, 2: 64, 3: 128. us of the whole
+// backward with 1, 2, 3: 2 x 512, 8 heads of 64, causal 34, 36, 42; 1 x 2048, heads of 128,
+// causal, 4 heads 71, 75, 100; 16 on 4 heads 176, 139, 158; 32 heads 301, 208, 209; 16 x 500,
+// 16 on 8 heads of 64 119, 95, 91; 4 x 4096, 32 heads of 128, causal 3610, 2460, 2270. 700 x
+// 16, 4 heads of 64, variants 0, 3: 42, 50.
 int dq_variant(const DiffShape& m, const DiffArgs& a) {
   if (m.N <= 32) return 0;
   const long b32 = tiles(a, a.heads, 32);
@@ -988,12 +989,13 @@ void launch_dq_variant(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
 // dK and dV by the launch: blocks of 32 G keys and 32 S queries a step. A block's walk over
 // the queries (a step is about 1 us for a wave alone on its SIMD) is the time of a small
 // call, so its waves share the queries there; large ones are better served by tiles that
-// more keys share. Sequences of at most 32 and 64 take blocks of one and two waves. Query tiles of 64 and 128 rows of heads of 128 leave a CU one
-// block, so those keep {4, 1} earlier and are cut into units instead. us of {1, 4}, {2, 2},
-// {4, 1}: heads of 64: 2 x 512, 8 heads, causal 19, 23, 32; 4 x 1024, 8 heads 59, 53, 78;
-// 16 x 500, 16 heads (8) 95, 86, 92; 4 x 4096, 24 heads, causal 1170, 1042, 1012; heads of
-// 128: 1 x 2048, 4 heads, causal 72, 79, 74; 8 x 256, 8 heads 38, 28, 35; 20 x 200, 8 heads
-// (4) 78, 68, 61; 1 x 2048, 16 heads (4), causal 173, 153, 134.
+// more keys share. Sequences of at most 32 and 64 take blocks of one and two waves. Query
+// tiles of 64 and 128 rows of heads of 128 leave a CU one block, so those keep {4, 1}
+// earlier and are cut into units instead. us of {1, 4}, {2, 2}, {4, 1}: heads of 64: 2 x 512,
+// 8 heads, causal 19, 23, 32; 4 x 1024, 8 heads 59, 53, 78; 16 x 500, 16 heads (8) 95, 86,
+// 92; 4 x 4096, 24 heads, causal 1170, 1042, 1012; heads of 128: 1 x 2048, 4 heads, causal
+// 72, 79, 74; 8 x 256, 8 heads 38, 28, 35; 20 x 200, 8 heads (4) 78, 68, 61; 1 x 2048, 16
+// heads (4), causal 173, 153, 134.
 struct KeyTile {
   int G, S;
 };
@@ -1007,44 +1009,59 @@ KeyTile key_tile(const DiffShape& m, const DiffArgs& a) {
   return steps <= 3 * 512 ? KeyTile{2, 2} : KeyTile{4, 1};
 }
 
-// Units of dK and dV: sets a.unit and a.units. Cut where the longest block has more than
-// twice the steps that every one of 768 would have (512 are resident; of {1, 4} 256): few
-// key heads with large groups, long causal sequences. 2 x 2031 tokens, 16 heads on 4 of
-// 128, causal, uncut 396 us, units of 1/512, 1/768 and 1/1024 of the steps 228, 201 and 205
-// (the whole backward); 1 x 4096, 8 on 2 heads 789, 236, 211, 217. {1, 4}: 2 x 443, 2 heads
-// on 1 of 128, units of 8 steps (uncut) and 2: 42, 32; 3 x 500, 3 heads on 1, causal 52, 37;
-// 1 x 3000, 1 head of 64, 8 and 3: 47, 56.
+// The unit that nt tiles of steps(tile) steps, `per` times over, are cut into: the smallest
+// (at least 2) whose blocks run in one round of `slots`; 0 (uncut): no such unit, or the
+// longest tile is less than the worth of the join longer (about 16 / S steps). A round that
+// is not full costs as much as a full one: the whole backward of 2 x 2031 tokens, 16 heads
+// on 4 of 128, causal, 512 slots: uncut 457 us; units of 34, 37, 40, 44, 51 steps (576,
+// 536, 488, 456, 408 blocks) 221, 203, 184, 188, 197; of 20 (920 blocks, two rounds) 198.
+template <class F>
+int cut(int nt, long per, long slots, int S, F&& steps, int& units) {
+  units = 0;
+  if (per == 0 || nt * per > slots) return 0;
+  long all = 0;
+  int longest = 0;
+  for (int i = 0; i < nt; ++i) {
+    all += steps(i);
+    longest = std::max(longest, steps(i));
+  }
+  auto count = [&](int unit) {
+    int n = 0;
+    for (int i = 0; i < nt; ++i) n += (steps(i) + unit - 1) / unit;
+    return n;
+  };
+  int lo = (int)std::max<long>((all * per + slots - 1) / slots, 2), hi = longest;
+  if (longest < lo + 16 / S) return 0;
+  while (lo < hi) {
+    const int mid = lo + (hi - lo) / 2;
+    if (count(mid) * per <= slots) hi = mid;
+    else lo = mid + 1;
+  }
+  if (longest < lo + 16 / S) return 0;
+  units = count(lo);
+  return lo;
+}
+
+// Units of dK and dV: a.unit, a.units. Two blocks to a CU, or one where 64 or 128 query rows
+// of heads of 128 fill its LDS. The whole backward uncut and cut: 2 x 1024, 4 heads on 1 of
+// 128, causal 92, 46 us; 1 x 2000, 2 on 1 of 128 100, 60; 1 x 3000, 1 head of 64 60, 44; 4 x
+// 1024, 8 on 2 of 128 249, 98; 2 x 1500, 16 on 2 of 64, causal 253, 82.
 void cut_units(const DiffShape& m, DiffArgs& a) {
   const KeyTile k = key_tile(m, a);
-  const int group = m.heads / m.kv, KB = 32 * k.G, QT = 32 * k.S, nt = (m.N + KB - 1) / KB;
-  const long per = (long)m.kv * a.nseq;
-  auto steps = [&](int kt) { return (long)group * ((m.N - (m.causal ? KB * kt : 0) + QT - 1) / QT); };
-  a.unit = a.units = 0;
-  if (per == 0) return;
-  long all = 0;
-  for (int kt = 0; kt < nt; ++kt) all += steps(kt);
-  const long unit = k.S == 4 ? std::max<long>(all * per / 256, 2) : std::max<long>(all * per / 768, 8);
-  if (steps(0) <= 2 * unit) return;
-  a.unit = (int)unit;
-  for (int kt = 0; kt < nt; ++kt) a.units += (int)((steps(kt) + unit - 1) / unit);
+  const int group = m.heads / m.kv, KB = 32 * k.G, QT = 32 * k.S;
+  a.unit = cut((m.N + KB - 1) / KB, (long)m.kv * a.nseq, m.D == 128 && k.S > 1 ? 256 : 512, k.S,
+               [&](int kt) { return group * ((m.N - (m.causal ? KB * kt : 0) + QT - 1) / QT); }, a.units);
 }
-// And of dQ, in its blocks of 32 queries and 128 keys a step (variant 1): a.qunit, a.qunits.
-// The whole backward uncut and cut: 1 x 773, 2 heads of 128 34, 29 us; 1 x 3000, 1 head of 64 46,
-// 40; 1 x 700, 2 heads on 1 23, 21.
+// And of dQ, in the blocks of its variants 1 and 2 (of 1 and heads of 128 one fills a CU):
+// a.qunit, a.qunits. The whole backward uncut and cut: 1 x 2859, 2 heads of 128, causal 92,
+// 84 us; 1 x 3000, 1 head of 64 60, 56; 1 x 773, 2 heads of 128 39, 36.
 void cut_query_units(const DiffShape& m, DiffArgs& a) {
+  const int v = dq_variant(m, a), QB = v == 1 ? 32 : 64, KT = v == 1 ? 128 : 64;
   a.qunit = a.qunits = 0;
-  const long per = (long)m.heads * a.nseq;
-  if (per == 0 || dq_variant(m, a) != 1) return;
-  const int nt = (m.N + 31) / 32;
-  auto steps = [&](int qt) {
-    return m.causal ? query_steps<true, 32, 128>(m.N, qt) : query_steps<false, 32, 128>(m.N, qt);
-  };
-  long all = 0;
-  for (int qt = 0; qt < nt; ++qt) all += steps(qt);
-  const long unit = std::max<long>(all * per / 256, 2);
-  if (steps(nt - 1) <= 2 * unit) return;
-  a.qunit = (int)unit;
-  for (int qt = 0; qt < nt; ++qt) a.qunits += (int)((steps(qt) + unit - 1) / unit);
+  if (v != 1 && v != 2) return;
+  a.qunit = cut((m.N + QB - 1) / QB, (long)m.heads * a.nseq, m.D == 128 && v == 1 ? 256 : 512, KT / 32,
+                [&](int qt) { return ((m.causal ? std::min(QB * (qt + 1), m.N) : m.N) + KT - 1) / KT; },
+                a.qunits);
 }
 size_t part_bytes(const DiffShape& m, const DiffArgs& a) {
   return align256((size_t)a.units * m.kv * a.nseq * 32 * key_tile(m, a).G * 2 * m.D * sizeof(float));
@@ -1061,7 +1078,7 @@ hipError_t launch_dkdv(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   if (e != hipSuccess || (a.unit == 0 && a.qunit == 0)) return e;
   DiffArgs j = a;
   j.kblocks = a.unit > 0 ? (int)(tiles(a, a.kv, 32 * G) * (2 * D / 32)) : 0;
-  const long nq = a.qunit > 0 ? tiles(a, a.heads, 32) * (D / 32) : 0;
+  const long nq = a.qunit > 0 ? tiles(a, a.heads, S == 4 ? 32 : 64) * (D / 32) : 0;
   return traced(FLOWMOE_K_DIFF_JOIN, st, [&] {
     const dim3 g((unsigned)(j.kblocks + nq)), b(64 * G);
     if (m.causal) hipLaunchKernelGGL((diff_join_kernel<D, true, G, S>), g, b, 0, st, j);
@@ -1083,7 +1100,7 @@ size_t diff_attn_ws_bytes(const DiffShape& m, int T) {
   DiffArgs a = diff_args(m, T);
   cut_units(m, a);
   cut_query_units(m, a);
-  return part_bytes(m, a) + align256((size_t)a.qunits * m.heads * a.nseq * 32 * m.D * sizeof(float));
+  return part_bytes(m, a) + align256((size_t)a.qunits * m.heads * a.nseq * (dq_variant(m, a) == 1 ? 32 : 64) * m.D * sizeof(float));
 }
 
 hipError_t launch_diff_attn_fwd(const DiffShape& m, int T, const void* qkv, const float* lambda,

@@ -192,8 +192,8 @@ __global__ __launch_bounds__(256) void head_norm_kernel(NormArgs a) {
 }
 
 // dx = r (u - x r^2 mean(u x)), u = scale gain dy; dgain's sums over the block's rows go
-// to `part`, in a fixed order. As above 402 MB in 80 us, 5.0 TB/s, with the join's 4 us; 512,
-// 1024 and 2048 blocks 111, 82 and 91.
+// to `part`, in a fixed order. As above 402 MB in 76 us, 5.3 TB/s, with the join's 5 us; 512,
+// 1024 and 2048 blocks (with an older join of 7) 111, 82 and 91.
 template <typename T, int L, bool NT>
 __global__ __launch_bounds__(256) void head_norm_bwd_kernel(NormArgs a) {
   __shared__ float sums[256 * 8];

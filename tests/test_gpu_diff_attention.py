@@ -112,6 +112,14 @@ CASES = [
     (2, 700, 12, 4, 64, False, [700, 450]),
     (2, 700, 12, 2, 128, False, None),
     (3, 600, 3, 3, 128, True, [600, 2, 333]),
+    # dQ cut into units too, in blocks of 32 and of 64 queries, also past a valid length
+    (2, 773, 2, 1, 64, False, [773, 300]),
+    (1, 1500, 3, 3, 128, False, None),
+    (1, 3000, 1, 1, 64, True, [1800]),
+    (1, 2048, 8, 8, 128, True, [2000]),
+    (1, 1100, 14, 2, 64, False, None),
+    (2, 1100, 7, 7, 64, False, [40, 900]),
+    (1, 2100, 12, 4, 64, True, None),
     # sequences of two tiles and of one
     (90, 37, 6, 3, 128, True, None),
     (80, 64, 8, 4, 64, False, [n % 65 for n in range(80)]),
@@ -183,7 +191,7 @@ def test_large_scores(hd):
 
 @pytest.mark.parametrize("nseq,seq,heads,kv,hd,causal", [
     (2, 130, 4, 1, 64, True), (1, 200, 4, 4, 128, False), (40, 32, 4, 2, 128, True),
-    (9, 400, 8, 4, 128, True)])
+    (9, 400, 8, 4, 128, True), (1, 700, 4, 2, 64, False), (1, 2048, 8, 2, 128, True)])
 def test_lambda_of_any_sign(nseq, seq, heads, kv, hd, causal):
     """Zero, negative and large lambda, also among the heads that share a key head."""
     need_gpu()

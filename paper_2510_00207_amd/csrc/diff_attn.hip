@@ -964,6 +964,18 @@ void launch_dq(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   else hipLaunchKernelGGL((diff_dq_kernel<D, false, NW, S, ONE>), g, b, 0, st, a);
 }
 
+// A backward of few queries: blocks of 32, whose waves share each other's keys or queries.
+// Long sequences have so many steps that larger tiles cut into units read less: us of the
+// whole backward with such blocks and without: heads of 128, 1 x 459, 1 head 29, 36 (its
+// walk is the time); 2 x 300, 8 heads, causal 26, 28; 3 x 770, 3 heads 42, 53; 1 x 2000, 2 on 1
+// 52, 60; 2 x 1024, 4 on 1, causal 47, 46; 1 x 2048, 4 heads, causal 69, 58; 1 x 2859, 2 heads,
+// causal 69, 58; 1 x 6000, 1 head, causal 126, 75; heads of 64, 1 x 1000, 8 on 2, causal 32,
+// 36; 1 x 1500, 4 heads, causal 29, 32; 1 x 3000, 1 head 35, 38; 1 x 8000, 1 head, causal 74, 65.
+bool few_queries(const DiffShape& m, const DiffArgs& a) {
+  const long b32 = tiles(a, a.heads, 32);
+  return b32 <= 256 && b32 * m.N <= 256 * 1536;
+}
+
 // dQ blocks by the launch: 0: one wave of 32 queries (sequences of at most 32); 4: two of
 // 64 (at most 64); four waves that share 1: 32 queries, 2: 64, 3: 128. us of the whole
 // backward with 1, 2, 3: 2 x 512, 8 heads of 64, causal 34, 36, 42; 1 x 2048, heads of 128,
@@ -973,7 +985,7 @@ void launch_dq(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
 int dq_variant(const DiffShape& m, const DiffArgs& a) {
   if (m.N <= 32) return 0;
   const long b32 = tiles(a, a.heads, 32);
-  return b32 <= 256 ? 1 : m.N <= 64 ? 4 : b32 <= 2048 ? 2 : 3;
+  return few_queries(m, a) ? 1 : m.N <= 64 ? 4 : b32 <= 2048 ? 2 : 3;
 }
 
 template <int D>
@@ -1001,7 +1013,7 @@ struct KeyTile {
 };
 KeyTile key_tile(const DiffShape& m, const DiffArgs& a) {
   if (m.N <= 32) return {1, 1};
-  if (tiles(a, a.heads, 32) <= 256) return {1, 4};
+  if (few_queries(m, a)) return {1, 4};
   if (m.N <= 64) return {2, 1};
   if (m.D == 64) return tiles(a, a.kv, 128) < 1024 ? KeyTile{2, 2} : KeyTile{4, 1};
   // 128 keys by 32 queries: up to three such steps for each of 512 resident blocks

@@ -120,6 +120,8 @@ CASES = [
     (1, 1100, 14, 2, 64, False, None),
     (2, 1100, 7, 7, 64, False, [40, 900]),
     (1, 2100, 12, 4, 64, True, None),
+    (1, 4200, 1, 1, 128, True, [4100]),
+    (1, 3500, 2, 1, 64, False, [3500]),
     # sequences of two tiles and of one
     (90, 37, 6, 3, 128, True, None),
     (80, 64, 8, 4, 64, False, [n % 65 for n in range(80)]),

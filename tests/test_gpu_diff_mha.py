@@ -141,6 +141,25 @@ def test_steps_and_products(nseq, seq, heads, kv, hd, causal, lens, rot, layout)
         assert torch.equal(o2[n], o[n]), n
 
 
+def test_padded_rows_add_nothing():
+    """Other finite rows past the lengths: zeros in out and d_in, the same gradients."""
+    need_gpu()
+    lens = [700, 0, 33]
+    a, b = (Block(3, 700, 4, 2, 64, True, 31, lens) for _ in range(2))
+    pad = torch.cat([torch.arange(700) >= n for n in lens]).to(dev())
+    b.t["inp"][pad] *= -3
+    b.t["d_out"][pad] = 100.0
+    for x in (a, b):
+        x.fwd()
+        x.bwd()
+    x, y = a.outputs(), b.outputs()
+    for n in ("out", "d_in", "d_qkv", "attn"):
+        assert not bool(y[n][pad].any()), n
+        assert torch.equal(x[n], y[n]), n
+    for n in ("dw_qkv", "dw_o", "d_lambda", "dgain"):
+        assert torch.equal(x[n], y[n]), n
+
+
 def test_no_tokens():
     need_gpu()
     s, d, n = (L.make_shape(0, 256, 8, 1, 1, 0, L.BF16), L.make_diff_shape(64, 4, 2, 64, True),

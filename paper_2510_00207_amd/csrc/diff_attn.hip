@@ -46,6 +46,7 @@ struct DiffArgs {
   float* delta;          // 2 x heads x T: d1, d2
   float* d_lambda;       // heads
   int T, N, heads, kv, nseq;
+  int sub;               // N holds N / sub short sequences (tile_rows)
   int accumulate;        // add to d_lambda
   long M, W;             // columns of a row of A, of qkv
   float *part, *qpart;   // sums of units: dK and dV, dQ
@@ -60,6 +61,57 @@ struct DiffArgs {
 // the valid tokens of sequence sq
 __device__ __forceinline__ int seq_end(const DiffArgs& a, int sq) {
   return a.lens == nullptr ? a.N : min(max(a.lens[sq], 0), a.N);
+}
+
+// Sequences of at most 16 tokens: a tile holds as many whole ones as fit, N = 32 / sub * sub
+// tokens (the last tile of a call fewer), so that its rows and products are not empty. A bit
+// of `valid` is a row. us of one sequence a tile and of several: 3357 x 1 token, 16 heads of
+// 128, forward 112, 19, backward 424, 54; 1339 x 3, 8 heads (4) of 64, causal, backward 45, 19;
+// 452 x 10, 16 heads (8) of 128, causal 25, 22 and 65, 60.
+struct TileRows {
+  unsigned valid;
+  int end, rows;  // past the last valid one; of the call
+};
+__device__ __forceinline__ TileRows tile_rows(const DiffArgs& a, int sq) {
+  const int r = threadIdx.x & 31, rows = min(a.N, a.T - sq * a.N), s = r / a.sub;
+  bool v = r < rows;
+  if (v && a.lens != nullptr) v = r - s * a.sub < a.lens[sq * (a.N / a.sub) + s];
+  const unsigned valid = (unsigned)__ballot(v);
+  return {valid, 32 - __clz((int)valid), rows};
+}
+// the valid tokens that row r of them sees (causal), or is seen by
+template <bool CAUSAL, bool BY>
+__device__ __forceinline__ unsigned partners(const DiffArgs& a, unsigned valid, int r) {
+  const unsigned own = (~0u >> (32 - a.sub)) << (r / a.sub * a.sub), upto = (2u << r) - 1u;
+  const unsigned order = !CAUSAL ? ~0u : BY ? ~(upto >> 1) : upto;
+  return valid >> r & 1 ? valid & own & order : 0u;
+}
+// zeros in the rows of a tile between valid ones that are not (those past the last are not
+// loaded): what they hold must not reach a sum
+template <int D, int THREADS>
+__device__ __forceinline__ void clear_rows(char* tile, unsigned valid, int tid) {
+  for (int i = tid; i < 4 * D; i += THREADS)
+    if (!(valid >> (i / (D / 8)) & 1)) reinterpret_cast<float4*>(tile)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+// A product multiplies another sequence's rows by zeros, which holds for finite ones only:
+// a tile of several sequences where this finds an infinity or a NaN in a product's rows is
+// run again a sequence at a time (the others' rows cleared).
+template <int D>
+__device__ __forceinline__ bool not_finite(const char* tile, int lane) {
+  typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+  u16x8 top = 0;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+    top = __builtin_elementwise_max(top, reinterpret_cast<const u16x8*>(tile)[64 * i + lane] & (unsigned short)0x7FFF);
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) bad = bad || top[i] >= 0x7F80;
+  return __any(bad);
+}
+// x, or `other` where bit i of `seen` is not set
+__device__ __forceinline__ float where_bit(unsigned seen, int i, float x, float other) {
+  const unsigned m = (unsigned)__builtin_amdgcn_sbfe((int)seen, i, 1);
+  return __uint_as_float((__float_as_uint(x) & m) | (__float_as_uint(other) & ~m));
 }
 
 // block -> (tile, head, sequence): tiles of the most causal work first (`rev`: the
@@ -101,25 +153,26 @@ struct FwdTile {
   static constexpr int G = NW / (2 * S), QB = 32 * G;  // groups of 32 queries, queries
   static constexpr int KB = S == 1 && NW == 8 ? 2 : 1, KT = 32 * KB * S;  // keys of a wave / 32, of a tile
 };
-template <int D, bool CAUSAL, int NW, int S, bool ONE>
-__global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffArgs a) {
+// The tile's rows in `own` are written; false: none, its sequences have to run one by one.
+template <int D, bool CAUSAL, int NW, int S, int ONE>
+__device__ __forceinline__ bool diff_fwd_tile(const DiffArgs& a, char* lds, float2* stat,
+                                              const TileRows& tr, unsigned own, int qt, int hd, int sq) {
   using Tile = FwdTile<NW, S>;
-  constexpr int SL = ONE ? 1 : 2;  // slots: ONE for sequences of one tile (more blocks to a CU)
+  // slots: ONE for sequences of one tile (1) or less (2) (more blocks to a CU)
+  constexpr int SL = ONE ? 1 : 2;
+  constexpr bool PACK = ONE == 2;  // several to a tile
   constexpr int KS = D / 32, DB = D / 32, QB = Tile::QB, KT = Tile::KT;  // KS: k steps of one map
   using Dma = TileDma<D, KT, NW>;
   constexpr int TB = Dma::TB;
-  // K slots, then V slots; at the end the waves' outputs (float)
-  __shared__ __attribute__((aligned(1024))) char lds[2 * SL * TB];
-  __shared__ float2 stat[S > 1 ? NW * 64 : 1];  // and their references and sums
   static_assert(2 * SL * TB >= (S > 1 ? NW : NW / 2) * 32 * D * 4, "the outputs fit the tiles' place");
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
   const int map = w & 1, grp = (w >> 1) % Tile::G, part = (w >> 1) / Tile::G;
-  int qt, hd, sq;
-  diff_decode(a, a.heads, CAUSAL, QB, qt, hd, sq);
-  const int end = seq_end(a, sq);
+  const int end = tr.end;
   const long tok0 = (long)sq * a.N, ld = a.W;
   const int q0 = qt * QB, qw = q0 + 32 * grp + lq;
+  const unsigned seen = PACK ? partners<CAUSAL, false>(a, tr.valid, lq) : 0u;
+  const bool live = PACK ? seen != 0u : qw < end;
 
   floatx16 o[DB];
 #pragma unroll
@@ -139,12 +192,12 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
     bf16x8 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-      qf[ks] = qw < end ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * (KS * map + ks) + 8 * h2)
-                        : zero8();
+      qf[ks] = live ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * (KS * map + ks) + 8 * h2)
+                    : zero8();
     l = 0.0f;
     int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
 
-    auto step = [&](const int t, auto stc) {
+    auto step = [&](const int t, auto stc) __attribute__((always_inline)) {
       constexpr int st = decltype(stc)::value;
       opaque(rbase, tb0, tb1);
       wait_vm<0>();   // K(t) and V(t): loaded a step ago
@@ -166,7 +219,10 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
 #pragma unroll
         for (int i = 0; i < KS; ++i)
           s = mfma(frag_row_x<D>(tk, rbase, 32 * kb, KS * map + i), qf[i], i == 0 ? zero16() : s);
-        if (kb0 + 32 > end || (CAUSAL && kb0 + 31 > q0 + 32 * grp)) {
+        if constexpr (PACK) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = where_bit(seen >> 4 * h2, 8 * (r >> 2) + (r & 3), s[r], -INFINITY);
+        } else if (kb0 + 32 > end || (CAUSAL && kb0 + 31 > q0 + 32 * grp)) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int key = kb0 + 8 * (r >> 2) + 4 * h2 + (r & 3);
@@ -211,6 +267,15 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
       }
     };
     if constexpr (ONE) {
+      if constexpr (PACK) {
+        wait_vm<0>();
+        lds_barrier();
+        if (tr.valid & (tr.valid + 1)) {
+          clear_rows<D, 64 * NW>(lds + TB, tr.valid, tid);
+          lds_barrier();
+        }
+        if (own == ~0u && not_finite<D>(lds + TB, lane)) return false;
+      }
       step(0, Stage<0>{});
     } else {
       for (int t = 0; t < nk; t += 2) {
@@ -268,11 +333,12 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
         o[db] = s;
       }
     }
-    const float inv = qw < end ? 1.0f / l : 0.0f;
-    const float lam = qw < end ? a.lambda[hd] : 0.0f;
+    const float inv = live ? 1.0f / l : 0.0f;
+    const float lam = live ? a.lambda[hd] : 0.0f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       if (S > 1 && db % S != part) continue;
+      if (PACK && !live) o[db] = zero16();  // (it saw no key: NaN)
       o[db] *= inv;
       if (map == 1) put(slot(1, part, db), o[db]);
     }
@@ -291,7 +357,7 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
       }
     }
   }
-  if (qw >= a.N) return;
+  if (qw >= tr.rows || (PACK && !(own >> lq & 1))) return true;
   bf16_t* out = map == 0 ? a.out : a.out2;
   if (out != nullptr) {
     bf16_t* Og = out + (tok0 + qw) * a.M + (long)hd * D;
@@ -300,7 +366,41 @@ __global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffA
       if (S == 1 || db % S == part) store_cols(Og + 32 * db, o[db], h2, 1.0f);
   }
   if (h2 == 0 && part == 0 && a.lse != nullptr)
-    a.lse[((long)map * a.heads + hd) * a.T + tok0 + qw] = qw < end ? (m + log2f(l)) * kLn2 : 0.0f;
+    a.lse[((long)map * a.heads + hd) * a.T + tok0 + qw] = live ? (m + log2f(l)) * kLn2 : 0.0f;
+  return true;
+}
+
+// run(rows, own) for a tile of short sequences, or (it gives false) for each of them
+template <class F>
+__device__ __forceinline__ void run_short(const DiffArgs& a, int sq, F&& run) {
+  const TileRows tr = tile_rows(a, sq);
+  TileRows part = tr;
+  unsigned own = ~0u;
+  for (int r = 0;; r += a.sub) {
+    if (run(part, own) && own == ~0u) return;
+    if (own == ~0u) r = -a.sub;  // (from here on one by one)
+    if (r + a.sub >= tr.rows) return;
+    own = (~0u >> (32 - a.sub)) << (r + a.sub);
+    part.valid = tr.valid & own;
+    part.end = 32 - __clz((int)part.valid);
+    wait_vm<0>();
+    lds_barrier();
+  }
+}
+
+template <int D, bool CAUSAL, int NW, int S, int ONE>
+__global__ __launch_bounds__(64 * NW, S == 1 ? 4 : 2) void diff_fwd_kernel(DiffArgs a) {
+  using Tile = FwdTile<NW, S>;
+  // K slots, then V slots; at the end the waves' outputs (float)
+  __shared__ __attribute__((aligned(1024))) char lds[(ONE ? 2 : 4) * TileDma<D, Tile::KT, NW>::TB];
+  __shared__ float2 stat[S > 1 ? NW * 64 : 1];  // and their references and sums
+  int qt, hd, sq;
+  diff_decode(a, a.heads, CAUSAL, Tile::QB, qt, hd, sq);
+  auto run = [&](const TileRows& tr, unsigned own) __attribute__((always_inline)) {
+    return diff_fwd_tile<D, CAUSAL, NW, S, ONE>(a, lds, stat, tr, own, qt, hd, sq);
+  };
+  if constexpr (ONE == 2) run_short(a, sq, run);
+  else run(TileRows{0u, seq_end(a, sq), a.N}, ~0u);
 }
 
 // S waves (the parts of a group) that hold sums of the same NB 32-row blocks: each hands
@@ -394,35 +494,23 @@ __device__ __forceinline__ UnitAt find_unit(int nt, int unit, F&& steps, int u, 
 // causal: 864 TFLOP/s of its 6 D flops a pair). The clock falls to 1.85 GHz with the matrix
 // pipes 45 % busy: power bounds it. Running dP and the first map's scores a tile ahead,
 // beside the elementwise work, measured 2 % slower (18 % with heads of 64).
-template <int D, bool CAUSAL, int NW, int S, bool ONE>
-__global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
-  constexpr int SL = ONE ? 1 : 2;  // slots: ONE for sequences of one tile
+template <int D, bool CAUSAL, int NW, int S, int ONE>
+__device__ __forceinline__ bool diff_dq_tile(const DiffArgs& a, char* lds, const TileRows& tr,
+                                             unsigned own, int qt, int hd, int sq, int units, int chunk) {
+  constexpr int SL = ONE ? 1 : 2;  // slots: ONE for sequences of one tile (1) or less (2)
+  constexpr bool PACK = ONE == 2;
   constexpr int KS = D / 16, DB = D / 32, G = NW / S, QB = 32 * G, KT = 32 * S;
   using Dma = TileDma<D, KT, NW>;
   using DmaG = TileDma<D, QB, NW>;
   constexpr int TB = Dma::TB, VB = SL * TB, GB = 2 * VB;  // K slots, V slots, the dO rows
-  __shared__ __attribute__((aligned(1024))) char lds[GB + QB * D * 2];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
   const int grp = w % G, part = w / G;
-  int qt, hd, sq, units = 1, chunk = 0;
-  if (a.qunit > 0) {
-    const int per = a.heads * a.nseq, rest = (int)(blockIdx.x % per);
-    const UnitAt at = find_unit((a.N + QB - 1) / QB, a.qunit,
-                                [&](int k) { return query_steps<CAUSAL, QB, KT>(a.N, k); },
-                                blockIdx.x / per, 0);
-    qt = at.kt;
-    units = at.units;
-    chunk = at.chunk;
-    hd = rest % a.heads;
-    sq = rest / a.heads;
-  } else {
-    diff_decode(a, a.heads, CAUSAL, QB, qt, hd, sq);
-  }
-  const int end = seq_end(a, sq);
+  const int end = tr.end;
   const long tok0 = (long)sq * a.N, ld = a.W;
   const int q0 = qt * QB, qw = q0 + 32 * grp + lq;
-  const bool live = qw < end;
+  const unsigned seen = PACK ? partners<CAUSAL, false>(a, tr.valid, lq) : 0u;
+  const bool live = PACK ? seen != 0u : qw < end;
   const long srow = (long)hd * a.T + tok0 + qw, smap = (long)a.heads * a.T;
   const float lam = a.lambda[hd];
 
@@ -475,7 +563,7 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
     // at k step i; then DB groups of K transposed, 16 keys by 64 columns each
     constexpr int NG = KS + DB, RS = 2;
     bf16x8 fr[RS][3];
-    auto read_group = [&](const char* tk, const char* tv, int i) {
+    auto read_group = [&](const char* tk, const char* tv, int i) __attribute__((always_inline)) {
       if (i < KS) {
         fr[i % RS][0] = frag_row_x<D>(tk, rbase, 0, i);
         fr[i % RS][1] = frag_row_x<D>(tv, rbase, 0, i);
@@ -487,7 +575,7 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
                                       32 * (2 * ((i - KS) % (DB / 2)) + u));
       }
     };
-    auto step = [&](const int t, auto stc) {
+    auto step = [&](const int t, auto stc) __attribute__((always_inline)) {
       constexpr int st = decltype(stc)::value;
       opaque(rbase, tb0, tb1);
       wait_vm<0>();   // K(t) and V(t): loaded a step ago
@@ -516,7 +604,7 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
         dp = mfma(fr[i % RS][1], fr[i % RS][2], dp);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (kb0 + 32 > end || (CAUSAL && kb0 + 31 > q0 + 32 * grp)) {
+      if (!PACK && (kb0 + 32 > end || (CAUSAL && kb0 + 31 > q0 + 32 * grp))) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = kb0 + 8 * (r >> 2) + 4 * h2 + (r & 3);
@@ -532,6 +620,11 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
         for (int j = 0; j < 2; ++j) {
           e[j] = exp2_fast(fmaf(s[0][r + j], a.c2, -l1)) * dp[r + j];
           f[j] = exp2_fast(fmaf(s[1][r + j], a.c2, -l2)) * (dp[r + j] + dd);
+          if constexpr (PACK) {
+            const int k = 8 * (r >> 2) + (r & 3) + j;
+            e[j] = where_bit(seen >> 4 * h2, k, e[j], 0.0f);
+            f[j] = where_bit(seen >> 4 * h2, k, f[j], 0.0f);
+          }
         }
         pw[0][r >> 1] = pack_bf16x2(e[0], e[1]);
         pw[1][r >> 1] = pack_bf16x2(f[0], f[1]);  // (times -lambda at the end)
@@ -553,6 +646,15 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
       }
     };
     if constexpr (ONE) {
+      if constexpr (PACK) {
+        wait_vm<0>();
+        lds_barrier();
+        if (tr.valid & (tr.valid + 1)) {
+          clear_rows<D, 64 * NW>(lds, tr.valid, tid);
+          lds_barrier();
+        }
+        if (own == ~0u && not_finite<D>(lds, lane)) return false;
+      }
       step(0, Stage<0>{});
     } else {
       for (int t = t0; t < nk; t += 2) {
@@ -579,14 +681,14 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
         if (i / 4 % S == part) x[i * 64 * G] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
       }
     }
-    if (chunk > 0) return;  // (the first unit writes the rows' d1 and d2)
+    if (chunk > 0) return true;  // (the first unit writes the rows' d1 and d2)
   }
-  if (qw >= a.N) return;
+  if (qw >= tr.rows || (PACK && !(own >> lq & 1))) return true;
   if (lead) {
     a.delta[srow] = d1;
     a.delta[srow + smap] = d2;
   }
-  if (units > 1) return;
+  if (units > 1) return true;
   bf16_t* dst = a.d_qkv + (tok0 + qw) * ld + (long)hd * D;
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
@@ -594,6 +696,32 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
     if (!live) dq[db] = zero16();
     store_cols(dst + 32 * db, dq[db], h2, db >= DB / 2 ? -lam * a.rs : a.rs);
   }
+  return true;
+}
+
+template <int D, bool CAUSAL, int NW, int S, int ONE>
+__global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
+  constexpr int QB = 32 * NW / S, KT = 32 * S;
+  __shared__ __attribute__((aligned(1024))) char lds[(ONE ? 2 : 4) * TileDma<D, KT, NW>::TB + QB * D * 2];
+  int qt, hd, sq, units = 1, chunk = 0;
+  if (a.qunit > 0) {
+    const int per = a.heads * a.nseq, rest = (int)(blockIdx.x % per);
+    const UnitAt at = find_unit((a.N + QB - 1) / QB, a.qunit,
+                                [&](int k) { return query_steps<CAUSAL, QB, KT>(a.N, k); },
+                                blockIdx.x / per, 0);
+    qt = at.kt;
+    units = at.units;
+    chunk = at.chunk;
+    hd = rest % a.heads;
+    sq = rest / a.heads;
+  } else {
+    diff_decode(a, a.heads, CAUSAL, QB, qt, hd, sq);
+  }
+  auto run = [&](const TileRows& tr, unsigned own) __attribute__((always_inline)) {
+    return diff_dq_tile<D, CAUSAL, NW, S, ONE>(a, lds, tr, own, qt, hd, sq, units, chunk);
+  };
+  if constexpr (ONE == 2) run_short(a, sq, run);
+  else run(TileRows{0u, seq_end(a, sq), a.N}, ~0u);
 }
 
 // dlambda_h = -sum of d2 over all rows, by a block
@@ -628,9 +756,10 @@ __device__ __forceinline__ void sum_d_lambda(const DiffArgs& a, int hd, float* p
 // registers at D = 128) and the K fragments leave none to read ahead of the products: with
 // read groups as in dQ 1570 us, the plain order 1350 (4 x 4096 tokens, 32 heads of 128,
 // causal: 815 TFLOP/s of its 8 D flops a pair, the clock at 2.0 GHz).
-template <int D, bool CAUSAL, int NW, int S, bool ONE>
-__global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
-  constexpr int SL = ONE ? 1 : 2;  // slots: ONE for sequences of one tile
+template <int D, bool CAUSAL, int NW, int S, int ONE>
+__global__ __launch_bounds__(64 * NW, ONE == 2 && D == 128 ? 1 : 2) void diff_dkdv_kernel(DiffArgs a) {
+  constexpr int SL = ONE ? 1 : 2;  // slots: ONE for sequences of one tile (1) or less (2)
+  constexpr bool PACK = ONE == 2;
   constexpr int KS = D / 16, DB = D / 32, G = NW / S, KB = 32 * G, QT = 32 * S;
   using Dma = TileDma<D, QT, NW>;
   using DmaV = TileDma<D, KB, NW>;
@@ -658,10 +787,15 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
     units = at.units;
     chunk = at.chunk;
   }
-  const int end = seq_end(a, sq);
+  TileRows tr = PACK ? tile_rows(a, sq) : TileRows{0u, seq_end(a, sq), a.N};
+  const unsigned all = tr.valid;
+  unsigned own = ~0u;  // (as in run_short, which as a function cost this kernel its registers)
+one:
+  const int end = tr.end;
   const long tok0 = (long)sq * a.N, ld = a.W;
   const int k0 = kt * KB, kw = k0 + 32 * grp + lq;
-  const bool live = kw < end;
+  const unsigned seen = PACK ? partners<CAUSAL, true>(a, tr.valid, lq) : 0u;
+  const bool live = PACK ? seen != 0u : kw < end;
   const long kcol = a.M + (long)kh * D, vcol = kcol + (long)a.kv * D;
   floatx16 dv[DB], dk[DB];
 #pragma unroll
@@ -701,14 +835,14 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
       const int srow = 32 * (tid >> 6) + lq;
       const float* sp = (isd ? a.delta : a.lse) + (long)hd * a.T + tok0 + srow;
       const long smap = (long)a.heads * a.T;
-      auto load_stat = [&](int qb) {
+      auto load_stat = [&](int qb) __attribute__((always_inline)) {
         if (tid < 64 * S) {
           const bool in = qb + srow < end;
           const float x = in ? sp[qb] : 0.0f, y = in ? sp[qb + smap] : 0.0f;
           rstat = isd ? make_float2(-x, sgn * (y - x)) : make_float2(x * kLog2e, y * kLog2e - llam);
         }
       };
-      auto store_stat = [&](int slot) {
+      auto store_stat = [&](int slot) __attribute__((always_inline)) {
         if (tid < 64 * S) {
           float* s = reinterpret_cast<float*>(lds + ST + SB * slot) + 128 * (tid >> 6) + (isd ? 64 : 0) + lq;
           s[0] = rstat.x;
@@ -726,7 +860,7 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
       store_stat(0);
 
       constexpr int H = KS / 2;
-      auto step = [&](const int it, auto stc) {
+      auto step = [&](const int it, auto stc) __attribute__((always_inline)) {
         constexpr int st = decltype(stc)::value;
         opaque(rbase, tb0, tb1);
         const int qt0 = qs0 + QT * it, qb = qt0 + 32 * part;
@@ -746,8 +880,8 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
         // a K fragment, whose reload waits for the loads under way, 8 % of the time)
         if (((S == 1 && CAUSAL) || qb < end) && (!CAUSAL || qb + 31 >= k0 + 32 * grp)) {
           const bool edge = qb + 32 > end || (CAUSAL && k0 + 32 * grp + 31 > qb);
-          auto mask = [&](floatx16& s) {
-            if (edge) {
+          auto mask = [&](floatx16& s) __attribute__((always_inline)) {
+            if (!PACK && edge) {
 #pragma unroll
               for (int r = 0; r < 16; ++r) {
                 const int q = qb + 8 * (r >> 2) + 4 * h2 + (r & 3);
@@ -755,7 +889,7 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
               }
             }
           };
-          auto row4 = [&](int k, int J) { return *reinterpret_cast<const float4*>(stat + 32 * k + 8 * J); };
+          auto row4 = [&](int k, int J) __attribute__((always_inline)) { return *reinterpret_cast<const float4*>(stat + 32 * k + 8 * J); };
           floatx16 s1, s2, dp;
           unsigned pp[8], pd[2][8];  // P_1 - lambda P_2 and dS of each map, bf16 pairs
           const char* tg = tq + TQ;
@@ -787,6 +921,11 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
               p[j] = fmaf(-sgn, p2, p1);
               e[j] = p1 * dp[r];
               f[j] = p2 * fmaf(-sgn, dp[r], dd[j]);
+              if constexpr (PACK) {
+                p[j] = where_bit(seen >> 4 * h2, 8 * J + j, p[j], 0.0f);
+                e[j] = where_bit(seen >> 4 * h2, 8 * J + j, e[j], 0.0f);
+                f[j] = where_bit(seen >> 4 * h2, 8 * J + j, f[j], 0.0f);
+              }
             }
 #pragma unroll
             for (int j = 0; j < 4; j += 2) {
@@ -809,6 +948,23 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
         if (!ONE && it + 1 < it1) store_stat(st ^ 1);
       };
       if constexpr (ONE) {
+        if constexpr (PACK) {
+          wait_vm<0>();
+          lds_barrier();
+          if (tr.valid & (tr.valid + 1)) {
+            clear_rows<D, 64 * NW>(lds, tr.valid, tid);
+            clear_rows<D, 64 * NW>(lds + TQ, tr.valid, tid);
+            lds_barrier();
+          }
+          if (own == ~0u && (not_finite<D>(lds, lane) || not_finite<D>(lds + TQ, lane)))
+          {
+            own = ~0u >> (32 - a.sub);
+            tr.valid = all & own;
+            tr.end = 32 - __clz((int)tr.valid);
+            lds_barrier();
+            goto one;
+          }
+        }
         step(it0, Stage<0>{});
       } else {
         for (int it = it0; it < it1; it += 2) {
@@ -826,16 +982,17 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
     add_parts<S>(dv, lds, grp, part, lane);
   }
   if (units > 1) {
-    if (k0 >= end) return;
+    if (!PACK && k0 >= end) return;
     float4* x = reinterpret_cast<float4*>(a.part) +
                 ((long)rest * a.units + blockIdx.x / per) * (8 * DB * 64 * G) + 64 * grp + lane;
 #pragma unroll
     for (int i = 0; i < 8 * DB; ++i) {
       const floatx16& v = i < 4 * DB ? dk[i / 4] : dv[i / 4 - DB];
       const int r = 4 * (i % 4);
-      if (i / 4 % DB % S == part) x[i * 64 * G] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
+      if (i / 4 % DB % S == part && (!PACK || (own >> lq & 1)))
+        x[i * 64 * G] = make_float4(v[r], v[r + 1], v[r + 2], v[r + 3]);
     }
-  } else if (kw < a.N) {  // (rows past the end: their accumulators hold only masked zeros)
+  } else if (kw < tr.rows && (!PACK || (own >> lq & 1))) {  // (rows past the end: their accumulators hold only masked zeros)
     bf16_t* dst = a.d_qkv + (tok0 + kw) * ld;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
@@ -844,6 +1001,16 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dkdv_kernel(DiffArgs a) {
       store_cols(dst + kcol + 32 * db, dk[db], h2, a.rs);
       store_cols(dst + vcol + 32 * db, dv[db], h2, 1.0f);
     }
+  }
+  if constexpr (PACK) {
+    if (own == ~0u) return;
+    own <<= a.sub;
+    if ((own & (~0u >> (32 - tr.rows))) == 0u) return;
+    tr.valid = all & own;
+    tr.end = 32 - __clz((int)tr.valid);
+    wait_vm<0>();
+    lds_barrier();
+    goto one;
   }
 }
 
@@ -865,9 +1032,10 @@ __global__ __launch_bounds__(64 * G) void diff_join_kernel(DiffArgs a) {
       q ? find_unit(nt, a.qunit, [&](int k) { return query_steps<CAUSAL, 32 * GQ, 32 * SQ>(a.N, k); }, -1, tile)
         : find_unit(nt, a.unit, [&](int k) { return group * key_steps<CAUSAL, KB, QT>(a.N, k); }, -1, tile);
   if (at.units == 1) return;
-  const int end = seq_end(a, sq), r0 = tile * 32 * g, rw = r0 + 32 * (tid >> 6) + (lane & 31);
+  const int rw = tile * 32 * g + 32 * (tid >> 6) + (lane & 31);
+  const TileRows tr = G * S == 1 ? tile_rows(a, sq) : TileRows{0u, seq_end(a, sq), a.N};
   floatx16 s = zero16();
-  if (rw < end) {
+  if (G * S == 1 ? tr.valid >> rw & 1 : rw < tr.end) {
     const int U = 4 * cols * 64 * g;  // float4s of a unit
     const float4* x = reinterpret_cast<const float4*>(q ? a.qpart : a.part) +
                       ((long)rest * (q ? a.qunits : a.units) + at.chunk) * U + 4 * col * 64 * g + tid;
@@ -879,7 +1047,7 @@ __global__ __launch_bounds__(64 * G) void diff_join_kernel(DiffArgs a) {
       }
     }
   }
-  if (rw >= a.N) return;
+  if (rw >= tr.rows) return;
   bf16_t* row = a.d_qkv + ((long)sq * a.N + rw) * a.W;
   if (q) {
     store_cols(row + (long)hd * D + 32 * col, s, lane >> 5, col >= DB / 2 ? -a.lambda[hd] * a.rs : a.rs);
@@ -896,6 +1064,12 @@ DiffArgs diff_args(const DiffShape& m, int T) {
   a.heads = m.heads;
   a.kv = m.kv;
   a.nseq = T / m.N;
+  a.sub = m.N;
+  if (m.N <= 16) {
+    const int n = 32 / m.N;
+    a.N = n * m.N;
+    a.nseq = (a.nseq + n - 1) / n;
+  }
   a.M = (long)m.heads * m.D;
   a.W = a.M + 2L * m.kv * m.D;
   a.c2 = kLog2e / sqrtf((float)(m.D / 2));
@@ -907,7 +1081,7 @@ long tiles(const DiffArgs& a, int heads, int rows) {
   return (long)((a.N + rows - 1) / rows) * heads * a.nseq;
 }
 
-template <int D, int NW, int S, bool ONE = false>
+template <int D, int NW, int S, int ONE = 0>
 void launch_fwd(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   const dim3 g((unsigned)tiles(a, a.heads, FwdTile<NW, S>::QB)), b(64 * NW);
   if (m.causal) hipLaunchKernelGGL((diff_fwd_kernel<D, true, NW, S, ONE>), g, b, 0, st, a);
@@ -923,8 +1097,8 @@ void launch_fwd(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
 // 4 x 4096, 32 heads 1719, 1648, 904, 885; 8 x 2048, 16 heads, bidirectional 803, 736,
 // 424, 413; 50 x 300 -, 155, 78, 90; 32 x 512, 32 heads -, 443, 241, 246. Heads of 64 leave
 // room for more blocks of variant 1: 1 x 4485, 8 heads, variant 1 53, 2 86. 4: sequences of
-// one tile, 32 queries by 2 waves: 407 x 1, 8 heads of 128 10, variant 2 19; 452 x 10, 16
-// heads 25, 38.
+// one tile or less, 32 queries by 2 waves: 407 x 1, 8 heads of 128 5, variant 2 19; 452 x 10,
+// 16 heads 22, 38.
 int fwd_variant(const DiffShape& m, const DiffArgs& a) {
   const long b32 = tiles(a, a.heads, 32), b128 = tiles(a, a.heads, 128);
   if (m.N <= 32) return 4;
@@ -953,10 +1127,11 @@ void launch_fwd_variant(int v, const DiffShape& m, const DiffArgs& a, hipStream_
   else if (v == 1) launch_fwd<D, 4, 2>(m, a, st);
   else if (v == 2) launch_fwd<D, 4, 1>(m, a, st);
   else if (v == 3) launch_fwd<D, 8, 1>(m, a, st);
-  else launch_fwd<D, 2, 1, true>(m, a, st);
+  else if (m.N > 16) launch_fwd<D, 2, 1, 1>(m, a, st);
+  else launch_fwd<D, 2, 1, 2>(m, a, st);
 }
 
-template <int D, int NW, int S, bool ONE = false>
+template <int D, int NW, int S, int ONE = 0>
 void launch_dq(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   const long n = a.qunit > 0 ? (long)a.qunits * a.heads * a.nseq : tiles(a, a.heads, 32 * NW / S);
   const dim3 g((unsigned)n), b(64 * NW);
@@ -991,7 +1166,8 @@ int dq_variant(const DiffShape& m, const DiffArgs& a) {
 template <int D>
 void launch_dq_variant(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   const int v = dq_variant(m, a);
-  if (v == 0) launch_dq<D, 1, 1, true>(m, a, st);
+  if (v == 0 && m.N > 16) launch_dq<D, 1, 1, 1>(m, a, st);
+  else if (v == 0) launch_dq<D, 1, 1, 2>(m, a, st);
   else if (v == 4) launch_dq<D, 2, 1>(m, a, st);
   else if (v == 1) launch_dq<D, 4, 4>(m, a, st);
   else if (v == 2) launch_dq<D, 4, 2>(m, a, st);
@@ -1079,7 +1255,7 @@ size_t part_bytes(const DiffShape& m, const DiffArgs& a) {
   return align256((size_t)a.units * m.kv * a.nseq * 32 * key_tile(m, a).G * 2 * m.D * sizeof(float));
 }
 
-template <int D, int G, int S, bool ONE = false>
+template <int D, int G, int S, int ONE = 0>
 hipError_t launch_dkdv(const DiffShape& m, const DiffArgs& a, hipStream_t st) {
   const long n = a.unit > 0 ? (long)a.units * a.kv * a.nseq : tiles(a, a.kv, 32 * G);
   const hipError_t e = traced(FLOWMOE_K_DIFF_BWD_DKDV, st, [&] {
@@ -1103,7 +1279,8 @@ hipError_t launch_dkdv_variant(const DiffShape& m, const DiffArgs& a, hipStream_
   const KeyTile k = key_tile(m, a);
   if (k.G == 4) return launch_dkdv<D, 4, 1>(m, a, st);
   if (k.G == 2) return k.S == 2 ? launch_dkdv<D, 2, 2>(m, a, st) : launch_dkdv<D, 2, 1>(m, a, st);
-  return k.S == 4 ? launch_dkdv<D, 1, 4>(m, a, st) : launch_dkdv<D, 1, 1, true>(m, a, st);
+  if (k.S == 4) return launch_dkdv<D, 1, 4>(m, a, st);
+  return m.N > 16 ? launch_dkdv<D, 1, 1, 1>(m, a, st) : launch_dkdv<D, 1, 1, 2>(m, a, st);
 }
 
 }  // namespace

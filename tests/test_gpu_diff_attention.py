@@ -122,6 +122,12 @@ CASES = [
     (1, 2100, 12, 4, 64, True, None),
     (1, 4200, 1, 1, 128, True, [4100]),
     (1, 3500, 2, 1, 64, False, [3500]),
+    # several sequences to a tile, the last tile not full, rows between that are not valid
+    *[(n, s, 4, 2, d, c, [(7 * i) % (s + 2) - 1 for i in range(n)] if l else None)
+      for n, s in ((1, 1), (32, 1), (70, 1), (33, 2), (21, 3), (13, 5), (4, 10), (5, 11), (3, 16), (5, 17))
+      for d, c, l in ((64, True, False), (64, False, True), (128, True, True))],
+    (300, 1, 40, 1, 64, False, None),
+    (9, 7, 40, 1, 128, True, [7, 0, 3, 7, 7, 1, 0, 0, 5]),
     # sequences of two tiles and of one
     (90, 37, 6, 3, 128, True, None),
     (80, 64, 8, 4, 64, False, [n % 65 for n in range(80)]),
@@ -170,6 +176,36 @@ def test_padding_may_hold_anything(hd, causal):
         assert not bool(y[n][pad].any()), n
     for n in ("lse", "delta"):
         assert not bool(y[n][:, :, pad].any()), n
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("seq", [1, 3, 10, 16])
+def test_short_sequences_stay_apart(seq, hd, causal):
+    """NaN and infinities of a sequence, or past its length, reach no other one."""
+    need_gpu()
+    nseq, heads, kv = 40, 2, 1
+    lens = [seq - n % 2 for n in range(nseq)]
+    qkv, lam, d_attn = make(nseq, seq, heads, kv, hd, 6)
+    a = Call(nseq, seq, heads, kv, hd, causal, qkv, lam, d_attn, lens)
+    a.fwd()
+    a.bwd()
+    bad = torch.zeros(nseq, dtype=torch.bool, device=dev())
+    bad[[0, 5, 6, 38]] = True
+    bad = bad.repeat_interleave(seq)
+    pad = torch.cat([torch.arange(seq) >= n for n in lens]).to(dev())
+    q2, g2 = qkv.clone(), d_attn.clone()
+    q2[bad, ::3], g2[bad, 1::3] = float("inf"), float("nan")
+    q2[pad], g2[pad] = float("nan"), float("inf")
+    b = Call(nseq, seq, heads, kv, hd, causal, q2, lam, g2, lens)
+    b.fwd()
+    b.bwd()
+    x, y = a.outputs(), b.outputs()
+    for n in ("attn", "attn2", "d_qkv"):
+        assert torch.equal(x[n][~bad], y[n][~bad]), n
+        assert not bool(y[n][pad].any()), n
+    for n in ("lse", "delta"):
+        assert torch.equal(x[n][:, :, ~bad], y[n][:, :, ~bad]), n
 
 
 @pytest.mark.parametrize("hd", [64, 128])

@@ -457,7 +457,7 @@ typedef struct {
   int32_t heads;    /* heads that turn, side by side from column 0: heads * head_dim <= M */
   int32_t head_dim; /* a multiple of 8, 8..512 */
   int32_t rot_dim;  /* columns of a head that turn, its first: even, 2..head_dim; the
-                       others are copied */
+                       others are copied, bit for bit */
   int32_t layout;   /* FLOWMOE_ROPE_HALF: columns i and i + rot_dim / 2 are a pair;
                        FLOWMOE_ROPE_PAIRS: columns 2 i and 2 i + 1 */
   int32_t scaling;  /* FLOWMOE_ROPE_NONE .. _BANDS */

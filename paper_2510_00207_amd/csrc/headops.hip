@@ -44,6 +44,27 @@ __device__ __forceinline__ double pair_turns(const RopeArgs& a, int i) {
   return f * a.scale;
 }
 
+// Of 8 columns the first n turned (p), the others as they came, bit for bit: a computed
+// copy would spread infinities and NaN and lose the sign of zeros. (n is even.)
+template <bool NT>
+__device__ __forceinline__ void store_turned(bf16_t* y, const float p[8], const Raw8b& r, int n) {
+  u32x4v_t q;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) q[w] = 2 * w < n ? pack_bf16x2(p[2 * w], p[2 * w + 1]) : r.a[w];
+  st16<NT>(reinterpret_cast<u32x4v_t*>(y), q);
+}
+template <bool NT>
+__device__ __forceinline__ void store_turned(float* y, const float p[8], const Raw8f& r, int n) {
+  u32x4v_t lo, hi;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    lo[i] = i < n ? __float_as_uint(p[i]) : r.a[i];
+    hi[i] = 4 + i < n ? __float_as_uint(p[4 + i]) : r.b[i];
+  }
+  st16<NT>(reinterpret_cast<u32x4v_t*>(y), lo);
+  st16<NT>(reinterpret_cast<u32x4v_t*>(y + 4), hi);
+}
+
 // A block's place: n threads hold the vectors (8 columns) of a head, `per` heads are held
 // at once, of `tps` tokens; a block has `tokens` tokens.
 struct RopeTile {
@@ -112,8 +133,10 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     for (int g = 0; g < a.heads; g += r.tps > 1 ? a.heads : r.per, ++step) {
       const bool in = live && g + h0 < a.heads;
       const long at = (long)(t0 + t) * a.ld + (long)(g + h0) * a.D + 8 * c;
-      float u[8] = {}, p[8];
-      if (in) load8(static_cast<const T*>(a.x) + at, u);
+      float u[8], p[8];
+      decltype(raw8_load(static_cast<const T*>(nullptr))) x = {};
+      if (in) x = raw8_load(static_cast<const T*>(a.x) + at);
+      raw8_f32(x, u);
       if constexpr (HALF) {
         float* s = stage[step & 1];
 #pragma unroll
@@ -125,7 +148,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[i] = u[i] * cs[i].x + u[i ^ 1] * cs[i].y;
       }
-      if (in) store8_t<NT>(static_cast<T*>(a.y) + at, p);
+      if (in) store_turned<NT>(static_cast<T*>(a.y) + at, p, x, a.rot - 8 * c);
     }
   }
 }

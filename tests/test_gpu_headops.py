@@ -99,6 +99,44 @@ def test_rope(T, M, heads, hd, rot, layout, dtype, scaling, positions, back):
     assert torch.equal(z[:, :n], y[:, :n]) and torch.equal(z[:, n:], x[:, n:])
 
 
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("T,heads,hd,rot", [
+    (9, 3, 128, 64), (33, 4, 64, 50), (1100, 2, 64, 2), (5, 2, 8, 6), (70, 11, 240, 238)])
+def test_rope_copies_the_other_columns(T, heads, hd, rot, layout, dtype, back):
+    """Columns past rot_dim bit for bit, infinities, NaN and -0 among them, which reach no
+    turned column either; out of place and in place."""
+    need_gpu()
+    M = heads * hd + 8
+    x = normal(T + rot, T, M, dtype=dtype)
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    # inf, -inf, quiet and signalling NaN, -0, 0, the smallest denormal, 1.5
+    odd = [0x7F80, 0xFF80, 0x7FC1, 0x7F81, 0x8000, 0, 1, 0x3FC0]
+    if dtype == "f32":
+        odd = [v << 16 if v != 1 else 1 for v in odd]
+    np_bits = np.array(odd, np.uint16 if dtype == "bf16" else np.uint32)
+    odd = torch.from_numpy(np_bits.view(np.int16 if dtype == "bf16" else np.int32)).to(dev())
+    col = torch.arange(M, device=dev())
+    other = (col < heads * hd) & (col % hd >= rot)
+    i = torch.arange(T, device=dev())[:, None] * 3 + col[None, :]
+    z = x.clone()
+    z.view(bits)[:, other] = odd[i % 8][:, other]
+    s = L.make_shape(T, M, 8, 1, 1, 0, DT[dtype])
+    r = L.make_rope_shape(heads, hd, rot, 50, layout=layout, mscale=1.25)
+    call = L.flowmoe_rope_bwd if back else L.flowmoe_rope_fwd
+    want, got = x.clone(), torch.full_like(z, 7.0)
+    call(s, r, x, None, want)
+    call(s, r, z, None, got)
+    kept = z.clone()
+    call(s, r, z, None, z)  # in place
+    torch.cuda.synchronize()
+    turned = (col < heads * hd) & ~other
+    for y in (got, z):
+        assert torch.equal(y.view(bits)[:, other], kept.view(bits)[:, other])
+        assert torch.equal(y[:, turned], want[:, turned])
+
+
 def test_rope_forward_then_backward_is_the_identity():
     need_gpu()
     x = normal(3, 300, 512, dtype="f32")

@@ -466,7 +466,8 @@ typedef struct {
   double factor;    /* LINEAR, BASE, BANDS: >= 1 */
   double orig_len;  /* BANDS: the context trained on, in tokens (> 0) */
   double low, high; /* BANDS: low < high turns */
-  double mscale;    /* of cosine and sine, so of every turned element (1: a rotation) */
+  double mscale;    /* of cosine and sine, so of every turned element (1: a rotation): 0 or
+                       a finite normal float */
 } flowmoe_rope_shape_t;
 
 /* y = x turned: for the pair (u, v) at angle phi,

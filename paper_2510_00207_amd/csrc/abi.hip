@@ -745,7 +745,10 @@ flowmoe_status_t check_rope(const flowmoe_shape_t* s, const flowmoe_rope_shape_t
   if (r->seq_len < 1) return fail(FLOWMOE_ERR_INVALID, "seq_len = %d < 1", r->seq_len);
   if (!(r->base > 1.0) || !isfinite(r->base))
     return fail(FLOWMOE_ERR_INVALID, "base = %g must be finite and > 1", r->base);
-  if (!isfinite(r->mscale)) return fail(FLOWMOE_ERR_INVALID, "mscale is not finite");
+  // (held in float)
+  const float mscale = (float)r->mscale;
+  if (!isfinite(mscale) || (r->mscale != 0.0 && fabsf(mscale) < FLT_MIN))
+    return fail(FLOWMOE_ERR_INVALID, "mscale = %g must be 0 or a finite normal float", r->mscale);
   const bool bands = r->scaling == FLOWMOE_ROPE_BANDS;
   if (r->scaling != FLOWMOE_ROPE_NONE && (!(r->factor >= 1.0) || !isfinite(r->factor)))
     return fail(FLOWMOE_ERR_INVALID, "factor = %g must be finite and >= 1", r->factor);
@@ -774,7 +777,7 @@ flowmoe_status_t check_rope(const flowmoe_shape_t* s, const flowmoe_rope_shape_t
     o.low = r->low;
     o.high = r->high;
   }
-  o.mscale = (float)r->mscale;
+  o.mscale = mscale;
   return FLOWMOE_OK;
 }
 

@@ -78,6 +78,13 @@ def test_rope_refusals(flowmoe_lib, kw, status, text):
         refused(status, text, call)
 
 
+@pytest.mark.parametrize("mscale", [1e39, -1e39, 1e300, float("nan"), 1e-40, -1e-46, 5e-324])
+def test_rope_mscale_as_the_kernel_holds_it_refused(flowmoe_lib, mscale):
+    """Values that a float would hold as infinite, denormal or zero."""
+    for call in calls(shape(), rope(mscale=mscale)):
+        refused(L.ERR_INVALID, "mscale", call)
+
+
 @pytest.mark.parametrize("sub,status,text", [
     (L.make_norm_shape(3, 64), L.ERR_INVALID, "heads * head_dim"),
     (L.make_norm_shape(0, 64), L.ERR_INVALID, "heads * head_dim"),

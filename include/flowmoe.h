@@ -614,12 +614,12 @@ typedef struct {
 
 /* In the place of flowmoe_mha_fwd: qkv = in [W^Q | W^K | W^V], Q and K turned by
  * their positions (rope: heads = 2 * (heads + kv_heads) of head_dim / 2 columns, each
- * map's queries and keys for themselves, seq_len as diff's; null: not turned), the
- * differential attention, the head norm (norm: diff's heads and head_dim), out =
- * normed W^O. bf16 only. Rows past a sequence's length are zeros in out and in the
- * backward's d_in, and add nothing to a gradient; unlike the attention's own they have
- * to be finite in `in` and d_out, as the products of dw_qkv and dw_o multiply them by
- * zeros. */
+ * map's queries and keys for themselves, seq_len as diff's, at most the tokens of
+ * flowmoe_rope_fwd; null: not turned), the differential attention, the head norm (norm:
+ * diff's heads and head_dim), out = normed W^O. bf16 only. Rows past a sequence's length
+ * are zeros in out and in the backward's d_in, and add nothing to a gradient; unlike the
+ * attention's own they have to be finite in `in` and d_out, as the products of dw_qkv and
+ * dw_o multiply them by zeros. */
 flowmoe_status_t flowmoe_diff_mha_fwd(const flowmoe_shape_t* shape,
                                       const flowmoe_diff_shape_t* diff,
                                       const flowmoe_rope_shape_t* rope,

@@ -434,6 +434,7 @@ struct RopeShape {
   double inv_factor, orig, low, high;  // bands
   float mscale;
 };
+bool rope_fits(const RopeShape& m, int T);  // a grid holds the call's blocks
 hipError_t launch_rope(const RopeShape& m, int dtype, int T, long ld, bool back, const void* x,
                        const int32_t* pos, void* y, hipStream_t st);
 // RMS norm of each of a row's heads

@@ -1366,6 +1366,7 @@ size_t diff_mha_ws_bytes(const DiffShape& m, const NormShape& n, int T) {
 hipError_t launch_diff_mha_fwd(const DiffShape& m, const RopeShape* r, const NormShape& n, int T,
                                const flowmoe_diff_mha_bufs_t& b, hipStream_t st) {
   if (T == 0) return hipSuccess;
+  if (r != nullptr && !rope_fits(*r, T)) return hipErrorInvalidConfiguration;  // (before any launch)
   const int M = m.heads * m.D, W = M + 2 * m.kv * m.D;
   hipError_t e = launch_dense_gemm(FLOWMOE_K_ATTN_QKV, T, b.in, M, M, b.w_qkv, W, false, W, b.qkv, W, st);
   if (e == hipSuccess && r != nullptr)
@@ -1379,6 +1380,7 @@ hipError_t launch_diff_mha_fwd(const DiffShape& m, const RopeShape* r, const Nor
 
 hipError_t launch_diff_mha_bwd(const DiffShape& m, const RopeShape* r, const NormShape& n, int T,
                                const flowmoe_diff_mha_bufs_t& b, int accumulate, hipStream_t st) {
+  if (r != nullptr && !rope_fits(*r, T)) return hipErrorInvalidConfiguration;
   const int M = m.heads * m.D, W = M + 2 * m.kv * m.D;
   hipError_t e = hipSuccess;
   // the gradient of the norm's output, B[k][n] = W^O[n][k]; the norm's backward in its place

@@ -311,11 +311,15 @@ int norm_bwd_blocks(long rows, int D) {
 
 }  // namespace
 
+bool rope_fits(const RopeShape& m, int T) {
+  const int tokens = rope_tile(m.D, m.heads, T).tokens;
+  return (T + (long)tokens - 1) / tokens <= kMaxBlocks;
+}
+
 hipError_t launch_rope(const RopeShape& m, int dtype, int T, long ld, bool back, const void* x,
                        const int32_t* pos, void* y, hipStream_t st) {
   if (T == 0) return hipSuccess;
-  const int tokens = rope_tile(m.D, m.heads, T).tokens;
-  if ((T + (long)tokens - 1) / tokens > kMaxBlocks) return hipErrorInvalidConfiguration;
+  if (!rope_fits(m, T)) return hipErrorInvalidConfiguration;
   RopeArgs a = {};
   a.x = x;
   a.y = y;

@@ -231,3 +231,14 @@ def test_more_tokens_than_a_grid_holds_refused(flowmoe_lib):
         L.flowmoe_rope_fwd(shape(T=1 << 26, M=2048), L.make_rope_shape(32, 64, 64, 16), FAKE, None, FAKE,
                            stream=0)
     assert ei.value.status == L.ERR_HIP and "invalid configuration" in str(ei.value)
+
+
+def test_block_of_more_tokens_than_positions_reach_refused(flowmoe_lib):
+    """Where the positions' grid would be cut off the block enqueues nothing, its first
+    products neither."""
+    T = 1 << 26
+    s, d, n = shape(T=T, M=256), L.make_diff_shape(4096, 2, 2, 128, True), L.make_norm_shape(2, 128)
+    r = L.make_rope_shape(8, 64, 64, 4096)
+    for call in (lambda: L.flowmoe_diff_mha_fwd(s, d, r, n, mha_bufs(), stream=0),
+                 lambda: L.flowmoe_diff_mha_bwd(s, d, r, n, mha_bufs(), 0, stream=0)):
+        refused(L.ERR_HIP, "invalid configuration", call)

@@ -22,6 +22,19 @@
 //   dQ_i = dS_i K_i / sqrt(d), dK_i = dS_i^T Q_i / sqrt(d),
 //   dV = (P_1 - lambda P_2)^T dA (one product), dlambda_h = -sum of d2 over the rows.
 // A key/value head's gradients are sums over the query heads of its group, in order.
+//
+// Rounded to bf16: probabilities before P_i V, and dS_i and P_1 - lambda P_2 before their
+// products, as matrix operands of one type with the bf16 tensors they multiply; sums, softmax
+// statistics and row sums are fp32. Against fp64, in the 2-norm, A is 2.2e-3 to 2.6e-3 off
+// (the output's own rounding is 1.7e-3; the maps' common part cancels in A, their errors do
+// not) and the gradients 2.3e-3. Probabilities in two bf16 parts, a product each, leave the
+// output's rounding alone (1.7e-3), for 1378 us in place of 879 (4 x 4096 tokens, 32 heads of
+// 128, causal), 38.6 of 31.1 (16 x 500, 16 heads of 64, padded). (fp16, 2^-11, would need V in
+// fp16 too, which bf16 values do not fit.) The row sum is of the unrounded ones, so that lse
+// is exact to fp32.
+//
+// Times in this file are of calls on the same inputs; new inputs each pass (nothing of them in
+// the Infinity Cache) add 1-3 %.
 #include <math.h>
 
 #include <algorithm>
@@ -145,9 +158,10 @@ __device__ __forceinline__ void diff_decode(const DiffArgs& a, int heads, bool r
 // registers), whose softmaxes and products overlap. The 32 keys' scores, their softmax
 // and their products follow each other in a wave. 4 x 4096 tokens, 32 heads of 128,
 // causal: two waves a SIMD, 64 keys at a time 1030 us; the same one tile ahead of itself
-// 973; four waves 897, 32 keys at a time 880 (936 TFLOP/s, 0.79 of what a large matrix
-// product reaches here). A timing copy without the exponentials takes 817: the matrix
-// products and their power bound it.
+// 973; four waves 897, 32 keys at a time 879 (938 TFLOP/s, 0.59 of what a large matrix
+// product reaches here). A timing copy without the exponentials takes 817. Matrix pipes and
+// LDS are busy for half of the cycles each, at a clock of 1.4-1.6 GHz: power, and the waits
+// of one for the other.
 template <int NW, int S>
 struct FwdTile {
   static constexpr int G = NW / (2 * S), QB = 32 * G;  // groups of 32 queries, queries
@@ -490,9 +504,9 @@ __device__ __forceinline__ UnitAt find_unit(int nt, int unit, F&& steps, int u, 
 //
 // 24 matrix products and 32 exponentials a lane for 32 x 32 pairs; the accumulators of dP
 // start at -d1, so that a map's factor is there without a subtraction. Every LDS read is a
-// group of products ahead of its use (991 -> 955 us at 4 x 4096 tokens, 32 heads of 128,
-// causal: 864 TFLOP/s of its 6 D flops a pair). The clock falls to 1.85 GHz with the matrix
-// pipes 45 % busy: power bounds it. Running dP and the first map's scores a tile ahead,
+// group of products ahead of its use, which takes 4 % off (935 us at 4 x 4096 tokens, 32 heads
+// of 128, causal: 882 TFLOP/s of its 6 D flops a pair). The matrix pipes are busy for 43 % of
+// the cycles, LDS for 57 %, at 1.9 GHz. Running dP and the first map's scores a tile ahead,
 // beside the elementwise work, measured 2 % slower (18 % with heads of 64).
 template <int D, bool CAUSAL, int NW, int S, int ONE>
 __device__ __forceinline__ bool diff_dq_tile(const DiffArgs& a, char* lds, const TileRows& tr,
@@ -724,7 +738,9 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
   else run(TileRows{0u, seq_end(a, sq), a.N}, ~0u);
 }
 
-// dlambda_h = -sum of d2 over all rows, by a block
+// dlambda_h = -sum of d2 over all rows, by a block (of one wave where sequences are short, so
+// that a call of very many is this sum's time: 2^20 of one token, 1 head of 64, 1.3 ms for
+// 1.2 GB)
 __device__ __forceinline__ void sum_d_lambda(const DiffArgs& a, int hd, float* part) {
   const float* d2 = a.delta + ((long)a.heads + hd) * a.T;
   float s8[8] = {};
@@ -754,8 +770,9 @@ __device__ __forceinline__ void sum_d_lambda(const DiffArgs& a, int hd, float* p
 //
 // 32 matrix products and 32 exponentials a lane for 32 x 32 pairs; both accumulators (128
 // registers at D = 128) and the K fragments leave none to read ahead of the products: with
-// read groups as in dQ 1570 us, the plain order 1350 (4 x 4096 tokens, 32 heads of 128,
-// causal: 815 TFLOP/s of its 8 D flops a pair, the clock at 2.0 GHz).
+// read groups as in dQ 1570 us, the plain order 1340 (4 x 4096 tokens, 32 heads of 128,
+// causal: 820 TFLOP/s of its 8 D flops a pair; the matrix pipes busy for 38 % of the cycles,
+// LDS for 68 %, at 2.0 GHz).
 template <int D, bool CAUSAL, int NW, int S, int ONE>
 __global__ __launch_bounds__(64 * NW, ONE == 2 && D == 128 ? 1 : 2) void diff_dkdv_kernel(DiffArgs a) {
   constexpr int SL = ONE ? 1 : 2;  // slots: ONE for sequences of one tile (1) or less (2)
@@ -1198,11 +1215,12 @@ KeyTile key_tile(const DiffShape& m, const DiffArgs& a) {
 }
 
 // The unit that nt tiles of steps(tile) steps, `per` times over, are cut into: the smallest
-// (at least 2) whose blocks run in one round of `slots`; 0 (uncut): no such unit, or the
-// longest tile is less than the worth of the join longer (about 16 / S steps). A round that
-// is not full costs as much as a full one: the whole backward of 2 x 2031 tokens, 16 heads
-// on 4 of 128, causal, 512 slots: uncut 457 us; units of 34, 37, 40, 44, 51 steps (576,
-// 536, 488, 456, 408 blocks) 221, 203, 184, 188, 197; of 20 (920 blocks, two rounds) 198.
+// (at least 2) whose blocks run in one round of `slots` (dlambda's, a head each and last in
+// the grid of dK and dV, are not counted and may wait for one that ends); 0 (uncut): no such
+// unit, or the longest tile is less than the worth of the join longer (about 16 / S steps). A
+// round that is not full costs as much as a full one: the whole backward of 2 x 2031 tokens,
+// 16 heads on 4 of 128, causal, 512 slots: uncut 457 us; units of 34, 37, 40, 44, 51 steps
+// (576, 536, 488, 456, 408 blocks) 221, 203, 184, 188, 197; of 20 (920 blocks, two rounds) 198.
 template <class F>
 int cut(int nt, long per, long slots, int S, F&& steps, int& units) {
   units = 0;

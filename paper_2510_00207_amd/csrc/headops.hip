@@ -10,9 +10,9 @@ namespace {
 
 // Non-temporal stores, for calls that move at least 256 MB: their lines would evict, from
 // the Infinity Cache, input that is still to be read. us, cached and non-temporal, with new
-// inputs each pass: 537 MB of rotary positions 110, 108; 402 MB of the norm's backward 81,
-// 80; 268 MB of its forward 51, 49; 50 MB of positions 10.3, 11.3. (A copy of 1 GB reaches
-// 5.05 TB/s here, which is 106, 80 and 53 us for the three large ones.)
+// inputs each pass: 537 MB of rotary positions 110, 107; 403 MB of the norm's backward 77.2,
+// 75.8; 268 MB of its forward 50.3, 48.8; 50 MB of positions 10.5, 11.4. (Copies of the large
+// ones' bytes, new buffers each pass, take 99, 74 and 51 us, 5.2-5.4 TB/s.)
 bool stream_past_caches(long bytes) { return bytes >= (256L << 20); }
 
 // ---------------------------------------------------------------------------
@@ -87,9 +87,9 @@ __host__ __device__ __forceinline__ RopeTile rope_tile(int D, int heads, int T) 
 // partner is its neighbour; with halves (HALF) it is half a rotation away, anywhere in
 // another thread's vector, and taken from LDS: element i of thread k lies at i * 256 + k
 // there, and the cosines likewise, so that a wave's reads, which all have one distance,
-// touch every bank once. 16384 tokens of 64 heads of 128, bf16: 537 MB in 108 us, 5.0 TB/s,
-// which is what a large copy reaches; with 122 columns turned the same (409 us with
-// 16-byte accesses to either half where it starts, a thread both).
+// touch every bank once. 16384 tokens of 64 heads of 128, bf16: 537 MB in 107 us, 5.0 TB/s
+// (a copy 5.4); with 122 columns turned the same (409 us with 16-byte accesses to either
+// half where it starts, a thread both).
 template <typename T, bool HALF, bool NT>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   extern __shared__ float2 table[];  // tokens x 8 x (pairs / 8, rounded up)
@@ -191,8 +191,8 @@ __device__ __forceinline__ float group_sum(float v) {
 }
 
 // L lanes (a power of two) hold a head's D <= 8 L elements, 8 each; a block's groups walk
-// the rows. 16384 tokens of 32 heads of 128, bf16: 268 MB in 49 us, 5.5 TB/s, the rate of a
-// large copy.
+// the rows. 16384 tokens of 32 heads of 128, bf16: 268 MB in 49 us, 5.5 TB/s (a copy of as
+// many bytes 51 us).
 template <typename T, int L, bool NT>
 __global__ __launch_bounds__(256) void head_norm_kernel(NormArgs a) {
   const int c = 8 * (threadIdx.x % L);
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256) void head_norm_kernel(NormArgs a) {
 }
 
 // dx = r (u - x r^2 mean(u x)), u = scale gain dy; dgain's sums over the block's rows go
-// to `part`, in a fixed order. As above 402 MB in 76 us, 5.3 TB/s, with the join's 5 us; 512,
+// to `part`, in a fixed order. As above 403 MB in 76 us, 5.3 TB/s, with the join's 5 us; 512,
 // 1024 and 2048 blocks (with an older join of 7) 111, 82 and 91.
 template <typename T, int L, bool NT>
 __global__ __launch_bounds__(256) void head_norm_bwd_kernel(NormArgs a) {

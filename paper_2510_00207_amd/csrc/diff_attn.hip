@@ -30,11 +30,11 @@
 // not) and the gradients 2.3e-3. Probabilities in two bf16 parts, a product each, leave the
 // output's rounding alone (1.7e-3), for 1378 us in place of 879 (4 x 4096 tokens, 32 heads of
 // 128, causal), 38.6 of 31.1 (16 x 500, 16 heads of 64, padded). (fp16, 2^-11, would need V in
-// fp16 too, which bf16 values do not fit.) The row sum is of the unrounded ones, so that lse
+// fp16 too, whose range bf16 values exceed.) The row sum is of the unrounded ones, so that lse
 // is exact to fp32.
 //
-// Times in this file are of calls on the same inputs; new inputs each pass (nothing of them in
-// the Infinity Cache) add 1-3 %.
+// Times in this file are of calls on the same inputs; new inputs each pass add 1-3 % to long
+// ones.
 #include <math.h>
 
 #include <algorithm>
@@ -504,7 +504,7 @@ __device__ __forceinline__ UnitAt find_unit(int nt, int unit, F&& steps, int u, 
 //
 // 24 matrix products and 32 exponentials a lane for 32 x 32 pairs; the accumulators of dP
 // start at -d1, so that a map's factor is there without a subtraction. Every LDS read is a
-// group of products ahead of its use, which takes 4 % off (935 us at 4 x 4096 tokens, 32 heads
+// group of products ahead of its use, which takes 4 % off (935 us of a kernel trace at 4 x 4096 tokens, 32 heads
 // of 128, causal: 882 TFLOP/s of its 6 D flops a pair). The matrix pipes are busy for 43 % of
 // the cycles, LDS for 57 %, at 1.9 GHz. Running dP and the first map's scores a tile ahead,
 // beside the elementwise work, measured 2 % slower (18 % with heads of 64).
@@ -738,9 +738,9 @@ __global__ __launch_bounds__(64 * NW, 2) void diff_dq_kernel(DiffArgs a) {
   else run(TileRows{0u, seq_end(a, sq), a.N}, ~0u);
 }
 
-// dlambda_h = -sum of d2 over all rows, by a block (of one wave where sequences are short, so
-// that a call of very many is this sum's time: 2^20 of one token, 1 head of 64, 1.3 ms for
-// 1.2 GB)
+// dlambda_h = -sum of d2 over all rows, by a block, of one wave where sequences are short: of
+// very many this sum outlasts the other blocks (2^20 of one token, 1 head of 64: dQ 230 us, dK
+// and dV with the sum 1098; 16384, 8 heads: 29 and 35)
 __device__ __forceinline__ void sum_d_lambda(const DiffArgs& a, int hd, float* part) {
   const float* d2 = a.delta + ((long)a.heads + hd) * a.T;
   float s8[8] = {};

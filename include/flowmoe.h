@@ -310,7 +310,16 @@ enum {
   FLOWMOE_K_DIFF_BWD_DKDV = 28,   /* differential attention backward: dK, dV */
   FLOWMOE_K_DIFF_JOIN = 29,       /* differential attention backward: sums of partial results */
   FLOWMOE_K_HEAD_NORM = 30,       /* head norm */
-  FLOWMOE_K_HEAD_NORM_BWD = 31    /* head norm backward */
+  FLOWMOE_K_HEAD_NORM_BWD = 31,   /* head norm backward */
+  /* past the 32 bits of flowmoe_trace_start's mask: flowmoe_trace_start64 */
+  FLOWMOE_K_LAYER_NORM = 32,      /* layer norm */
+  FLOWMOE_K_LAYER_NORM_BWD = 33,  /* layer norm backward */
+  FLOWMOE_K_EMBED = 34,           /* embedding lookup */
+  FLOWMOE_K_EMBED_SORT = 35,      /* embedding gradient: the tokens by id */
+  FLOWMOE_K_EMBED_BWD = 36,       /* embedding gradient: sums of the tokens' rows */
+  FLOWMOE_K_PACKED_JOIN = 37      /* attention over packed sequences, backward: sums of
+                                     partial dK, dV (its other kernels are of the kinds
+                                     FLOWMOE_K_ATTN_FWD, _BWD_DQ and _BWD_DKDV) */
 };
 
 /* Start tracing on the calling host thread: every later kernel launch whose
@@ -321,6 +330,10 @@ enum {
  * only records events; it changes no result. */
 flowmoe_status_t flowmoe_trace_start(hipEvent_t* events, int32_t* kinds, int32_t pairs,
                                      uint32_t mask);
+
+/* The same with a mask that has a bit for every kind. */
+flowmoe_status_t flowmoe_trace_start64(hipEvent_t* events, int32_t* kinds, int32_t pairs,
+                                       uint64_t mask);
 
 /* Stop tracing; returns the number of pairs recorded since the start. */
 int32_t flowmoe_trace_stop(void);
@@ -640,6 +653,168 @@ flowmoe_status_t flowmoe_diff_mha_bwd(const flowmoe_shape_t* shape,
                                       const flowmoe_norm_shape_t* norm,
                                       const flowmoe_diff_mha_bufs_t* bufs, int32_t accumulate,
                                       hipStream_t stream);
+
+/* ---- attention over packed sequences ------------------------------------------ */
+
+/* In the place of flowmoe_attention_*, for documents of any lengths side by side and
+ * query heads that share key/value heads. shape->M = heads * head_dim; qkv rows hold
+ * W = M + 2 * kv_heads * head_dim elements, [Q | K | V], and query head h reads key head
+ * h / (heads / kv_heads). bf16 only; 16-byte aligned; only shape->T, M (at most 2^21) and
+ * dtype are used. */
+typedef struct {
+  int32_t nseq;     /* sequences, >= 0 */
+  int32_t heads;
+  int32_t kv_heads; /* divides heads */
+  int32_t head_dim; /* 64 or 128 (else FLOWMOE_ERR_UNSUPPORTED) */
+  int32_t causal;   /* 1: token i attends to tokens j <= i of its sequence;
+                       0: to every token of its sequence */
+} flowmoe_packed_shape_t;
+
+/* Attention within each sequence, A_h = softmax(Q_h K_h^T / sqrt(head_dim)) V_h.
+ *   qkv    T x W (in)
+ *   starts nseq + 1 int32 (in; nullable with nseq 0): sequence i is rows starts[i] ..
+ *          starts[i + 1] - 1. Ascending from 0 to at most T (device data, so not checked on
+ *          the host: starts[0] is taken as 0, the others are cut to 0 .. T; of a list
+ *          that descends the results are unspecified, within the buffers). Equal
+ *          neighbours are a sequence without tokens. Rows from starts[nseq] on are of no
+ *          sequence: they may hold anything, NaN as well, and their rows of every output
+ *          are zeros. No row of a sequence is affected by another's, finite or not.
+ *   attn   T x M (out)
+ *   lse    heads x T float (out): the natural log of each row's softmax denominator, as
+ *          flowmoe_attention_fwd
+ * Probabilities are rounded to bf16 before they multiply V; sums in float. */
+flowmoe_status_t flowmoe_packed_attention_fwd(const flowmoe_shape_t* shape,
+                                              const flowmoe_packed_shape_t* packed,
+                                              const void* qkv, const int32_t* starts, void* attn,
+                                              float* lse, hipStream_t stream);
+
+/* Bytes of scratch flowmoe_packed_attention_bwd needs (0 for an invalid shape). */
+size_t flowmoe_packed_attention_ws_bytes(const flowmoe_shape_t* shape,
+                                         const flowmoe_packed_shape_t* packed);
+
+/* Its gradient, from d_attn (T x M) and the forward's inputs, attn and lse:
+ *   d_qkv T x W (out); shared key/value heads get the sum over their group
+ *   delta heads x T float (out): rowsum(d_attn_h * attn_h), an intermediate (written, then
+ *         read)
+ *   ws    flowmoe_packed_attention_ws_bytes bytes (nullable when that is 0) */
+flowmoe_status_t flowmoe_packed_attention_bwd(const flowmoe_shape_t* shape,
+                                              const flowmoe_packed_shape_t* packed,
+                                              const void* qkv, const int32_t* starts,
+                                              const void* attn, const float* lse,
+                                              const void* d_attn, void* d_qkv, float* delta,
+                                              void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Buffers of flowmoe_packed_mha_fwd / _bwd, W = M + 2 * kv_heads * head_dim. */
+typedef struct {
+  /* parameters and inputs */
+  const void* in;           /* T x M: the block input */
+  const void* w_qkv;        /* M x W: [W^Q | W^K | W^V] side by side */
+  const void* w_o;          /* M x M */
+  const int32_t* positions; /* T: each token's position in its sequence; with rope */
+  const int32_t* starts;    /* nseq + 1 (flowmoe_packed_attention_fwd) */
+  /* forward (all but out kept for the backward) */
+  void* qkv;                /* T x W: Q and K turned */
+  void* attn;               /* T x M */
+  float* lse;               /* heads x T */
+  void* out;                /* T x M */
+  /* backward */
+  const void* d_out;        /* T x M */
+  void* d_attn;             /* T x M */
+  void* d_qkv;              /* T x W */
+  float* delta;             /* heads x T */
+  void* d_in;               /* T x M */
+  float* dw_qkv;            /* M x W */
+  float* dw_o;              /* M x M */
+  /* scratch of the backward: flowmoe_packed_mha_ws_bytes bytes */
+  void* ws;
+  size_t ws_bytes;
+} flowmoe_packed_mha_bufs_t;
+
+/* In the place of flowmoe_mha_fwd: qkv = in [W^Q | W^K | W^V], Q and K turned by their
+ * positions (rope: heads = packed's heads + kv_heads of head_dim columns, at most the
+ * tokens of flowmoe_rope_fwd; its seq_len is not used; null: not turned), the attention over
+ * the packed sequences, out = attn W^O. bf16 only. Rows of no sequence are zeros in out
+ * and in the backward's d_in, and add nothing to a gradient; unlike the attention's own they
+ * have to be finite in `in` and d_out, as the products of dw_qkv and dw_o multiply them by
+ * zeros. */
+flowmoe_status_t flowmoe_packed_mha_fwd(const flowmoe_shape_t* shape,
+                                        const flowmoe_packed_shape_t* packed,
+                                        const flowmoe_rope_shape_t* rope,
+                                        const flowmoe_packed_mha_bufs_t* bufs, hipStream_t stream);
+
+/* Bytes of scratch flowmoe_packed_mha_bwd needs (0 for an invalid shape). */
+size_t flowmoe_packed_mha_ws_bytes(const flowmoe_shape_t* shape,
+                                   const flowmoe_packed_shape_t* packed);
+
+/* Its backward: d_attn = d_out W^O^T, the attention backward (d_qkv, delta), Q's and K's
+ * columns of d_qkv turned back, d_in = d_qkv [W^Q | W^K | W^V]^T, dw_o = attn^T d_out,
+ * dw_qkv = in^T d_qkv; with accumulate != 0, dw_qkv and dw_o are added to, else
+ * overwritten. */
+flowmoe_status_t flowmoe_packed_mha_bwd(const flowmoe_shape_t* shape,
+                                        const flowmoe_packed_shape_t* packed,
+                                        const flowmoe_rope_shape_t* rope,
+                                        const flowmoe_packed_mha_bufs_t* bufs, int32_t accumulate,
+                                        hipStream_t stream);
+
+/* ---- layer norm ----------------------------------------------------------------- */
+
+/* Layer norm of T rows of M (M at most 16384, else FLOWMOE_ERR_UNSUPPORTED), with the
+ * residual's addition: h = x (+ res), y = (h - mean(h)) / sqrt(var(h) + eps) * gain + bias,
+ * mean and variance (over M) in float. y is of the unrounded h.
+ *   x     T x M layer dtype; only shape->T, M and dtype are used
+ *   eps   > 0, a normal float
+ *   res   T x M (in, nullable: none)
+ *   gain, bias  M float, each nullable (ones, zeros)
+ *   sum   T x M (out, nullable): h in the layer dtype, which the backward reads as its x
+ *   y     T x M (out)
+ * y and sum may each be x or res (in place), but not each other. */
+flowmoe_status_t flowmoe_layer_norm_fwd(const flowmoe_shape_t* shape, float eps, const void* x,
+                                        const void* res, const float* gain, const float* bias,
+                                        void* sum, void* y, hipStream_t stream);
+
+/* Bytes of scratch flowmoe_layer_norm_bwd needs (0 for an invalid shape). */
+size_t flowmoe_layer_norm_ws_bytes(const flowmoe_shape_t* shape);
+
+/* Its gradients, from x as the norm read it (with a residual: the forward's sum):
+ *   dy    T x M (in)
+ *   d_sum T x M (in, nullable): what else h's gradient holds (of the residual stream past
+ *         the norm), added to dx before it is rounded
+ *   dx    T x M (out): the gradient of h, so of x and of res alike; may be x, dy or d_sum
+ *   dgain, dbias  M float (out, each nullable: not computed), summed over the rows; with
+ *         accumulate != 0 added to
+ *   ws    flowmoe_layer_norm_ws_bytes bytes, nullable without dgain and dbias */
+flowmoe_status_t flowmoe_layer_norm_bwd(const flowmoe_shape_t* shape, float eps, const void* x,
+                                        const float* gain, const void* dy, const void* d_sum,
+                                        void* dx, float* dgain, float* dbias, int32_t accumulate,
+                                        void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---- embedding -------------------------------------------------------------------- */
+
+typedef struct {
+  int32_t vocab; /* rows of the table, >= 1 */
+  float scale;   /* a constant factor (1, or sqrt(M)), finite */
+} flowmoe_embed_shape_t;
+
+/* Embedding lookup: y[t] = scale * table[ids[t]], zeros for an id outside [0, vocab).
+ *   ids   T int32;  table vocab x M, y T x M layer dtype
+ * Only shape->T, M and dtype are used. */
+flowmoe_status_t flowmoe_embed_fwd(const flowmoe_shape_t* shape, const flowmoe_embed_shape_t* embed,
+                                   const int32_t* ids, const void* table, void* y,
+                                   hipStream_t stream);
+
+/* Bytes of scratch flowmoe_embed_bwd needs (0 for an invalid shape). */
+size_t flowmoe_embed_ws_bytes(const flowmoe_shape_t* shape, const flowmoe_embed_shape_t* embed);
+
+/* Its gradient: dtable[v] = scale * the sum of dy[t] over the tokens with ids[t] = v, in an
+ * order that the ids alone decide.
+ *   dy     T x M layer dtype
+ *   dtable vocab x M float (out), 16-byte aligned: every row written (zeros without tokens);
+ *          with accumulate != 0 the rows that have tokens are added to, the others not touched
+ *   ws     flowmoe_embed_ws_bytes bytes, 16-byte aligned (nullable when that is 0) */
+flowmoe_status_t flowmoe_embed_bwd(const flowmoe_shape_t* shape, const flowmoe_embed_shape_t* embed,
+                                   const int32_t* ids, const void* dy, float* dtable,
+                                   int32_t accumulate, void* ws, size_t ws_bytes,
+                                   hipStream_t stream);
 
 /* ---- the R-chunk two-stream layer (Sec. 3.2, Eqs. 3-6) -------------------- */
 

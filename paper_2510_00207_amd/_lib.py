@@ -58,6 +58,15 @@ class DiffShape(ctypes.Structure):
                 for n in ("seq_len", "heads", "kv_heads", "head_dim", "causal")]
 
 
+class PackedShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32)
+                for n in ("nseq", "heads", "kv_heads", "head_dim", "causal")]
+
+
+class EmbedShape(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 _VP = ctypes.c_void_p
 _LAYER_FIELDS = [
     "w_gate", "bias", "w1", "w3", "w2", "b1", "b3", "b2",
@@ -85,6 +94,16 @@ class DiffMhaBufs(ctypes.Structure):
     _fields_ = [(n, _VP) for n in _DIFF_MHA_FIELDS] + [("ws_bytes", ctypes.c_size_t)]
 
 
+_PACKED_MHA_FIELDS = [
+    "in", "w_qkv", "w_o", "positions", "starts", "qkv", "attn", "lse", "out",
+    "d_out", "d_attn", "d_qkv", "delta", "d_in", "dw_qkv", "dw_o", "ws",
+]
+
+
+class PackedMhaBufs(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in _PACKED_MHA_FIELDS] + [("ws_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -106,6 +125,8 @@ def load():
     MP = ctypes.POINTER(MhaShape)
     RP, NP, DP = (ctypes.POINTER(c) for c in (RopeShape, NormShape, DiffShape))
     BP = ctypes.POINTER(DiffMhaBufs)
+    KP, EP, KBP = (ctypes.POINTER(c) for c in (PackedShape, EmbedShape, PackedMhaBufs))
+    F = ctypes.c_float
     sig = {
         "flowmoe_version": ([], ctypes.c_char_p),
         "flowmoe_last_error": ([], ctypes.c_char_p),
@@ -124,6 +145,7 @@ def load():
         "flowmoe_gate_topk_bwd": ([SP, P, P, P, P, P, P, P, P, P, P, I32, P, SZ, P], I32),
         "flowmoe_gate_topk_bwd_noalloc": ([SP, P, P, P, P, P, P, P, P, P, P, I32, P], I32),
         "flowmoe_trace_start": ([P, P, I32, ctypes.c_uint32], I32),
+        "flowmoe_trace_start64": ([P, P, I32, ctypes.c_uint64], I32),
         "flowmoe_trace_stop": ([], I32),
         "flowmoe_set_gemm_tiles": ([I32], I32),
         "flowmoe_set_row_streams": ([I32], I32),
@@ -143,6 +165,18 @@ def load():
         "flowmoe_diff_mha_fwd": ([SP, DP, RP, NP, BP, P], I32),
         "flowmoe_diff_mha_ws_bytes": ([SP, DP, NP], SZ),
         "flowmoe_diff_mha_bwd": ([SP, DP, RP, NP, BP, I32, P], I32),
+        "flowmoe_packed_attention_fwd": ([SP, KP] + [P] * 5, I32),
+        "flowmoe_packed_attention_ws_bytes": ([SP, KP], SZ),
+        "flowmoe_packed_attention_bwd": ([SP, KP] + [P] * 8 + [SZ, P], I32),
+        "flowmoe_packed_mha_fwd": ([SP, KP, RP, KBP, P], I32),
+        "flowmoe_packed_mha_ws_bytes": ([SP, KP], SZ),
+        "flowmoe_packed_mha_bwd": ([SP, KP, RP, KBP, I32, P], I32),
+        "flowmoe_layer_norm_fwd": ([SP, F] + [P] * 7, I32),
+        "flowmoe_layer_norm_ws_bytes": ([SP], SZ),
+        "flowmoe_layer_norm_bwd": ([SP, F] + [P] * 7 + [I32, P, SZ, P], I32),
+        "flowmoe_embed_fwd": ([SP, EP] + [P] * 4, I32),
+        "flowmoe_embed_ws_bytes": ([SP, EP], SZ),
+        "flowmoe_embed_bwd": ([SP, EP] + [P] * 3 + [I32, P, SZ, P], I32),
         "flowmoe_layer_fwd": ([SP, I32, ctypes.POINTER(LayerBufs), P, P, P], I32),
         "flowmoe_layer_bwd": ([SP, I32, ctypes.POINTER(LayerBufs), P, P, P], I32),
     }
@@ -410,12 +444,101 @@ def flowmoe_diff_mha_bwd(shape, diff, rope, norm, bufs, accumulate, stream=None)
                                        _stream(stream)))
 
 
+# ---- attention over packed sequences, layer norm, embedding ----------------------------
+def make_packed_shape(nseq, heads, kv_heads, head_dim, causal) -> PackedShape:
+    return PackedShape(nseq, heads, kv_heads, head_dim, int(bool(causal)))
+
+
+def flowmoe_packed_attention_fwd(shape, packed, qkv, starts, attn, lse, stream=None):
+    _check(load().flowmoe_packed_attention_fwd(ctypes.byref(shape), ctypes.byref(packed), ptr(qkv),
+                                               ptr(starts), ptr(attn), ptr(lse), _stream(stream)))
+
+
+def flowmoe_packed_attention_ws_bytes(shape, packed) -> int:
+    return load().flowmoe_packed_attention_ws_bytes(ctypes.byref(shape), ctypes.byref(packed))
+
+
+def flowmoe_packed_attention_bwd(shape, packed, qkv, starts, attn, lse, d_attn, d_qkv, delta,
+                                 ws=None, ws_bytes=0, stream=None):
+    _check(load().flowmoe_packed_attention_bwd(ctypes.byref(shape), ctypes.byref(packed), ptr(qkv),
+                                               ptr(starts), ptr(attn), ptr(lse), ptr(d_attn),
+                                               ptr(d_qkv), ptr(delta), ptr(ws), int(ws_bytes),
+                                               _stream(stream)))
+
+
+def packed_mha_bufs(**tensors) -> PackedMhaBufs:
+    """PackedMhaBufs from keyword tensors (names of the C struct fields; ``in`` as ``inp``)."""
+    b = PackedMhaBufs()
+    for name, t in tensors.items():
+        name = "in" if name == "inp" else name
+        if name == "ws_bytes":
+            b.ws_bytes = int(t)
+        elif name not in _PACKED_MHA_FIELDS:
+            raise KeyError(name)
+        else:
+            setattr(b, name, ptr(t))
+    return b
+
+
+def flowmoe_packed_mha_fwd(shape, packed, rope, bufs, stream=None):
+    _check(load().flowmoe_packed_mha_fwd(ctypes.byref(shape), ctypes.byref(packed),
+                                         None if rope is None else ctypes.byref(rope),
+                                         ctypes.byref(bufs), _stream(stream)))
+
+
+def flowmoe_packed_mha_ws_bytes(shape, packed) -> int:
+    return load().flowmoe_packed_mha_ws_bytes(ctypes.byref(shape), ctypes.byref(packed))
+
+
+def flowmoe_packed_mha_bwd(shape, packed, rope, bufs, accumulate, stream=None):
+    _check(load().flowmoe_packed_mha_bwd(ctypes.byref(shape), ctypes.byref(packed),
+                                         None if rope is None else ctypes.byref(rope),
+                                         ctypes.byref(bufs), int(accumulate), _stream(stream)))
+
+
+def flowmoe_layer_norm_fwd(shape, eps, x, res, gain, bias, sum_, y, stream=None):
+    _check(load().flowmoe_layer_norm_fwd(ctypes.byref(shape), eps, ptr(x), ptr(res), ptr(gain),
+                                         ptr(bias), ptr(sum_), ptr(y), _stream(stream)))
+
+
+def flowmoe_layer_norm_ws_bytes(shape) -> int:
+    return load().flowmoe_layer_norm_ws_bytes(ctypes.byref(shape))
+
+
+def flowmoe_layer_norm_bwd(shape, eps, x, gain, dy, d_sum, dx, dgain, dbias, accumulate, ws=None,
+                           ws_bytes=0, stream=None):
+    _check(load().flowmoe_layer_norm_bwd(ctypes.byref(shape), eps, ptr(x), ptr(gain), ptr(dy),
+                                         ptr(d_sum), ptr(dx), ptr(dgain), ptr(dbias),
+                                         int(accumulate), ptr(ws), int(ws_bytes),
+                                         _stream(stream)))
+
+
+def make_embed_shape(vocab, scale=1.0) -> EmbedShape:
+    return EmbedShape(vocab, scale)
+
+
+def flowmoe_embed_fwd(shape, embed, ids, table, y, stream=None):
+    _check(load().flowmoe_embed_fwd(ctypes.byref(shape), ctypes.byref(embed), ptr(ids), ptr(table),
+                                    ptr(y), _stream(stream)))
+
+
+def flowmoe_embed_ws_bytes(shape, embed) -> int:
+    return load().flowmoe_embed_ws_bytes(ctypes.byref(shape), ctypes.byref(embed))
+
+
+def flowmoe_embed_bwd(shape, embed, ids, dy, dtable, accumulate, ws=None, ws_bytes=0, stream=None):
+    _check(load().flowmoe_embed_bwd(ctypes.byref(shape), ctypes.byref(embed), ptr(ids), ptr(dy),
+                                    ptr(dtable), int(accumulate), ptr(ws), int(ws_bytes),
+                                    _stream(stream)))
+
+
 # ---- kernel tracing --------------------------------------------------------------
 K_NAMES = ["gate", "route", "scan", "gather", "ffn1", "ffn2", "swiglu_act", "combine",
            "combine_bwd", "dgrad1", "wgrad2", "wgrad1", "dgrad2", "gate_bwd_wt", "gate_bwd_token",
            "gate_bwd_dw", "gate_bwd_reduce", "bias_grad", "attn_qkv", "attn_fwd", "attn_out",
            "attn_dgrad", "attn_bwd_dq", "attn_bwd_dkdv", "attn_wgrad", "rope", "diff_fwd",
-           "diff_bwd_dq", "diff_bwd_dkdv", "diff_join", "head_norm", "head_norm_bwd"]
+           "diff_bwd_dq", "diff_bwd_dkdv", "diff_join", "head_norm", "head_norm_bwd",
+           "layer_norm", "layer_norm_bwd", "embed", "embed_sort", "embed_bwd", "packed_join"]
 K = {n: i for i, n in enumerate(K_NAMES)}
 K_GEMM = ("ffn1", "ffn2", "dgrad1", "wgrad2", "wgrad1", "dgrad2")
 
@@ -431,6 +554,12 @@ def flowmoe_trace_start(events, kinds, pairs: int, mask: int):
     """events: ctypes array of 2*pairs hipEvent_t; kinds: ctypes int32 array."""
     _check(load().flowmoe_trace_start(ctypes.cast(events, ctypes.c_void_p),
                                       ctypes.cast(kinds, ctypes.c_void_p), pairs, mask))
+
+
+def flowmoe_trace_start64(events, kinds, pairs: int, mask: int):
+    """flowmoe_trace_start with a mask that has a bit for every kind."""
+    _check(load().flowmoe_trace_start64(ctypes.cast(events, ctypes.c_void_p),
+                                        ctypes.cast(kinds, ctypes.c_void_p), pairs, mask))
 
 
 def flowmoe_trace_stop() -> int:

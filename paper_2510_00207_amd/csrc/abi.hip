@@ -149,7 +149,7 @@ struct TraceState {
   int32_t* kinds = nullptr;
   int32_t pairs = 0;
   int32_t used = 0;
-  uint32_t mask = 0;
+  uint64_t mask = 0;
   bool open = false;  // a begin was recorded for the current launch
 };
 thread_local TraceState g_trace;
@@ -162,7 +162,7 @@ inline char* mptr(void* p, long off) { return p == nullptr ? nullptr : static_ca
 namespace flowmoe {
 hipError_t trace_mark(int kind, bool end, hipStream_t st) {
   TraceState& t = g_trace;
-  if (t.ev == nullptr || kind < 0 || kind >= 32 || !((t.mask >> kind) & 1u)) return hipSuccess;
+  if (t.ev == nullptr || kind < 0 || kind >= 64 || !((t.mask >> kind) & 1u)) return hipSuccess;
   if (!end) {
     if (t.used >= t.pairs) return hipSuccess;
     t.open = true;
@@ -181,6 +181,11 @@ extern "C" {
 
 flowmoe_status_t flowmoe_trace_start(hipEvent_t* events, int32_t* kinds, int32_t pairs,
                                      uint32_t mask) {
+  return flowmoe_trace_start64(events, kinds, pairs, mask);
+}
+
+flowmoe_status_t flowmoe_trace_start64(hipEvent_t* events, int32_t* kinds, int32_t pairs,
+                                       uint64_t mask) {
   if (pairs < 0) return fail(FLOWMOE_ERR_INVALID, "pairs = %d < 0", pairs);
   if (pairs > 0 && (events == nullptr || kinds == nullptr))
     return fail(FLOWMOE_ERR_INVALID, "events and kinds must be given");
@@ -1080,6 +1085,288 @@ flowmoe_status_t flowmoe_diff_mha_bwd(const flowmoe_shape_t* shape,
   return hip_status(launch_diff_mha_bwd(m, rope ? &r : nullptr, n, shape->T, *b, accumulate != 0,
                                         stream),
                     "flowmoe_diff_mha_bwd");
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// attention over packed sequences, layer norm, embedding
+// ---------------------------------------------------------------------------
+namespace {
+
+flowmoe_status_t check_packed(const flowmoe_shape_t* s, const flowmoe_packed_shape_t* m,
+                              PackedShape* out) {
+  flowmoe_status_t st = check_rows(s);
+  if (st != FLOWMOE_OK) return st;
+  if (m == nullptr) return fail(FLOWMOE_ERR_INVALID, "packed is null");
+  if (s->dtype != FLOWMOE_BF16)
+    return fail(FLOWMOE_ERR_UNSUPPORTED, "the attention runs in FLOWMOE_BF16 only");
+  if (m->head_dim != 64 && m->head_dim != 128)
+    return fail(FLOWMOE_ERR_UNSUPPORTED, "head_dim = %d is not 64 or 128", m->head_dim);
+  if (m->heads < 1 || (long)m->heads * m->head_dim != s->M)
+    return fail(FLOWMOE_ERR_INVALID, "heads * head_dim = %d * %d is not M = %d", m->heads,
+                m->head_dim, s->M);
+  if (m->kv_heads < 1 || m->heads % m->kv_heads)
+    return fail(FLOWMOE_ERR_INVALID, "kv_heads = %d does not divide heads = %d", m->kv_heads,
+                m->heads);
+  if (m->nseq < 0) return fail(FLOWMOE_ERR_INVALID, "nseq = %d < 0", m->nseq);
+  if (m->causal != 0 && m->causal != 1)
+    return fail(FLOWMOE_ERR_INVALID, "causal = %d is not 0 or 1", m->causal);
+  // (a tile's rows are reached by 32-bit byte offsets; a grid holds kMaxBlocks)
+  if ((long)s->T * 3 * s->M > (1L << 40) || s->T > (1 << 30) || s->M > (1 << 21))
+    return fail(FLOWMOE_ERR_UNSUPPORTED, "tensor too large");
+  if ((s->T / 32 + (long)m->nseq + 1) * m->heads > kMaxBlocks)
+    return fail(FLOWMOE_ERR_UNSUPPORTED, "too many attention tiles");
+  *out = PackedShape{m->nseq, m->heads, m->kv_heads, m->head_dim, m->causal};
+  return FLOWMOE_OK;
+}
+
+// `starts`, nullable without sequences
+#define REQUIRE_STARTS(m, p, name)                                                              \
+  if ((m).nseq > 0 && (p) == nullptr) return fail(FLOWMOE_ERR_INVALID, "%s is null", name);     \
+  CHECK_A4(p, name)
+
+flowmoe_status_t check_packed_mha(const flowmoe_shape_t* shape,
+                                  const flowmoe_packed_shape_t* packed,
+                                  const flowmoe_rope_shape_t* rope, PackedShape* m, RopeShape* r) {
+  flowmoe_status_t st = check_packed(shape, packed, m);
+  if (st != FLOWMOE_OK || rope == nullptr) return st;
+  flowmoe_shape_t row = *shape;
+  row.M = shape->M + 2 * m->kv * m->D;
+  st = check_rope(&row, rope, r);
+  if (st != FLOWMOE_OK) return st;
+  if (r->D != m->D || r->heads != m->heads + m->kv)
+    return fail(FLOWMOE_ERR_INVALID, "rope's heads * head_dim = %d * %d are not Q's and K's (%d + %d) * %d",
+                r->heads, r->D, m->heads, m->kv, m->D);
+  return FLOWMOE_OK;
+}
+
+flowmoe_status_t check_layer_norm(const flowmoe_shape_t* s, float eps) {
+  flowmoe_status_t st = check_rows(s);
+  if (st != FLOWMOE_OK) return st;
+  if (s->M > kMaxNormM) return fail(FLOWMOE_ERR_UNSUPPORTED, "M = %d > %d", s->M, kMaxNormM);
+  if (!(eps >= FLT_MIN) || !isfinite(eps))
+    return fail(FLOWMOE_ERR_INVALID, "eps = %g must be a finite normal float > 0", eps);
+  return FLOWMOE_OK;
+}
+
+flowmoe_status_t check_embed(const flowmoe_shape_t* s, const flowmoe_embed_shape_t* e) {
+  flowmoe_status_t st = check_rows(s);
+  if (st != FLOWMOE_OK) return st;
+  if (e == nullptr) return fail(FLOWMOE_ERR_INVALID, "embed is null");
+  if (e->vocab < 1) return fail(FLOWMOE_ERR_INVALID, "vocab = %d < 1", e->vocab);
+  if (!isfinite(e->scale)) return fail(FLOWMOE_ERR_INVALID, "scale is not finite");
+  if ((long)e->vocab * s->M > (1L << 40) || s->T > (1 << 30) || e->vocab > (1 << 30) ||
+      !embed_fits(s->T, s->M, e->vocab))
+    return fail(FLOWMOE_ERR_UNSUPPORTED, "tensor too large");
+  return FLOWMOE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+flowmoe_status_t flowmoe_packed_attention_fwd(const flowmoe_shape_t* shape,
+                                              const flowmoe_packed_shape_t* packed,
+                                              const void* qkv, const int32_t* starts, void* attn,
+                                              float* lse, hipStream_t stream) {
+  PackedShape m;
+  flowmoe_status_t st = check_packed(shape, packed, &m);
+  if (st != FLOWMOE_OK) return st;
+  if (shape->T == 0) return ok();
+  REQUIRE_T(qkv, "qkv");
+  REQUIRE_STARTS(m, starts, "starts");
+  REQUIRE_T(attn, "attn");
+  REQUIRE_F(lse, "lse");
+  return hip_status(launch_packed_attn_fwd(m, shape->T, qkv, starts, attn, lse, stream),
+                    "flowmoe_packed_attention_fwd");
+}
+
+size_t flowmoe_packed_attention_ws_bytes(const flowmoe_shape_t* shape,
+                                         const flowmoe_packed_shape_t* packed) {
+  PackedShape m;
+  if (check_packed(shape, packed, &m) != FLOWMOE_OK) return 0;
+  return packed_attn_ws_bytes(m, shape->T);
+}
+
+flowmoe_status_t flowmoe_packed_attention_bwd(const flowmoe_shape_t* shape,
+                                              const flowmoe_packed_shape_t* packed,
+                                              const void* qkv, const int32_t* starts,
+                                              const void* attn, const float* lse,
+                                              const void* d_attn, void* d_qkv, float* delta,
+                                              void* ws, size_t ws_bytes, hipStream_t stream) {
+  PackedShape m;
+  flowmoe_status_t st = check_packed(shape, packed, &m);
+  if (st != FLOWMOE_OK) return st;
+  if (shape->T == 0) return ok();
+  REQUIRE_T(qkv, "qkv");
+  REQUIRE_STARTS(m, starts, "starts");
+  REQUIRE_T(attn, "attn");
+  REQUIRE_F(lse, "lse");
+  REQUIRE_T(d_attn, "d_attn");
+  REQUIRE_T(d_qkv, "d_qkv");
+  REQUIRE_F(delta, "delta");
+  const size_t need = packed_attn_ws_bytes(m, shape->T);
+  st = check_ws(ws, ws_bytes, need, "flowmoe_packed_attention_bwd");
+  if (st != FLOWMOE_OK) return st;
+  if (need > 0) REQUIRE_T(ws, "ws");
+  return hip_status(launch_packed_attn_bwd(m, shape->T, qkv, starts, attn, lse, d_attn, d_qkv,
+                                           delta, ws, stream),
+                    "flowmoe_packed_attention_bwd");
+}
+
+flowmoe_status_t flowmoe_packed_mha_fwd(const flowmoe_shape_t* shape,
+                                        const flowmoe_packed_shape_t* packed,
+                                        const flowmoe_rope_shape_t* rope,
+                                        const flowmoe_packed_mha_bufs_t* b, hipStream_t stream) {
+  PackedShape m;
+  RopeShape r;
+  flowmoe_status_t st = check_packed_mha(shape, packed, rope, &m, &r);
+  if (st != FLOWMOE_OK) return st;
+  if (b == nullptr) return fail(FLOWMOE_ERR_INVALID, "bufs is null");
+  if (shape->T == 0) return ok();
+  REQUIRE_T(b->in, "bufs->in");
+  REQUIRE_T(b->w_qkv, "bufs->w_qkv");
+  REQUIRE_T(b->w_o, "bufs->w_o");
+  if (rope != nullptr) REQUIRE_F(b->positions, "bufs->positions");
+  REQUIRE_STARTS(m, b->starts, "bufs->starts");
+  REQUIRE_T(b->qkv, "bufs->qkv");
+  REQUIRE_T(b->attn, "bufs->attn");
+  REQUIRE_F(b->lse, "bufs->lse");
+  REQUIRE_T(b->out, "bufs->out");
+  return hip_status(launch_packed_mha_fwd(m, rope ? &r : nullptr, shape->T, *b, stream),
+                    "flowmoe_packed_mha_fwd");
+}
+
+size_t flowmoe_packed_mha_ws_bytes(const flowmoe_shape_t* shape,
+                                   const flowmoe_packed_shape_t* packed) {
+  PackedShape m;
+  if (check_packed(shape, packed, &m) != FLOWMOE_OK) return 0;
+  return packed_mha_ws_bytes(m, shape->T);
+}
+
+flowmoe_status_t flowmoe_packed_mha_bwd(const flowmoe_shape_t* shape,
+                                        const flowmoe_packed_shape_t* packed,
+                                        const flowmoe_rope_shape_t* rope,
+                                        const flowmoe_packed_mha_bufs_t* b, int32_t accumulate,
+                                        hipStream_t stream) {
+  PackedShape m;
+  RopeShape r;
+  flowmoe_status_t st = check_packed_mha(shape, packed, rope, &m, &r);
+  if (st != FLOWMOE_OK) return st;
+  if (b == nullptr) return fail(FLOWMOE_ERR_INVALID, "bufs is null");
+  REQUIRE_T(b->dw_qkv, "bufs->dw_qkv");
+  REQUIRE_T(b->dw_o, "bufs->dw_o");
+  if (shape->T > 0) {
+    REQUIRE_T(b->in, "bufs->in");
+    REQUIRE_T(b->w_qkv, "bufs->w_qkv");
+    REQUIRE_T(b->w_o, "bufs->w_o");
+    if (rope != nullptr) REQUIRE_F(b->positions, "bufs->positions");
+    REQUIRE_STARTS(m, b->starts, "bufs->starts");
+    REQUIRE_T(b->qkv, "bufs->qkv");
+    REQUIRE_T(b->attn, "bufs->attn");
+    REQUIRE_F(b->lse, "bufs->lse");
+    REQUIRE_T(b->d_out, "bufs->d_out");
+    REQUIRE_T(b->d_attn, "bufs->d_attn");
+    REQUIRE_T(b->d_qkv, "bufs->d_qkv");
+    REQUIRE_F(b->delta, "bufs->delta");
+    REQUIRE_T(b->d_in, "bufs->d_in");
+  }
+  const size_t need = packed_mha_ws_bytes(m, shape->T);
+  st = check_ws(b->ws, b->ws_bytes, need, "flowmoe_packed_mha_bwd");
+  if (st != FLOWMOE_OK) return st;
+  if (need > 0) REQUIRE_T(b->ws, "bufs->ws");
+  return hip_status(launch_packed_mha_bwd(m, rope ? &r : nullptr, shape->T, *b, accumulate != 0,
+                                          stream),
+                    "flowmoe_packed_mha_bwd");
+}
+
+flowmoe_status_t flowmoe_layer_norm_fwd(const flowmoe_shape_t* shape, float eps, const void* x,
+                                        const void* res, const float* gain, const float* bias,
+                                        void* sum, void* y, hipStream_t stream) {
+  flowmoe_status_t st = check_layer_norm(shape, eps);
+  if (st != FLOWMOE_OK) return st;
+  if (shape->T == 0) return ok();
+  REQUIRE_T(x, "x");
+  if (res != nullptr) REQUIRE_T(res, "res");
+  CHECK_A4(gain, "gain");
+  CHECK_A4(bias, "bias");
+  if (sum != nullptr) REQUIRE_T(sum, "sum");
+  REQUIRE_T(y, "y");
+  if (sum == y) return fail(FLOWMOE_ERR_INVALID, "sum and y are one buffer");
+  return hip_status(launch_layer_norm_fwd(shape->dtype, shape->T, shape->M, eps, x, res, gain, bias,
+                                          sum, y, stream),
+                    "flowmoe_layer_norm_fwd");
+}
+
+size_t flowmoe_layer_norm_ws_bytes(const flowmoe_shape_t* shape) {
+  if (check_layer_norm(shape, 1.0f) != FLOWMOE_OK) return 0;
+  return layer_norm_ws_bytes(shape->T, shape->M);
+}
+
+flowmoe_status_t flowmoe_layer_norm_bwd(const flowmoe_shape_t* shape, float eps, const void* x,
+                                        const float* gain, const void* dy, const void* d_sum,
+                                        void* dx, float* dgain, float* dbias, int32_t accumulate,
+                                        void* ws, size_t ws_bytes, hipStream_t stream) {
+  flowmoe_status_t st = check_layer_norm(shape, eps);
+  if (st != FLOWMOE_OK) return st;
+  if (shape->T > 0) {
+    REQUIRE_T(x, "x");
+    CHECK_A4(gain, "gain");
+    REQUIRE_T(dy, "dy");
+    if (d_sum != nullptr) REQUIRE_T(d_sum, "d_sum");
+    REQUIRE_T(dx, "dx");
+  }
+  CHECK_A4(dgain, "dgain");
+  CHECK_A4(dbias, "dbias");
+  if (dgain != nullptr || dbias != nullptr) {
+    const size_t need = layer_norm_ws_bytes(shape->T, shape->M);
+    st = check_ws(ws, ws_bytes, need, "flowmoe_layer_norm_bwd");
+    if (st != FLOWMOE_OK) return st;
+    if (need > 0) REQUIRE_T(ws, "ws");
+  }
+  return hip_status(launch_layer_norm_bwd(shape->dtype, shape->T, shape->M, eps, x, gain, dy, d_sum,
+                                          dx, dgain, dbias, accumulate != 0, ws, stream),
+                    "flowmoe_layer_norm_bwd");
+}
+
+flowmoe_status_t flowmoe_embed_fwd(const flowmoe_shape_t* shape, const flowmoe_embed_shape_t* embed,
+                                   const int32_t* ids, const void* table, void* y,
+                                   hipStream_t stream) {
+  flowmoe_status_t st = check_embed(shape, embed);
+  if (st != FLOWMOE_OK) return st;
+  if (shape->T == 0) return ok();
+  REQUIRE_F(ids, "ids");
+  REQUIRE_T(table, "table");
+  REQUIRE_T(y, "y");
+  return hip_status(launch_embed_fwd(shape->dtype, shape->T, shape->M, embed->vocab, embed->scale,
+                                     ids, table, y, stream),
+                    "flowmoe_embed_fwd");
+}
+
+size_t flowmoe_embed_ws_bytes(const flowmoe_shape_t* shape, const flowmoe_embed_shape_t* embed) {
+  if (check_embed(shape, embed) != FLOWMOE_OK) return 0;
+  return embed_ws_bytes(shape->T, shape->M);
+}
+
+flowmoe_status_t flowmoe_embed_bwd(const flowmoe_shape_t* shape, const flowmoe_embed_shape_t* embed,
+                                   const int32_t* ids, const void* dy, float* dtable,
+                                   int32_t accumulate, void* ws, size_t ws_bytes,
+                                   hipStream_t stream) {
+  flowmoe_status_t st = check_embed(shape, embed);
+  if (st != FLOWMOE_OK) return st;
+  REQUIRE_T(dtable, "dtable");
+  if (shape->T > 0) {
+    REQUIRE_F(ids, "ids");
+    REQUIRE_T(dy, "dy");
+  }
+  const size_t need = embed_ws_bytes(shape->T, shape->M);
+  st = check_ws(ws, ws_bytes, need, "flowmoe_embed_bwd");
+  if (st != FLOWMOE_OK) return st;
+  if (need > 0) REQUIRE_T(ws, "ws");
+  return hip_status(launch_embed_bwd(shape->dtype, shape->T, shape->M, embed->vocab, embed->scale,
+                                     ids, dy, dtable, accumulate != 0, ws, stream),
+                    "flowmoe_embed_bwd");
 }
 
 }  // extern "C"

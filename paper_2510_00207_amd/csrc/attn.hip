@@ -23,6 +23,8 @@
 //     the key as the accumulator column, dV^T += dO^T P, dK^T += Q^T dS.
 #include <math.h>
 
+#include <algorithm>
+
 #include "attn_tiles.hpp"
 #include "common.hpp"
 
@@ -42,6 +44,10 @@ struct AttnArgs {
   int pair;  // causal grid of one round of resident blocks: pair long and short tiles (decode)
   float c2;  // log2(e) / sqrt(D): a score times c2 is its base-2 exponent
   float rs;  // 1 / sqrt(D)
+  // packed sequences (locate): nseq of them from rows starts[i] on, query heads in groups
+  // that share kv key/value heads
+  const int32_t* starts;
+  int kv;
 };
 
 // block -> (query or key tile, head, sequence). Blocks are dispatched in
@@ -75,6 +81,83 @@ __device__ __forceinline__ void decode(const AttnArgs& a, bool rev, bool shared,
   sq = rest / a.heads;
 }
 
+// A block's rows: tokens tok0 .. tok0 + N - 1 are the sequence, `tile` of it the block's;
+// qkv rows are ld apart, head hd's K and V columns k and v past its Q columns.
+struct Span {
+  long tok0, ld, k, v;
+  int N, tile, hd;
+  bool none;  // packed: no sequence's rows, whose outputs are zeros
+};
+
+// Packed sequences: tile t of sequence i has slot starts[i] / rows + i + t. Sequence i has
+// at most as many tiles as there are slots before sequence i + 1's, so that a block finds
+// its sequence by a search for its slot, without sums over the lengths, and a launch has
+// T / rows + nseq + 1 slots whatever the lengths are; those behind a sequence's last tile
+// stay empty (false). The rows behind the last sequence are a sequence of their own. The
+// search is a wave's: 64 starts at a time. Whatever `starts` holds, rows stay in 0 .. T.
+__device__ __forceinline__ int packed_start(const AttnArgs& a, int i) {
+  return i == 0 ? 0 : i > a.nseq ? a.T : min(max(a.starts[i], 0), a.T);
+}
+__device__ __forceinline__ bool locate(const AttnArgs& a, int slot, int rows, int lane, Span& s) {
+  int lo = 0, hi = a.nseq + 1;  // sequences lo .. hi - 1 may hold the slot, lo starts before it
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+    const bool before = i < hi && packed_start(a, i) / rows + i <= slot;
+    const int n = max(1, (int)__popcll(__ballot(before)));
+    lo += (n - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  const int i = __builtin_amdgcn_readfirstlane(lo);
+  const int r0 = __builtin_amdgcn_readfirstlane(packed_start(a, i));
+  s.tok0 = r0;
+  s.N = __builtin_amdgcn_readfirstlane(packed_start(a, i + 1)) - r0;
+  s.tile = slot - r0 / rows - i;
+  s.none = i == a.nseq;
+  return s.tile >= 0 && s.tile * (long)rows < s.N;
+}
+
+// The packed grid: slots in descending order (a sequence's longest causal tiles first),
+// `per` heads of a slot side by side; where per is a multiple of 8, those of a group on
+// one XCD, through whose L2 they read their keys.
+__device__ __forceinline__ bool packed_span(const AttnArgs& a, int per, bool rev, int rows,
+                                            int lane, Span& s) {
+  const int j = (int)(blockIdx.x % per), u = (int)(blockIdx.x / per);
+  s.hd = per % 8 == 0 ? (j & 7) * (per >> 3) + (j >> 3) : j;
+  return locate(a, rev ? (int)(gridDim.x / per) - 1 - u : u, rows, lane, s);
+}
+
+// zeros in `cols` columns of rows r0 .. r0 + n - 1 (16-byte vectors)
+__device__ __forceinline__ void zero_rows(bf16_t* dst, long ld, long r0, int n, int cols, int tid,
+                                          int threads) {
+  const int c = cols / 8;
+  for (int i = tid; i < n * c; i += threads)
+    *reinterpret_cast<u32x4*>(dst + (r0 + i / c) * ld + 8 * (i % c)) = u32x4{0, 0, 0, 0};
+}
+
+// Query tiles: the block's span, with or without packing; false: no rows
+template <bool PACKED>
+__device__ __forceinline__ bool query_span(const AttnArgs& a, int D, bool causal, int rows,
+                                           int lane, Span& s) {
+  if constexpr (PACKED) {
+    const bool any = packed_span(a, a.heads, true, rows, lane, s);
+    s.ld = (long)(a.heads + 2 * a.kv) * D;
+    const int g = s.hd / (a.heads / a.kv);
+    s.k = (long)(a.heads + g - s.hd) * D;
+    s.v = s.k + (long)a.kv * D;
+    return any;
+  } else {
+    int sq;
+    decode(a, causal, a.shared != 0, s.tile, s.hd, sq, rows);
+    s.N = a.N;
+    s.tok0 = (long)sq * a.N;
+    s.ld = 3L * a.M;
+    s.k = a.M;
+    s.v = 2L * a.M;
+    s.none = false;
+    return true;
+  }
+}
+
 // Forward: blocks of 4 waves of 32 queries (8 in some launches of heads of 64), two to
 // four to a CU.
 //
@@ -100,7 +183,7 @@ __device__ __forceinline__ void decode(const AttnArgs& a, bool rev, bool shared,
 // where a launch is several rounds. us of the loop before, ahead, in turn: 32
 // sequences of 512, 16 heads, bidirectional 56, 62, 51 (8 waves); 4 x 4096, 24 heads,
 // causal 252, 266, 229; 8 x 512 20, 19, 18; 1 x 4096, 8 heads 64, 54, 55.
-template <int D, bool CAUSAL, int NW>
+template <int D, bool CAUSAL, int NW, bool PACKED>
 __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(AttnArgs a) {
   constexpr bool AHEAD = D == 128;
   constexpr int KS = D / 16, DB = D / 32, QB = 32 * NW;
@@ -112,18 +195,28 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
   // scalar branches instead of exec-mask ones (backward 7-10% faster)
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
-  int qt, hd, sq;
-  decode(a, CAUSAL, a.shared != 0, qt, hd, sq, QB);
-  const long tok0 = (long)sq * a.N, ld = 3L * a.M;
+  Span sp;
+  if (!query_span<PACKED>(a, D, CAUSAL, QB, lane, sp)) return;
+  const long tok0 = sp.tok0, ld = sp.ld;
+  const int hd = sp.hd, N = sp.N, q0 = sp.tile * QB, qw = q0 + 32 * w + lq;
+  if constexpr (PACKED) {
+    if (sp.none) {
+      const int n = min(QB, N - q0);
+      zero_rows(a.out + (long)hd * D, a.M, tok0 + q0, n, D, tid, 64 * NW);
+      for (int i = tid; i < n; i += 64 * NW) a.lse[(long)hd * a.T + tok0 + q0 + i] = 0.0f;
+      return;
+    }
+  }
   const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
-  const bf16_t* Kg = Qg + a.M;
-  const bf16_t* Vg = Qg + 2L * a.M;
-  const int q0 = qt * QB, qw = q0 + 32 * w + lq;
+  const bf16_t* Kg = Qg + sp.k;
+  const bf16_t* Vg = Qg + sp.v;
 
-  const int kend = CAUSAL ? min(a.N, q0 + QB) : a.N;
+  const int kend = CAUSAL ? min(N, q0 + QB) : N;
   const int nk = (kend + 63) / 64;
-  // (causal: a wave whose queries all precede a tile has nothing in it)
-  const int nkw = CAUSAL ? min(nk, (q0 + 32 * w + 31) / 64 + 1) : nk;
+  // (causal: a wave whose queries all precede a tile has nothing in it; packed: nor one
+  // without queries)
+  const int nkc = CAUSAL ? min(nk, (q0 + 32 * w + 31) / 64 + 1) : nk;
+  const int nkw = PACKED && q0 + 32 * w >= N ? 0 : nkc;
   const Dma dma(lds_base(lds), w, lane, ld);
   const long kstep = 64 * ld;
   dma.load(Kg, kend, 0);
@@ -133,7 +226,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
   bf16x8 qf[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks)
-    qf[ks] = qw < a.N ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * ks + 8 * h2) : zero8();
+    qf[ks] = qw < N ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * ks + 8 * h2) : zero8();
   floatx16 o[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = zero16();
@@ -141,13 +234,13 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
 
   int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
   auto mask = [&](floatx16 (&s)[2], int kb0) {
-    if (kb0 + 64 > a.N || (CAUSAL && kb0 + 63 > q0 + 32 * w)) {
+    if (kb0 + 64 > N || (CAUSAL && kb0 + 63 > q0 + 32 * w)) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = kb0 + 32 * kb + 8 * (r >> 2) + 4 * h2 + (r & 3);
-          if (key >= a.N || (CAUSAL && key > qw)) s[kb][r] = -INFINITY;
+          if (key >= N || (CAUSAL && key > qw)) s[kb][r] = -INFINITY;
         }
     }
   };
@@ -356,7 +449,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
     step(t, Stage<0>{});
     if (t + 1 < nk) step(t + 1, Stage<1>{});
   }
-  if (qw < a.N) {
+  if (qw < N) {
     const float inv = 1.0f / l;
     bf16_t* Og = a.out + (tok0 + qw) * a.M + (long)hd * D;
 #pragma unroll
@@ -374,7 +467,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
 // rows are read from LDS (registers hold Q). Before -> now: 4 x 4096 tokens, 32 heads
 // of 128, causal 970 -> 850 us; one sequence of 4096, 16 heads 171 -> 135; 4 x 1500, 20
 // heads of 64, bidirectional 112 -> 102.
-template <int D, bool CAUSAL>
+template <int D, bool CAUSAL, bool PACKED>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int KS = D / 16, DB = D / 32, NW = 4, QB = 32 * NW;
   using Dma = TileDma<D, 32, NW>;
@@ -385,28 +478,38 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   // scalar branches instead of exec-mask ones (backward 7-10% faster)
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
-  int qt, hd, sq;
-  decode(a, CAUSAL, a.shared != 0, qt, hd, sq, QB);
-  const long tok0 = (long)sq * a.N, ld = 3L * a.M;
+  Span sp;
+  if (!query_span<PACKED>(a, D, CAUSAL, QB, lane, sp)) return;
+  const long tok0 = sp.tok0, ld = sp.ld;
+  const int hd = sp.hd, N = sp.N, q0 = sp.tile * QB, qw = q0 + 32 * w + lq;
+  if constexpr (PACKED) {
+    if (sp.none) {
+      const int n = min(QB, N - q0);
+      zero_rows(a.d_qkv + (long)hd * D, ld, tok0 + q0, n, D, tid, 64 * NW);
+      for (int i = tid; i < n; i += 64 * NW) a.delta[(long)hd * a.T + tok0 + q0 + i] = 0.0f;
+      return;
+    }
+  }
   const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
-  const bf16_t* Kg = Qg + a.M;
-  const bf16_t* Vg = Qg + 2L * a.M;
+  const bf16_t* Kg = Qg + sp.k;
+  const bf16_t* Vg = Qg + sp.v;
   const bf16_t* Gg = a.d_o + tok0 * a.M + (long)hd * D;
   const bf16_t* Og = a.o + tok0 * a.M + (long)hd * D;
-  const int q0 = qt * QB, qw = q0 + 32 * w + lq;
-  const bool live = qw < a.N;
+  const bool live = qw < N;
 
-  const int kend = CAUSAL ? min(a.N, q0 + QB) : a.N;
+  const int kend = CAUSAL ? min(N, q0 + QB) : N;
   const int nk = (kend + 31) / 32;
-  // (causal: a wave whose queries all precede a tile has nothing in it)
-  const int nkw = CAUSAL ? min(nk, (q0 + 32 * w + 31) / 32 + 1) : nk;
+  // (causal: a wave whose queries all precede a tile has nothing in it; packed: nor one
+  // without queries)
+  const int nkc = CAUSAL ? min(nk, (q0 + 32 * w + 31) / 32 + 1) : nk;
+  const int nkw = PACKED && q0 + 32 * w >= N ? 0 : nkc;
   const long kstep = 32 * ld;
   const Dma dma(lds_base(lds), w, lane, ld);
   {
     const Dma dmag(lds_base(lds), w, lane, a.M);
 #pragma unroll
     for (int i = 0; i < NW; ++i)
-      dmag.load(Gg + (long)(q0 + 32 * i) * a.M, a.N - q0 - 32 * i, GB + i * TB);
+      dmag.load(Gg + (long)(q0 + 32 * i) * a.M, N - q0 - 32 * i, GB + i * TB);
   }
   dma.load(Kg, kend, 0);
   dma.load(Vg, kend, VB);
@@ -454,11 +557,11 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     y = mfma(fr[i % RS][1], fr[i % RS][2], i == 0 ? zero16() : y);
   };
   auto mask = [&](floatx16& x, int kb0) {
-    if (kb0 + 32 > a.N || (CAUSAL && kb0 + 31 > q0 + 32 * w)) {
+    if (kb0 + 32 > N || (CAUSAL && kb0 + 31 > q0 + 32 * w)) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int key = kb0 + 8 * (r >> 2) + 4 * h2 + (r & 3);
-        if (key >= a.N || (CAUSAL && key > qw)) x[r] = -INFINITY;
+        if (key >= N || (CAUSAL && key > qw)) x[r] = -INFINITY;
       }
     }
   };
@@ -561,7 +664,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
 // the CU fills the elementwise part (half of it beside the first products of
 // dV and dK was 2-4% slower at D = 128). Before -> now, as above: 1258 -> 1120, 256 ->
 // 182 and 163 -> 127 us.
-template <int D, bool CAUSAL>
+template <int D, bool CAUSAL, bool PACKED>
 __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
   constexpr int KS = D / 16, DB = D / 32, NW = 4, KB = 32 * NW;
   using Dma = TileDma<D, 32, NW>;
@@ -574,38 +677,68 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
   // scalar branches instead of exec-mask ones (backward 7-10% faster)
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
-  int kt, hd, sq;
-  decode(a, false, false, kt, hd, sq, KB);
-  const long tok0 = (long)sq * a.N, ld = 3L * a.M;
+  Span sp;
+  int nh = 1;  // query heads from hd on
+  if constexpr (PACKED) {
+    const bool any = packed_span(a, a.kv, false, KB, lane, sp);
+    if (!any) return;
+    const int g = sp.hd;
+    nh = a.heads / a.kv;
+    sp.hd = g * nh;
+    sp.ld = (long)(a.heads + 2 * a.kv) * D;
+    sp.k = (long)(a.heads + g - sp.hd) * D;
+    sp.v = sp.k + (long)a.kv * D;
+  } else {
+    int sq;
+    decode(a, false, false, sp.tile, sp.hd, sq, KB);
+    sp.N = a.N;
+    sp.tok0 = (long)sq * a.N;
+    sp.ld = 3L * a.M;
+    sp.k = a.M;
+    sp.v = 2L * a.M;
+    sp.none = false;
+  }
+  const long tok0 = sp.tok0, ld = sp.ld;
+  const int hd = sp.hd, N = sp.N, k0 = sp.tile * KB, kw = k0 + 32 * w + lq;
+  if constexpr (PACKED) {
+    if (sp.none) {
+      const int n = min(KB, N - k0);
+      zero_rows(a.d_qkv + hd * D + sp.k, ld, tok0 + k0, n, D, tid, 64 * NW);
+      zero_rows(a.d_qkv + hd * D + sp.v, ld, tok0 + k0, n, D, tid, 64 * NW);
+      return;
+    }
+  }
   const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
   const bf16_t* Gg = a.d_o + tok0 * a.M + (long)hd * D;
   const long srow0 = (long)hd * a.T + tok0;
-  const int k0 = kt * KB, kw = k0 + 32 * w + lq;
-  const bool live = kw < a.N;
+  const bool live = kw < N;
   // query steps of 32: causal keys k0.. are seen by queries >= k0 only
   const int qs0 = CAUSAL ? k0 : 0;
-  const int nqs = (a.N - qs0 + 31) / 32;
+  const int nqs = (N - qs0 + 31) / 32;
+  // packed: the group's query heads one after the other, nqs steps each
+  const int steps = PACKED ? nh * nqs : nqs;
+  int qi = 0;  // step of the head
 
   const Dma dma(lds_base(lds), w, lane, ld), dmag(lds_base(lds), w, lane, a.M);
 #pragma unroll
   for (int i = 0; i < NW; ++i)
-    dma.load(Qg + 2L * a.M + (long)(k0 + 32 * i) * ld, a.N - k0 - 32 * i, VT + i * TQ);
+    dma.load(Qg + sp.v + (long)(k0 + 32 * i) * ld, N - k0 - 32 * i, VT + i * TQ);
   bf16x8 kf[KS];
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks)
-    kf[ks] = live ? *reinterpret_cast<const bf16x8*>(Qg + a.M + kw * ld + 16 * ks + 8 * h2) : zero8();
+    kf[ks] = live ? *reinterpret_cast<const bf16x8*>(Qg + sp.k + kw * ld + 16 * ks + 8 * h2) : zero8();
   float rstat = 0.0f;  // (the block's first 64 threads)
-  const float* sp = (tid < 32 ? a.lse : a.delta) + srow0 + (tid & 31);
+  const float* sp_stat = (tid < 32 ? a.lse : a.delta) + srow0 + (tid & 31);
   auto load_stat = [&](int qb) {
-    if (tid < 64) rstat = qb + (tid & 31) < a.N ? sp[qb] * (tid < 32 ? kLog2e : 1.0f) : 0.0f;
+    if (tid < 64) rstat = qb + (tid & 31) < N ? sp_stat[qb] * (tid < 32 ? kLog2e : 1.0f) : 0.0f;
   };
   auto store_stat = [&](int slot) {
     if (tid < 64) reinterpret_cast<float*>(lds + ST + 256 * slot)[tid] = rstat;
   };
   const bf16_t* Qt = Qg + qs0 * ld;
   const bf16_t* Gt = Gg + (long)qs0 * a.M;
-  dma.load(Qt, a.N - qs0, 0);
-  dmag.load(Gt, a.N - qs0, TQ);
+  dma.load(Qt, N - qs0, 0);
+  dmag.load(Gt, N - qs0, TQ);
   load_stat(qs0);
   store_stat(0);
   floatx16 dv[DB], dk[DB];
@@ -634,21 +767,34 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
   auto step = [&](const int it, auto stc) {
     constexpr int st = decltype(stc)::value;
     opaque(rbase, tb0, tb1);
-    const int qb = qs0 + 32 * it;
+    const int qb = qs0 + 32 * (PACKED ? qi : it);
     wait_vm<0>();   // this tile's loads
     lds_barrier();  // and every wave's reads of the other slot are done
     const char* tq = lds + st * 2 * TQ;
     const float* l2 = reinterpret_cast<const float*>(lds + ST + 256 * st);
-    const bool mine = !CAUSAL || qb + 31 >= k0 + 32 * w;
+    // (packed: nor for a wave without keys)
+    const bool mine = (!CAUSAL || qb + 31 >= k0 + 32 * w) && !(PACKED && k0 + 32 * w >= N);
     if (mine) {
       read_group(tq, 0);
       if constexpr (RS > 2) read_group(tq, 1);
     }
+    int qn = qb + 32;
     Qt += 32 * ld;
     Gt += 32L * a.M;
-    dma.load(Qt, a.N - qb - 32, (st ^ 1) * 2 * TQ);
-    dmag.load(Gt, a.N - qb - 32, (st ^ 1) * 2 * TQ + TQ);
-    if (it + 1 < nqs) load_stat(qb + 32);
+    if constexpr (PACKED) {
+      if (++qi == nqs) {  // the next head's first step
+        qi = 0;
+        qn = qs0;
+        Qt += D - 32 * nqs * ld;
+        Gt += D - 32L * nqs * a.M;
+        sp_stat += a.T;
+      }
+    }
+    // (after the last step: its head's rows end, or there is no further head)
+    const int left = !PACKED || it + 1 < steps ? N - qn : 0;
+    dma.load(Qt, left, (st ^ 1) * 2 * TQ);
+    dmag.load(Gt, left, (st ^ 1) * 2 * TQ + TQ);
+    if (it + 1 < steps) load_stat(qn);
     if (mine) {
       floatx16 s, dp;
       __builtin_amdgcn_sched_barrier(0);
@@ -660,11 +806,11 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
         dp = mfma(fr[i % RS][1], fr[i % RS][2], i == 0 ? zero16() : dp);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (qb + 32 > a.N || (CAUSAL && k0 + 32 * w + 31 > qb)) {
+      if (qb + 32 > N || (CAUSAL && k0 + 32 * w + 31 > qb)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int q = qb + 8 * (r >> 2) + 4 * h2 + (r & 3);
-          if (q >= a.N || (CAUSAL && kw > q)) s[r] = -INFINITY;
+          if (q >= N || (CAUSAL && kw > q)) s[r] = -INFINITY;
         }
       }
       unsigned pp[8], pd[8];  // P and dS of this lane, bf16 pairs
@@ -696,18 +842,18 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (it + 1 < nqs) store_stat(st ^ 1);
+    if (it + 1 < steps) store_stat(st ^ 1);
   };
-  for (int it = 0; it < nqs; it += 2) {
+  for (int it = 0; it < steps; it += 2) {
     step(it, Stage<0>{});
-    if (it + 1 < nqs) step(it + 1, Stage<1>{});
+    if (it + 1 < steps) step(it + 1, Stage<1>{});
   }
   if (live) {
     bf16_t* dst = a.d_qkv + (tok0 + kw) * ld + (long)hd * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-      store_cols(dst + a.M + 32 * db, dk[db], h2, a.rs);
-      store_cols(dst + 2L * a.M + 32 * db, dv[db], h2, 1.0f);
+      store_cols(dst + sp.k + 32 * db, dk[db], h2, a.rs);
+      store_cols(dst + sp.v + 32 * db, dv[db], h2, 1.0f);
     }
   }
 }
@@ -768,19 +914,19 @@ bool shared_order(const AttnShape& m, const AttnArgs& a) {
 template <int D, int NW>
 void launch_fwd(const AttnShape& m, const AttnArgs& a, hipStream_t st) {
   const dim3 g(attn_blocks(a, 32 * NW)), b(64 * NW);
-  if (m.causal) hipLaunchKernelGGL((attn_fwd_kernel<D, true, NW>), g, b, 0, st, a);
-  else hipLaunchKernelGGL((attn_fwd_kernel<D, false, NW>), g, b, 0, st, a);
+  if (m.causal) hipLaunchKernelGGL((attn_fwd_kernel<D, true, NW, false>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((attn_fwd_kernel<D, false, NW, false>), g, b, 0, st, a);
 }
 
 #define FLOWMOE_ATTN_LAUNCH(KERNEL, a, st)                                       \
   do {                                                                            \
     const dim3 g(attn_blocks(a)), b(256);                                         \
     if (m.D == 128) {                                                             \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true>), g, b, 0, st, a);      \
-      else hipLaunchKernelGGL((KERNEL<128, false>), g, b, 0, st, a);              \
+      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true, false>), g, b, 0, st, a);      \
+      else hipLaunchKernelGGL((KERNEL<128, false, false>), g, b, 0, st, a);              \
     } else {                                                                      \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true>), g, b, 0, st, a);       \
-      else hipLaunchKernelGGL((KERNEL<64, false>), g, b, 0, st, a);               \
+      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true, false>), g, b, 0, st, a);       \
+      else hipLaunchKernelGGL((KERNEL<64, false, false>), g, b, 0, st, a);               \
     }                                                                             \
   } while (0)
 
@@ -819,6 +965,124 @@ hipError_t launch_attn_bwd(const AttnShape& m, int T, int M, const void* qkv, co
   if (e != hipSuccess) return e;
   return traced(FLOWMOE_K_ATTN_BWD_DKDV, st,
                 [&] { FLOWMOE_ATTN_LAUNCH(attn_dkdv_kernel, a, st); });
+}
+
+// ---------------------------------------------------------------------------
+// packed sequences
+// ---------------------------------------------------------------------------
+namespace {
+
+AttnArgs packed_args(const PackedShape& m, int T, const void* qkv, const int32_t* starts) {
+  AttnArgs a = {};
+  a.T = T;
+  a.M = m.heads * m.D;
+  a.heads = m.heads;
+  a.kv = m.kv;
+  a.nseq = m.nseq;
+  a.starts = starts;
+  a.c2 = kLog2e / sqrtf((float)m.D);
+  a.rs = 1.0f / sqrtf((float)m.D);
+  a.qkv = static_cast<const bf16_t*>(qkv);
+  return a;
+}
+
+// blocks of a packed grid: its slots (locate) times `per` heads
+unsigned packed_blocks(const AttnArgs& a, int rows, int per) {
+  return (unsigned)((a.T / rows + a.nseq + 1) * (long)per);
+}
+
+}  // namespace
+
+size_t packed_attn_ws_bytes(const PackedShape&, int) { return 0; }
+
+#define FLOWMOE_PACKED_LAUNCH(KERNEL, ARGS64, ARGS128, grid, threads)                         \
+  do {                                                                                        \
+    const dim3 g(grid), b(threads);                                                           \
+    if (m.D == 128) {                                                                         \
+      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true ARGS128, true>), g, b, 0, st, a);    \
+      else hipLaunchKernelGGL((KERNEL<128, false ARGS128, true>), g, b, 0, st, a);            \
+    } else {                                                                                  \
+      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true ARGS64, true>), g, b, 0, st, a);      \
+      else hipLaunchKernelGGL((KERNEL<64, false ARGS64, true>), g, b, 0, st, a);              \
+    }                                                                                         \
+  } while (0)
+#define FLOWMOE_NW4 , 4
+#define FLOWMOE_NONE
+
+hipError_t launch_packed_attn_fwd(const PackedShape& m, int T, const void* qkv,
+                                  const int32_t* starts, void* o, float* lse, hipStream_t st) {
+  if (T == 0) return hipSuccess;
+  AttnArgs a = packed_args(m, T, qkv, starts);
+  a.out = static_cast<bf16_t*>(o);
+  a.lse = lse;
+  return traced(FLOWMOE_K_ATTN_FWD, st, [&] {
+    FLOWMOE_PACKED_LAUNCH(attn_fwd_kernel, FLOWMOE_NW4, FLOWMOE_NW4, packed_blocks(a, 128, m.heads), 256);
+  });
+}
+
+hipError_t launch_packed_attn_bwd(const PackedShape& m, int T, const void* qkv,
+                                  const int32_t* starts, const void* o, const float* lse,
+                                  const void* d_o, void* d_qkv, float* delta, void*,
+                                  hipStream_t st) {
+  if (T == 0) return hipSuccess;
+  AttnArgs a = packed_args(m, T, qkv, starts);
+  a.o = static_cast<const bf16_t*>(o);
+  a.d_o = static_cast<const bf16_t*>(d_o);
+  a.d_qkv = static_cast<bf16_t*>(d_qkv);
+  a.lse = const_cast<float*>(lse);
+  a.delta = delta;
+  const hipError_t e = traced(FLOWMOE_K_ATTN_BWD_DQ, st, [&] {
+    FLOWMOE_PACKED_LAUNCH(attn_dq_kernel, FLOWMOE_NONE, FLOWMOE_NONE, packed_blocks(a, 128, m.heads), 256);
+  });
+  if (e != hipSuccess) return e;
+  return traced(FLOWMOE_K_ATTN_BWD_DKDV, st, [&] {
+    FLOWMOE_PACKED_LAUNCH(attn_dkdv_kernel, FLOWMOE_NONE, FLOWMOE_NONE, packed_blocks(a, 128, m.kv), 256);
+  });
+}
+
+size_t packed_mha_ws_bytes(const PackedShape& m, int T) {
+  const int M = m.heads * m.D, W = M + 2 * m.kv * m.D;
+  return align256(std::max(packed_attn_ws_bytes(m, T),
+                           std::max(wgrad_part_bytes(M, W, T), wgrad_part_bytes(M, M, T))));
+}
+
+hipError_t launch_packed_mha_fwd(const PackedShape& m, const RopeShape* r, int T,
+                                 const flowmoe_packed_mha_bufs_t& b, hipStream_t st) {
+  if (T == 0) return hipSuccess;
+  if (r != nullptr && !rope_fits(*r, T)) return hipErrorInvalidConfiguration;  // (before any launch)
+  const int M = m.heads * m.D, W = M + 2 * m.kv * m.D;
+  hipError_t e = launch_dense_gemm(FLOWMOE_K_ATTN_QKV, T, b.in, M, M, b.w_qkv, W, false, W, b.qkv, W, st);
+  if (e == hipSuccess && r != nullptr)
+    e = launch_rope(*r, FLOWMOE_BF16, T, W, false, b.qkv, b.positions, b.qkv, st);
+  if (e == hipSuccess) e = launch_packed_attn_fwd(m, T, b.qkv, b.starts, b.attn, b.lse, st);
+  if (e != hipSuccess) return e;
+  return launch_dense_gemm(FLOWMOE_K_ATTN_OUT, T, b.attn, M, M, b.w_o, M, false, M, b.out, M, st);
+}
+
+hipError_t launch_packed_mha_bwd(const PackedShape& m, const RopeShape* r, int T,
+                                 const flowmoe_packed_mha_bufs_t& b, int accumulate,
+                                 hipStream_t st) {
+  if (r != nullptr && !rope_fits(*r, T)) return hipErrorInvalidConfiguration;
+  const int M = m.heads * m.D, W = M + 2 * m.kv * m.D;
+  hipError_t e = hipSuccess;
+  if (T > 0) {
+    e = launch_dense_gemm(FLOWMOE_K_ATTN_DGRAD, T, b.d_out, M, M, b.w_o, M, true, M, b.d_attn, M, st);
+    if (e == hipSuccess)
+      e = launch_packed_attn_bwd(m, T, b.qkv, b.starts, b.attn, b.lse, b.d_attn, b.d_qkv, b.delta,
+                                 b.ws, st);
+    if (e == hipSuccess && r != nullptr)
+      e = launch_rope(*r, FLOWMOE_BF16, T, W, true, b.d_qkv, b.positions, b.d_qkv, st);
+    if (e == hipSuccess)
+      e = launch_dense_gemm(FLOWMOE_K_ATTN_DGRAD, T, b.d_qkv, W, W, b.w_qkv, W, true, M, b.d_in, M, st);
+  }
+  float* part = static_cast<float*>(b.ws);
+  if (e == hipSuccess)
+    e = launch_dense_wgrad(FLOWMOE_K_ATTN_WGRAD, T, 1, b.attn, M, 0, M, b.d_out, M, 0, M, b.dw_o, M,
+                           accumulate, wgrad_part_bytes(M, M, T) ? part : nullptr, st);
+  if (e == hipSuccess)
+    e = launch_dense_wgrad(FLOWMOE_K_ATTN_WGRAD, T, 1, b.in, M, 0, M, b.d_qkv, W, 0, W, b.dw_qkv, W,
+                           accumulate, wgrad_part_bytes(M, W, T) ? part : nullptr, st);
+  return e;
 }
 
 hipError_t launch_mha_fwd(const AttnShape& m, int T, int M, const void* in, const void* w_qkv,

@@ -411,6 +411,24 @@ hipError_t launch_mha_wgrad(int T, int M, int R, const void* in, const void* att
                             const void* d_out, const void* d_qkv, float* dw_qkv, float* dw_o,
                             int accumulate, void* ws, hipStream_t st);
 
+// Attention over packed sequences: sequence i of nseq is rows starts[i] .. starts[i + 1] - 1
+// (device data) of T, heads query heads on kv key/value heads of width D (64 or 128), bf16
+struct PackedShape {
+  int nseq, heads, kv, D, causal;
+};
+size_t packed_attn_ws_bytes(const PackedShape& m, int T);
+hipError_t launch_packed_attn_fwd(const PackedShape& m, int T, const void* qkv,
+                                  const int32_t* starts, void* o, float* lse, hipStream_t st);
+hipError_t launch_packed_attn_bwd(const PackedShape& m, int T, const void* qkv,
+                                  const int32_t* starts, const void* o, const float* lse,
+                                  const void* d_o, void* d_qkv, float* delta, void* ws,
+                                  hipStream_t st);
+// partial sums of a weight gradient (M x N) whose rows are split
+inline size_t wgrad_part_bytes(int M, int N, long rows) {
+  const int s = dense_wgrad_splits(M, N, rows);
+  return s > 1 ? (size_t)s * M * N * sizeof(float) : 0;
+}
+
 // Differential attention: T tokens = T / N sequences of N, `heads` query heads and `kv`
 // key/value heads of width D (64 or 128), two maps of width D / 2 each, bf16
 struct DiffShape {
@@ -449,7 +467,35 @@ hipError_t launch_head_norm_bwd(const NormShape& m, int dtype, int T, const void
                                 const float* gain, const void* dy, void* dx, float* dgain,
                                 int accumulate, void* ws, hipStream_t st);
 
-// The block's attention with these (rope null: not turned)
+// The block's attention over packed sequences (rope null: not turned)
+size_t packed_mha_ws_bytes(const PackedShape& m, int T);
+hipError_t launch_packed_mha_fwd(const PackedShape& m, const RopeShape* r, int T,
+                                 const flowmoe_packed_mha_bufs_t& b, hipStream_t st);
+hipError_t launch_packed_mha_bwd(const PackedShape& m, const RopeShape* r, int T,
+                                 const flowmoe_packed_mha_bufs_t& b, int accumulate,
+                                 hipStream_t st);
+
+// Layer norm of T rows of M (at most kMaxNormM), with the residual's addition
+constexpr int kMaxNormM = 16384;
+size_t layer_norm_ws_bytes(int T, int M);
+hipError_t launch_layer_norm_fwd(int dtype, int T, int M, float eps, const void* x,
+                                 const void* res, const float* gain, const float* bias, void* sum,
+                                 void* y, hipStream_t st);
+hipError_t launch_layer_norm_bwd(int dtype, int T, int M, float eps, const void* x,
+                                 const float* gain, const void* dy, const void* d_sum, void* dx,
+                                 float* dgain, float* dbias, int accumulate, void* ws,
+                                 hipStream_t st);
+
+// Embedding lookup in a table V x M, and its gradient
+bool embed_fits(int T, int M, int V);  // a grid holds the calls' blocks
+size_t embed_ws_bytes(int T, int M);
+hipError_t launch_embed_fwd(int dtype, int T, int M, int V, float scale, const int32_t* ids,
+                            const void* table, void* y, hipStream_t st);
+hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const int32_t* ids,
+                            const void* dy, float* dtable, int accumulate, void* ws,
+                            hipStream_t st);
+
+// The block's differential attention with rotary positions and head norm (rope null: not turned)
 size_t diff_mha_ws_bytes(const DiffShape& m, const NormShape& n, int T);
 hipError_t launch_diff_mha_fwd(const DiffShape& m, const RopeShape* r, const NormShape& n, int T,
                                const flowmoe_diff_mha_bufs_t& b, hipStream_t st);

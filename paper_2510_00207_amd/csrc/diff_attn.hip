@@ -1367,14 +1367,6 @@ hipError_t launch_diff_attn_bwd(const DiffShape& m, int T, const void* qkv, cons
 // ---------------------------------------------------------------------------
 // the block's attention: projections, positions, differential attention, head norm
 // ---------------------------------------------------------------------------
-namespace {
-// partial sums of a weight gradient (M x N) whose rows are split
-size_t wgrad_part_bytes(int M, int N, long rows) {
-  const int s = dense_wgrad_splits(M, N, rows);
-  return s > 1 ? (size_t)s * M * N * sizeof(float) : 0;
-}
-}  // namespace
-
 size_t diff_mha_ws_bytes(const DiffShape& m, const NormShape& n, int T) {
   const int M = m.heads * m.D, W = M + 2 * m.kv * m.D;
   return align256(std::max(std::max(diff_attn_ws_bytes(m, T), head_norm_ws_bytes(T, n.heads, n.D)),

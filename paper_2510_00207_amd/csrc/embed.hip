@@ -3,7 +3,7 @@
 // have no row: zeros forward, no gradient.
 //
 // Both are bound by HBM. The gradient needs a row's tokens side by side: a stable radix sort
-// of (id, t) by 8 bits a pass, then a wave walks the tokens of its table rows.
+// of (id, t) by 8 bits a pass, then sums of equally many tokens a wave.
 #include <algorithm>
 
 #include "common.hpp"
@@ -18,7 +18,7 @@ struct EmbedArgs {
   const void* dy;
   void* y;
   float* dtable;
-  float* part;  // sums of chunks of 64 sorted tokens of one id, or null
+  float* part;  // the runs' parts
   int T, M, V, rows;
   float scale;
 };
@@ -79,17 +79,21 @@ __global__ __launch_bounds__(1024) void embed_hist_kernel(SortArgs a) {
 // where this block's items of digit d go from (thread d < 256): the smaller digits' items
 // of all blocks, then d's of the blocks before; `tot` d's items of all blocks
 __device__ __forceinline__ void digit_bases(int* base, int tot, int before) {
-  // an exclusive scan of tot over 256 threads, through LDS
-  const int tid = threadIdx.x;
-  if (tid < 256) base[tid] = tot;
-  __syncthreads();
-  for (int o = 1; o < 256; o <<= 1) {
-    const int v = tid < 256 && tid >= o ? base[tid - o] : 0;
-    __syncthreads();
-    if (tid < 256) base[tid] += v;
-    __syncthreads();
+  // an exclusive scan of tot over the first four waves
+  __shared__ int sums[4];
+  const int tid = threadIdx.x, lane = tid & 63;
+  int run = tot;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(run, o);
+    if (lane >= o) run += v;
   }
-  if (tid < 256) base[tid] += before - tot;
+  if (tid < 256 && lane == 63) sums[tid >> 6] = run;
+  __syncthreads();
+  if (tid < 256) {
+    for (int k = 0; k < tid >> 6; ++k) run += sums[k];
+    base[tid] = run - tot + before;
+  }
   __syncthreads();
 }
 
@@ -136,7 +140,7 @@ __device__ __forceinline__ void place_items(const SortArgs& a, int i0, int i1, i
 __global__ __launch_bounds__(1024) void embed_place_kernel(SortArgs a) {
   __shared__ int base[256];
   __shared__ int cnt[16][256];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, i0 = blockIdx.x * a.per;
   int tot = 0, before = 0;
   if (tid < 256) {
 #pragma unroll 8
@@ -147,113 +151,97 @@ __global__ __launch_bounds__(1024) void embed_place_kernel(SortArgs a) {
     }
   }
   digit_bases(base, tot, before);
-  place_items(a, blockIdx.x * a.per, (int)min((long)a.T, ((long)blockIdx.x + 1) * a.per), base, cnt);
+  place_items(a, i0, (int)min((long)a.T, (long)i0 + a.per), base, cnt);
 }
 
-// every pass in one block, from `in` through x and y in turn; the last pass writes y
-__global__ __launch_bounds__(1024) void embed_sort_kernel(const int32_t* in, int32_t* x, int32_t* y,
-                                                          int T, int V, int passes) {
-  __shared__ int base[256];
-  __shared__ int cnt[16][256];
-  const int tid = threadIdx.x;
-  SortArgs a = {in, nullptr, nullptr, nullptr, nullptr, T, V, T, 0};
-  for (int p = 0; p < passes; ++p) {
-    int32_t* out = (passes - 1 - p) % 2 ? x : y;
-    a.key = out;
-    a.val = out + T;
-    a.shift = 8 * p;
-    if (tid < 256) cnt[0][tid] = 0;
-    __syncthreads();
-    for (int i = tid; i < T; i += 1024) atomicAdd(&cnt[0][(sort_key(a, i) >> a.shift) & 255], 1);
-    __syncthreads();
-    const int tot = tid < 256 ? cnt[0][tid] : 0;
-    digit_bases(base, tot, 0);
-    place_items(a, 0, T, base, cnt);
-    __threadfence_block();
-    __syncthreads();
-    a.key_in = out;
-    a.val_in = out + T;
+// Few tokens, in one launch: an item's place is the number of items that sort before it.
+// A block finds those of 64 items, a lane each; its 16 waves compare them with every 16th 64
+// of all items each.
+__global__ __launch_bounds__(1024) void embed_rank_kernel(const int32_t* ids, int32_t* key,
+                                                          int32_t* val, int T, int V) {
+  __shared__ int part[16][64];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int b0 = blockIdx.x * 64, i = b0 + lane;
+  // (an id of no row sorts as V, a place behind the items before all)
+  auto in = [&](int j) { return j < T ? (int)min((unsigned)ids[j], (unsigned)V) : 0x7FFFFFFF; };
+  const int k = in(i);
+  int n = 0;
+  for (int j = 64 * w; j < T; j += 1024) {
+    const int q = in(j + lane);
+    // (as one comparison: those before the block's sort before equal ones)
+    const int kk = j < b0 ? k : k - 1;
+#pragma unroll
+    for (int u = 0; u < 64; ++u) {
+      const int o = __builtin_amdgcn_readlane(q, u);
+      n += o <= kk;
+      if (j == b0) n += o == k && u < lane;
+    }
   }
+  part[w][lane] = n;
+  __syncthreads();
+  if (w != 0 || i >= T) return;
+  n = 0;
+#pragma unroll
+  for (int u = 0; u < 16; ++u) n += part[u][lane];
+  key[n] = k;
+  val[n] = i;
 }
 
 // ---- sums of rows -----------------------------------------------------------------------
-// 8 columns a lane from c on; `on`: the lane has columns
-struct Cols {
-  int c;
-  bool on;
-};
+// The sorted tokens in chunks of C, a wave a chunk and 512 columns (8 a lane): whatever runs
+// of one id it holds, a wave reads the same rows, eight in flight. A run inside a chunk is
+// written by its wave; of one that crosses chunks each leaves its part, and the join adds them
+// up in order. part: chunks x [a run that began before | a run that goes on] x M.
 
-__device__ __forceinline__ void add8(float acc[8], const float v[8], bool on) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] += on ? v[i] : 0.0f;
-}
-
-// acc += dy of the tokens that lanes i0 .. i1 - 1 hold, four rows in flight
-template <typename T>
-__device__ __forceinline__ void add_tokens(const EmbedArgs& a, Cols s, int tok, int i0, int i1,
-                                           float acc[8]) {
-  for (int k = i0; k < i1; k += 4) {
-    float v[4][8] = {};
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const long t = __builtin_amdgcn_readlane(tok, min(k + u, i1 - 1));
-      if (s.on) load8(static_cast<const T*>(a.dy) + t * a.M + s.c, v[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) add8(acc, v[u], k + u < i1);
-  }
-}
-
-// The sorted tokens 64 at a time: ids and tokens of window `wb`, a lane each (past the last:
-// no id's)
-struct Window {
-  int wb, id, tok;
-  __device__ __forceinline__ void load(const EmbedArgs& a, int base, int lane) {
-    wb = base;
-    const bool there = base + lane < a.T;
-    id = there ? a.ids[base + lane] : 0x7FFFFFFF;
-    tok = there ? a.tok[base + lane] : 0;
-  }
-};
-
-// acc = the sum of id v's tokens, the first of which is at or past pos (in window w); pos is
-// then behind the last
-template <typename T>
-__device__ __forceinline__ void sum_id(const EmbedArgs& a, Cols s, int lane, int v, int& pos,
-                                       Window& w, float acc[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
-  for (;;) {
-    const unsigned long m = __ballot(w.id == v && w.wb + lane >= pos);
-    const int n = __popcll(m), i0 = pos - w.wb;
-    if (n == 64 && a.part != nullptr) {
-      float t[8] = {};
-      if (s.on) load8(a.part + (long)(w.wb / 64) * a.M + s.c, t);
-      add8(acc, t, true);
-    } else {
-      add_tokens<T>(a, s, w.tok, i0, i0 + n, acc);
-    }
-    pos += n;
-    if (i0 + n < 64) return;
-    w.load(a, w.wb + 64, lane);
-  }
-}
-
-// the sums of the chunks of 64 sorted tokens that are one id's, a wave a chunk and 512 columns
-template <typename T>
-__global__ __launch_bounds__(256) void embed_chunk_kernel(EmbedArgs a) {
-  const int lane = threadIdx.x & 63, slabs = (a.M + 511) / 512;
-  const long u = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int ch = (int)(u / slabs), c = (int)(u % slabs) * 512 + 8 * lane;
-  if (ch >= a.T / 64) return;
-  const int first = a.ids[ch * 64];
-  if (first >= a.V || first != a.ids[ch * 64 + 63]) return;
-  Window w;
-  w.load(a, ch * 64, lane);
+template <typename T, int C, bool ADD, bool NT>
+__device__ __forceinline__ void sum_chunk(const EmbedArgs& a, int ch, int c, int lane) {
+  constexpr int B = ADD ? 4 : 8;  // rows in flight (ADD: and what they are added to)
+  const bool on = c < a.M;
+  // lane l has position ch * C + l - 1: one before the chunk, the chunk, one behind it
+  const int p = ch * C + lane - 1;
+  const bool there = p >= 0 && p < a.T && lane < C + 2;
+  const int id = there ? a.ids[p] : p < 0 ? -1 : 0x7FFFFFFF, tok = there ? a.tok[p] : 0;
+  const int before = __shfl_up(id, 1);
+  const bool mine = lane >= 1 && lane <= C && id < a.V;
+  const int n = __popcll(__ballot(mine));
+  // bit k: token k begins, ends a run (the last one: or its part of one)
+  const unsigned head = (unsigned)(__ballot(mine && id != before) >> 1);
+  const unsigned end = (head >> 1) | (n > 0 ? 1u << (n - 1) : 0u);
+  const bool goes_on = n == C && __builtin_amdgcn_readlane(id, C + 1) ==
+                                          __builtin_amdgcn_readlane(id, C);
   float acc[8] = {};
-  const Cols s = {c, c < a.M};
-  add_tokens<T>(a, s, w.tok, 0, 64, acc);
-  if (s.on) store8(a.part + (long)ch * a.M + c, acc);
+  for (int k = 0; k < n; k += B) {
+    float v[B][8] = {}, old[ADD ? B : 1][8] = {};
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const int i = min(k + u, n - 1);
+      const long t = __builtin_amdgcn_readlane(tok, i + 1);
+      if (on) load8(static_cast<const T*>(a.dy) + t * a.M + c, v[u]);
+      if constexpr (ADD) {
+        const long r = __builtin_amdgcn_readlane(id, i + 1);
+        if (on && (end >> i & 1)) load8(a.dtable + r * a.M + c, old[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const int i = k + u;
+      if (i >= n) break;
+      const bool first = head >> i & 1;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = (first ? 0.0f : acc[e]) + v[u][e];
+      if (!(end >> i & 1) || !on) continue;
+      const bool began = (head & ((2u << i) - 1)) == 0, open = i == n - 1 && goes_on;
+      if (began || open) {
+        store8(a.part + (2L * ch + (began ? 0 : 1)) * a.M + c, acc);
+      } else {
+        const long r = __builtin_amdgcn_readlane(id, i + 1);
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = ADD ? old[ADD ? u : 0][e] + a.scale * acc[e] : a.scale * acc[e];
+        store8_t<NT>(a.dtable + r * a.M + c, o);
+      }
+    }
+  }
 }
 
 // the first sorted position whose id is at least v, a wave's search of 64 at a time
@@ -269,71 +257,108 @@ __device__ __forceinline__ int first_of(const EmbedArgs& a, int v, int lane) {
   return lo;
 }
 
-// The whole table: a wave has `rows` rows of it, 512 columns
-template <typename T, bool NT>
+// zeros in the rows v0 .. v0 + rows - 1 (at most 64) that have no tokens
+template <bool NT>
+__device__ __forceinline__ void zero_absent(const EmbedArgs& a, long v0, int lane) {
+  const int v1 = (int)min((long)a.V, v0 + a.rows), v = (int)v0 + lane;
+  int lo = first_of(a, (int)v0, lane);
+  bool absent = v < v1;
+  const int q = lo + lane < a.T ? a.ids[lo + lane] : 0x7FFFFFFF;
+  if (__builtin_amdgcn_readlane(q, 63) >= v1) {  // the rows' tokens are at most these
+    for (int u = 0; u < 64; ++u) {
+      const int o = __builtin_amdgcn_readlane(q, u);
+      if (o >= v1) break;
+      absent = absent && o != v;
+    }
+  } else {  // each lane searches its own row's first
+    const int end = first_of(a, v1, lane);
+    int hi = end;
+    while (__any(lo < hi)) {
+      const int mid = (lo + hi) >> 1;
+      const bool less = lo < hi && a.ids[mid] < v;
+      if (lo < hi) {
+        if (less) lo = mid + 1;
+        else hi = mid;
+      }
+    }
+    absent = absent && !(lo < end && a.ids[lo] == v);
+  }
+  unsigned long m = __ballot(absent);
+  while (m) {
+    const long r = v0 + __builtin_ctzll(m);
+    m &= m - 1;
+#pragma unroll 4
+    for (int c = 4 * lane; c < a.M; c += 256)
+      st16<NT>(reinterpret_cast<u32x4v_t*>(a.dtable + r * a.M + c), u32x4v_t{0, 0, 0, 0});
+  }
+}
+
+// waves 0 .. chunks * slabs - 1: the chunks; the others: the rows without tokens
+template <typename T, int C, bool ADD, bool NT>
 __global__ __launch_bounds__(256) void embed_bwd_kernel(EmbedArgs a) {
   const int lane = threadIdx.x & 63, slabs = (a.M + 511) / 512;
   const long u = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = (int)(u % slabs) * 512 + 8 * lane;
-  const long v0 = u / slabs * a.rows;
-  if (v0 >= a.V) return;
-  const int v1 = (int)min((long)a.V, v0 + a.rows);
-  const Cols s = {c, c < a.M};
-  int pos = first_of(a, (int)v0, lane);
-  Window w;
-  w.load(a, pos & ~63, lane);
-  for (int v = (int)v0; v < v1; ++v) {
-    float acc[8];
-    sum_id<T>(a, s, lane, v, pos, w, acc);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] *= a.scale;
-    if (s.on) store8_t<NT>(a.dtable + (long)v * a.M + c, acc);
+  const long sums = ((long)a.T + C - 1) / C * slabs;
+  if (u < sums) {
+    sum_chunk<T, C, ADD, NT>(a, (int)(u / slabs), (int)(u % slabs) * 512 + 8 * lane, lane);
+  } else if constexpr (!ADD) {
+    const long v0 = (u - sums) * a.rows;
+    if (v0 < a.V) zero_absent<NT>(a, v0, lane);
   }
 }
 
-// Added to the rows that have tokens: a wave has `rows` sorted positions (a divisor of 64),
-// and of them the ids that begin there
-template <typename T>
-__global__ __launch_bounds__(256) void embed_bwd_add_kernel(EmbedArgs a) {
+// runs that cross chunks: the wave of the chunk where one begins adds up its parts
+template <int C, bool ADD>
+__global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a) {
   const int lane = threadIdx.x & 63, slabs = (a.M + 511) / 512;
   const long u = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = (int)(u % slabs) * 512 + 8 * lane;
-  const long p0 = u / slabs * a.rows;
-  if (p0 >= a.T) return;
-  const int p1 = (int)min((long)a.T, p0 + a.rows);
-  const Cols s = {c, c < a.M};
-  int pos = (int)p0;
-  Window w;
-  w.load(a, pos & ~63, lane);
-  if (pos > 0) {  // an id that began before
-    const int v = a.ids[pos - 1];
-    const unsigned long m = __ballot(w.id == v && w.wb + lane >= pos);
-    pos += __popcll(m);  // (past the window: its last position is past p1 as well)
-  }
-  while (pos < p1) {
-    const int v = __builtin_amdgcn_readlane(w.id, pos - w.wb);
-    if (v >= a.V) return;
-    float* d = a.dtable + (long)v * a.M + c;
-    float acc[8], old[8] = {};
-    if (s.on) load8(d, old);
-    sum_id<T>(a, s, lane, v, pos, w, acc);
+  const int ch = (int)(u / slabs), c = (int)(u % slabs) * 512 + 8 * lane;
+  const long p = (long)ch * C;
+  if (p + C >= a.T) return;
+  const int id = a.ids[p + C - 1];
+  if (id >= a.V || a.ids[p + C] != id) return;
+  if (a.ids[p] == id && p > 0 && a.ids[p - 1] == id) return;  // began before
+  const bool on = c < a.M;
+  float acc[8] = {}, old[8] = {};
+  if (on) load8(a.part + (2L * ch + 1) * a.M + c, acc);
+  if (ADD && on) load8(a.dtable + (long)id * a.M + c, old);
+  for (int j = ch + 1;; j += 64) {
+    const long q = (long)(j + lane) * C;
+    const int n = __popcll(__ballot(q < a.T && a.ids[q] == id));
+    for (int k = 0; k < n; k += 16) {
+      float v[16][8] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = old[i] + a.scale * acc[i];
-    if (s.on) store8(d, acc);
+      for (int e = 0; e < 16; ++e)
+        if (on) load8(a.part + 2L * (j + min(k + e, n - 1)) * a.M + c, v[e]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (k + e < n)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] += v[e][i];
+    }
+    if (n < 64) break;
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] = ADD ? old[i] + a.scale * acc[i] : a.scale * acc[i];
+  if (on) store8(a.dtable + (long)id * a.M + c, acc);
 }
 
 // ---- host -------------------------------------------------------------------------------
+constexpr int kFew = 8192;
 int key_passes(int V) {  // keys 0 .. V
   int p = 1;
   while (p < 4 && ((unsigned)V >> (8 * p)) != 0) ++p;
   return p;
 }
-// a block sorts up to 4096 items alone
-constexpr int kSortOne = 4096;
-int sort_per(int T) {
-  return T <= kSortOne ? T : std::max(1, (int)(((long)T + 262143) / 262144)) * 1024;
-}
+// Tokens a chunk: few tokens are better served by more waves, many by fewer parts of runs. us
+// with 8 and 32: 1000 tokens of 1000 x 2048 in 5003 rows 20, 32; 4096 x 1024, 32000 rows 46,
+// 55; 16384 65, 69, all of one id 248, 114; 32768 x 2048, 50021 rows 169, 135.
+int embed_chunk(int T) { return T <= kFew ? 8 : 32; }
+
+// The most items that are ranked: us of the whole gradient ranked and sorted: 1000 tokens 21,
+// 28; 4096 46, 44; 8192 63, 50.
+constexpr int kRank = 2048;
+int sort_per(int T) { return std::max(1, (int)(((long)T + 262143) / 262144)) * 1024; }
 int sort_blocks(int T) { return (int)(((long)T + sort_per(T) - 1) / sort_per(T)); }
 
 struct EmbedWs {
@@ -345,8 +370,8 @@ EmbedWs embed_ws(int T, int M) {
   w.a = 0;
   w.b = items;
   w.hist = 2 * items;
-  w.part = w.hist + align256(T <= kSortOne ? 0 : (size_t)sort_blocks(T) * 1024);
-  w.bytes = w.part + align256((size_t)(T / 64) * M * sizeof(float));
+  w.part = w.hist + align256(T <= kRank ? 0 : (size_t)sort_blocks(T) * 1024);
+  w.bytes = w.part + align256(((size_t)T + embed_chunk(T) - 1) / embed_chunk(T) * 2 * M * sizeof(float));
   return w;
 }
 
@@ -354,9 +379,9 @@ hipError_t sort_tokens(int T, int V, const int32_t* ids, const EmbedWs& w, char*
   const int passes = key_passes(V);
   int32_t* x = reinterpret_cast<int32_t*>(ws + w.b);
   int32_t* y = reinterpret_cast<int32_t*>(ws + w.a);
-  if (T <= kSortOne)
+  if (T <= kRank)
     return traced(FLOWMOE_K_EMBED_SORT, st, [&] {
-      hipLaunchKernelGGL(embed_sort_kernel, dim3(1), dim3(1024), 0, st, ids, x, y, T, V, passes);
+      hipLaunchKernelGGL(embed_rank_kernel, dim3((T + 63) / 64), dim3(1024), 0, st, ids, y, y + T, T, V);
     });
   SortArgs a = {ids, nullptr, nullptr, nullptr, reinterpret_cast<int32_t*>(ws + w.hist), T, V,
                 sort_per(T), 0};
@@ -385,14 +410,17 @@ int embed_lanes(int M) {
 
 }  // namespace
 
-// rows of the table that a wave of the gradient has
-static int embed_rows(int M) { return M >= 512 ? 8 : 16; }
-static constexpr int kAddRows = 8;
+// rows of the table that a wave looks at for those without tokens
+static int embed_rows(int M) { return M >= 512 ? 16 : 64; }
+static long embed_waves(int T, int M, int V, bool add) {
+  const long slabs = (M + 511) / 512;
+  return ((long)T + embed_chunk(T) - 1) / embed_chunk(T) * slabs +
+         (add ? 0 : (V + embed_rows(M) - 1L) / embed_rows(M));
+}
 
 bool embed_fits(int T, int M, int V) {
-  const long slabs = (M + 511) / 512, f = 4 * (256 / embed_lanes(M));
-  const long n = std::max(((V + embed_rows(M) - 1L) / embed_rows(M)), (T + kAddRows - 1L) / kAddRows);
-  return (T + f - 1) / f <= kMaxBlocks && (n * slabs + 3) / 4 <= kMaxBlocks;
+  const long f = 4 * (256 / embed_lanes(M));
+  return (T + f - 1) / f <= kMaxBlocks && (embed_waves(T, M, V, false) + 3) / 4 <= kMaxBlocks;
 }
 
 size_t embed_ws_bytes(int T, int M) { return T == 0 ? 0 : embed_ws(T, M).bytes; }
@@ -436,7 +464,6 @@ hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const i
   if (T == 0 && accumulate) return hipSuccess;
   const EmbedWs w = embed_ws(T, M);
   char* base = static_cast<char*>(ws);
-  const long slabs = (M + 511) / 512;
   EmbedArgs a = {};
   a.dy = dy;
   a.dtable = dtable;
@@ -449,31 +476,34 @@ hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const i
     if (e != hipSuccess) return e;
     a.ids = reinterpret_cast<const int32_t*>(base + w.a);
     a.tok = a.ids + T;
-    if (T >= 256) {
-      a.part = reinterpret_cast<float*>(base + w.part);
-      const dim3 g((unsigned)((T / 64 * slabs + 3) / 4)), b(256);
-      const hipError_t e2 = traced(FLOWMOE_K_EMBED_BWD, st, [&] {
-        if (dtype == FLOWMOE_BF16) hipLaunchKernelGGL(embed_chunk_kernel<bf16_t>, g, b, 0, st, a);
-        else hipLaunchKernelGGL(embed_chunk_kernel<float>, g, b, 0, st, a);
-      });
-      if (e2 != hipSuccess) return e2;
-    }
+    a.part = reinterpret_cast<float*>(base + w.part);
   }
-  a.rows = accumulate ? kAddRows : embed_rows(M);
-  const long n = ((accumulate ? T : V) + (long)a.rows - 1) / a.rows;
-  const dim3 g((unsigned)((n * slabs + 3) / 4)), b(256);
+  a.rows = embed_rows(M);
+  const dim3 g((unsigned)((embed_waves(T, M, V, accumulate) + 3) / 4)), b(256);
   const bool nt = (long)V * M * 4 >= (256L << 20);
-  return traced(FLOWMOE_K_EMBED_BWD, st, [&] {
-    if (accumulate) {
-      if (dtype == FLOWMOE_BF16) hipLaunchKernelGGL(embed_bwd_add_kernel<bf16_t>, g, b, 0, st, a);
-      else hipLaunchKernelGGL(embed_bwd_add_kernel<float>, g, b, 0, st, a);
+  const bool few = embed_chunk(T) == 8;
+  const hipError_t e = traced(FLOWMOE_K_EMBED_BWD, st, [&] {
+#define FLOWMOE_EMBED_BWD(T, C)                                                                 \
+  if (accumulate) hipLaunchKernelGGL((embed_bwd_kernel<T, C, true, false>), g, b, 0, st, a);    \
+  else if (nt) hipLaunchKernelGGL((embed_bwd_kernel<T, C, false, true>), g, b, 0, st, a);       \
+  else hipLaunchKernelGGL((embed_bwd_kernel<T, C, false, false>), g, b, 0, st, a)
+    if (few && dtype == FLOWMOE_BF16) {
+      FLOWMOE_EMBED_BWD(bf16_t, 8);
+    } else if (few) {
+      FLOWMOE_EMBED_BWD(float, 8);
     } else if (dtype == FLOWMOE_BF16) {
-      if (nt) hipLaunchKernelGGL((embed_bwd_kernel<bf16_t, true>), g, b, 0, st, a);
-      else hipLaunchKernelGGL((embed_bwd_kernel<bf16_t, false>), g, b, 0, st, a);
+      FLOWMOE_EMBED_BWD(bf16_t, 32);
     } else {
-      if (nt) hipLaunchKernelGGL((embed_bwd_kernel<float, true>), g, b, 0, st, a);
-      else hipLaunchKernelGGL((embed_bwd_kernel<float, false>), g, b, 0, st, a);
+      FLOWMOE_EMBED_BWD(float, 32);
     }
+  });
+  if (e != hipSuccess || T <= embed_chunk(T)) return e;
+  return traced(FLOWMOE_K_EMBED_BWD, st, [&] {
+    const dim3 gj((unsigned)((embed_waves(T, M, V, true) + 3) / 4));
+    if (few && accumulate) hipLaunchKernelGGL((embed_join_kernel<8, true>), gj, b, 0, st, a);
+    else if (few) hipLaunchKernelGGL((embed_join_kernel<8, false>), gj, b, 0, st, a);
+    else if (accumulate) hipLaunchKernelGGL((embed_join_kernel<32, true>), gj, b, 0, st, a);
+    else hipLaunchKernelGGL((embed_join_kernel<32, false>), gj, b, 0, st, a);
   });
 }
 

@@ -1301,7 +1301,7 @@ flowmoe_status_t flowmoe_layer_norm_fwd(const flowmoe_shape_t* shape, float eps,
 
 size_t flowmoe_layer_norm_ws_bytes(const flowmoe_shape_t* shape) {
   if (check_layer_norm(shape, 1.0f) != FLOWMOE_OK) return 0;
-  return layer_norm_ws_bytes(shape->T, shape->M);
+  return layer_norm_ws_bytes(shape->T, shape->M, shape->dtype);
 }
 
 flowmoe_status_t flowmoe_layer_norm_bwd(const flowmoe_shape_t* shape, float eps, const void* x,
@@ -1320,7 +1320,7 @@ flowmoe_status_t flowmoe_layer_norm_bwd(const flowmoe_shape_t* shape, float eps,
   CHECK_A4(dgain, "dgain");
   CHECK_A4(dbias, "dbias");
   if (dgain != nullptr || dbias != nullptr) {
-    const size_t need = layer_norm_ws_bytes(shape->T, shape->M);
+    const size_t need = layer_norm_ws_bytes(shape->T, shape->M, shape->dtype);
     st = check_ws(ws, ws_bytes, need, "flowmoe_layer_norm_bwd");
     if (st != FLOWMOE_OK) return st;
     if (need > 0) REQUIRE_T(ws, "ws");

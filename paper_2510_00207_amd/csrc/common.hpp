@@ -477,7 +477,7 @@ hipError_t launch_packed_mha_bwd(const PackedShape& m, const RopeShape* r, int T
 
 // Layer norm of T rows of M (at most kMaxNormM), with the residual's addition
 constexpr int kMaxNormM = 16384;
-size_t layer_norm_ws_bytes(int T, int M);
+size_t layer_norm_ws_bytes(int T, int M, int dtype);
 hipError_t launch_layer_norm_fwd(int dtype, int T, int M, float eps, const void* x,
                                  const void* res, const float* gain, const float* bias, void* sum,
                                  void* y, hipStream_t st);

@@ -34,39 +34,54 @@ struct LnArgs {
   int accumulate;
 };
 
-__device__ __forceinline__ float wave_sum(float v) {
+// the sum over the L lanes of a row (its part)
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
 
-// rows a block works on side by side, and its threads
-template <int W>
-constexpr int kRows = W < 4 ? 4 / W : 1;
-template <int W>
-constexpr int kThreads = W < 4 ? 256 : 64 * W;
+// a row's vectors as stored, loaded a row ahead of their use
+template <typename T>
+using Raw8 = decltype(raw8_load(static_cast<const T*>(nullptr)));
+template <typename T, int V>
+__device__ __forceinline__ void load_row(Raw8<T> (&q)[V], const void* x, long r, bool row, int M,
+                                         const int (&c)[V], const bool (&in)[V]) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    q[v] = Raw8<T>{};
+    if (row && in[v]) q[v] = raw8_load(static_cast<const T*>(x) + r * M + c[v]);
+  }
+}
 
-// elements of a row in wave w of its W waves, V vectors a thread
-template <int W, int V>
-__device__ __forceinline__ int wave_count(int M, int w) {
+// threads of a block, and the rows it works on side by side
+template <int L, int W>
+constexpr int kThreads = W < 4 ? 256 : 64 * W;
+template <int L, int W>
+constexpr int kRows = kThreads<L, W> / (L * W);
+
+// elements of a row in part w of its W waves (of L lanes), V vectors a thread
+template <int L, int W, int V>
+__device__ __forceinline__ int part_count(int M, int w) {
   int n = 0;
 #pragma unroll
-  for (int v = 0; v < V; ++v) n += min(max(M - 512 * (w + W * v), 0), 512);
+  for (int v = 0; v < V; ++v) n += min(max(M - 8 * L * (w + W * v), 0), 8 * L);
   return n;
 }
 
-template <typename T, int W, int V, bool NT>
-__global__ __launch_bounds__(kThreads<W>) void layer_norm_kernel(LnArgs a) {
-  constexpr int G = kRows<W>;
-  __shared__ float red[2][G * W][2];
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6),
-            w = wv % W, g = wv / W;
+template <typename T, int L, int W, int V, bool NT>
+__global__ __launch_bounds__((kThreads<L, W>)) void layer_norm_kernel(LnArgs a) {
+  constexpr int G = kRows<L, W>;
+  __shared__ float red[2][W > 1 ? G * W : 1][2];
+  const int lane = threadIdx.x % L, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6),
+            w = W > 1 ? wv % W : 0, g = W > 1 ? wv / W : threadIdx.x / L;
   int c[V];
   bool in[V];
   float gn[V][8], bs[V][8];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    c[v] = 8 * (lane + 64 * (w + W * v));
+    c[v] = 8 * (lane + L * (w + W * v));
     in[v] = c[v] < a.M;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -74,28 +89,34 @@ __global__ __launch_bounds__(kThreads<W>) void layer_norm_kernel(LnArgs a) {
       bs[v][i] = in[v] && a.bias ? a.bias[c[v] + i] : 0.0f;
     }
   }
-  const int nw = wave_count<W, V>(a.M, w);
+  const int nw = part_count<L, W, V>(a.M, w);
   const float rn = nw > 0 ? 1.0f / nw : 0.0f;
   int ph = 0;
-  for (long r0 = (long)blockIdx.x * G; r0 < a.rows; r0 += (long)gridDim.x * G, ph ^= 1) {
+  const long step = (long)gridDim.x * G;
+  Raw8<T> qx[V], qr[V];
+  load_row<T>(qx, a.x, (long)blockIdx.x * G + g, (long)blockIdx.x * G + g < a.rows, a.M, c, in);
+  load_row<T>(qr, a.res, (long)blockIdx.x * G + g,
+              a.res && (long)blockIdx.x * G + g < a.rows, a.M, c, in);
+  for (long r0 = (long)blockIdx.x * G; r0 < a.rows; r0 += step, ph ^= 1) {
     const long r = r0 + g;
-    const bool row = r < a.rows;
-    float h[V][8], s = 0.0f;
+    const bool row = r < a.rows, next = r + step < a.rows;
+    float h[V][8], t[V][8], s = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const bool on = row && in[v];
-      float t[8] = {};
+      raw8_f32(qx[v], h[v]);
+      raw8_f32(qr[v], t[v]);
+    }
+    load_row<T>(qx, a.x, r + step, next, a.M, c, in);
+    load_row<T>(qr, a.res, r + step, a.res && next, a.M, c, in);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[v][i] = 0.0f;
-      if (on) load8(static_cast<const T*>(a.x) + r * a.M + c[v], h[v]);
-      if (on && a.res) load8(static_cast<const T*>(a.res) + r * a.M + c[v], t);
+    for (int v = 0; v < V; ++v) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        h[v][i] += t[i];
+        h[v][i] += t[v][i];
         s += h[v][i];
       }
     }
-    float mu = wave_sum(s) * rn, m2 = 0.0f;
+    float mu = lanes_sum<L>(s) * rn, m2 = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -103,23 +124,18 @@ __global__ __launch_bounds__(kThreads<W>) void layer_norm_kernel(LnArgs a) {
         const float d = in[v] ? h[v][i] - mu : 0.0f;
         m2 += d * d;
       }
-    m2 = wave_sum(m2);
+    m2 = lanes_sum<L>(m2);
     if constexpr (W > 1) {
       if (lane == 0) {
         red[ph][wv][0] = mu;
         red[ph][wv][1] = m2;
       }
       __syncthreads();
-      float t = 0.0f;
-#pragma unroll
-      for (int k = 0; k < W; ++k) t += wave_count<W, V>(a.M, k) * red[ph][g * W + k][0];
-      mu = t * a.rm;
-      m2 = 0.0f;
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        const float d = red[ph][g * W + k][0] - mu;
-        m2 += red[ph][g * W + k][1] + wave_count<W, V>(a.M, k) * d * d;
-      }
+      // (a lane a part)
+      const int k = lane % W, nk = part_count<L, W, V>(a.M, k);
+      const float* p = red[ph][g * W + k];
+      mu = lanes_sum<W>(nk * p[0]) * a.rm;
+      m2 = lanes_sum<W>(p[1] + nk * (p[0] - mu) * (p[0] - mu));
     }
     const float rs = rsqrtf(m2 * a.rm + a.eps);
 #pragma unroll
@@ -133,57 +149,78 @@ __global__ __launch_bounds__(kThreads<W>) void layer_norm_kernel(LnArgs a) {
   }
 }
 
-template <typename T, int W, int V, bool NT>
-__global__ __launch_bounds__(kThreads<W>) void layer_norm_bwd_kernel(LnArgs a) {
-  constexpr int G = kRows<W>, NTH = kThreads<W>;
-  __shared__ float red[2][G * W][4];
-  __shared__ float cols[G > 1 ? 2 * 512 * W * V : 1];
-  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6),
-            w = wv % W, g = wv / W;
+template <typename T, int L, int W, int V, bool NT>
+__global__ __launch_bounds__((kThreads<L, W>)) void layer_norm_bwd_kernel(LnArgs a) {
+  constexpr int G = kRows<L, W>;
+  __shared__ float red[2][W > 1 ? G * W : 1][4];
+  __shared__ float cols[G > 1 ? 2 * 8 * L * W * V : 1];
+  // (rows of 16 waves leave no registers for a row ahead, nor for the gains)
+  constexpr bool AHEAD = W < 16;
+  __shared__ __attribute__((aligned(16))) float gains[AHEAD ? 4 : 8 * L * W * V];
+  const int lane = threadIdx.x % L, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6),
+            w = W > 1 ? wv % W : 0, g = W > 1 ? wv / W : threadIdx.x / L;
   int c[V];
   bool in[V];
-  float gn[V][8], dg[V][8], db[V][8];
+  float gn[AHEAD ? V : 1][8], dg[V][8], db[V][8];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    c[v] = 8 * (lane + 64 * (w + W * v));
+    c[v] = 8 * (lane + L * (w + W * v));
     in[v] = c[v] < a.M;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      gn[v][i] = in[v] && a.gain ? a.gain[c[v] + i] : 1.0f;
+      const float gi = in[v] && a.gain ? a.gain[c[v] + i] : 1.0f;
+      if constexpr (AHEAD) gn[v][i] = gi;
+      else gains[c[v] + i] = gi;
       dg[v][i] = db[v][i] = 0.0f;
     }
   }
-  const int nw = wave_count<W, V>(a.M, w);
+  const int nw = part_count<L, W, V>(a.M, w);
   const float rn = nw > 0 ? 1.0f / nw : 0.0f;
   int ph = 0;
-  for (long r0 = (long)blockIdx.x * G; r0 < a.rows; r0 += (long)gridDim.x * G, ph ^= 1) {
+  const long step = (long)gridDim.x * G;
+  Raw8<T> qx[V], qd[V], qs[V];
+  if constexpr (AHEAD) {
+    const long r = (long)blockIdx.x * G + g;
+    load_row<T>(qx, a.x, r, r < a.rows, a.M, c, in);
+    load_row<T>(qd, a.dy, r, r < a.rows, a.M, c, in);
+    load_row<T>(qs, a.d_sum, r, a.d_sum && r < a.rows, a.M, c, in);
+  }
+  for (long r0 = (long)blockIdx.x * G; r0 < a.rows; r0 += step, ph ^= 1) {
     const long r = r0 + g;
-    const bool row = r < a.rows;
-    float h[V][8], d[V][8], s = 0.0f;
+    const bool row = r < a.rows, next = r + step < a.rows;
+    float h[V][8], d[V][8], t[V][8], s = 0.0f;
+    if constexpr (!AHEAD) {
+      load_row<T>(qx, a.x, r, row, a.M, c, in);
+      load_row<T>(qd, a.dy, r, row, a.M, c, in);
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[v][i] = d[v][i] = 0.0f;
-      if (row && in[v]) {
-        load8(static_cast<const T*>(a.x) + r * a.M + c[v], h[v]);
-        load8(static_cast<const T*>(a.dy) + r * a.M + c[v], d[v]);
-      }
+      raw8_f32(qx[v], h[v]);
+      raw8_f32(qd[v], d[v]);
+      if constexpr (AHEAD) raw8_f32(qs[v], t[v]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += h[v][i];
     }
-    float mu = wave_sum(s) * rn, m2 = 0.0f, su = 0.0f, sx = 0.0f;
+    if constexpr (AHEAD) {
+      load_row<T>(qx, a.x, r + step, next, a.M, c, in);
+      load_row<T>(qd, a.dy, r + step, next, a.M, c, in);
+      load_row<T>(qs, a.d_sum, r + step, a.d_sum && next, a.M, c, in);
+    } else {
+      load_row<T>(qs, a.d_sum, r, a.d_sum && row, a.M, c, in);
+    }
+    float mu = lanes_sum<L>(s) * rn, m2 = 0.0f, su = 0.0f, sx = 0.0f;
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float e = in[v] ? h[v][i] - mu : 0.0f, u = d[v][i] * gn[v][i];
+        const float e = in[v] ? h[v][i] - mu : 0.0f, u = d[v][i] * (AHEAD ? gn[AHEAD ? v : 0][i] : gains[c[v] + i]);
         m2 += e * e;
         su += u;
         sx += u * e;
       }
-    m2 = wave_sum(m2);
-    su = wave_sum(su);
-    sx = wave_sum(sx);
+    m2 = lanes_sum<L>(m2);
+    su = lanes_sum<L>(su);
+    sx = lanes_sum<L>(sx);
     if constexpr (W > 1) {
       if (lane == 0) {
         red[ph][wv][0] = mu;
@@ -192,35 +229,29 @@ __global__ __launch_bounds__(kThreads<W>) void layer_norm_bwd_kernel(LnArgs a) {
         red[ph][wv][3] = sx;
       }
       __syncthreads();
-      float t = 0.0f;
-#pragma unroll
-      for (int k = 0; k < W; ++k) t += wave_count<W, V>(a.M, k) * red[ph][g * W + k][0];
-      mu = t * a.rm;
-      m2 = su = sx = 0.0f;
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        const float* p = red[ph][g * W + k];
-        const float e = p[0] - mu;
-        m2 += p[1] + wave_count<W, V>(a.M, k) * e * e;
-        su += p[2];
-        sx += p[3] + e * p[2];  // u (h - mu) = u (h - mu_w) + u (mu_w - mu)
-      }
+      // (a lane a part)
+      const int k = lane % W, nk = part_count<L, W, V>(a.M, k);
+      const float* p = red[ph][g * W + k];
+      mu = lanes_sum<W>(nk * p[0]) * a.rm;
+      const float e = p[0] - mu;
+      m2 = lanes_sum<W>(p[1] + nk * e * e);
+      su = lanes_sum<W>(p[2]);
+      sx = lanes_sum<W>(p[3] + e * p[2]);  // u (h - mu) = u (h - mu_w) + u (mu_w - mu)
     }
     const float rs = rsqrtf(m2 * a.rm + a.eps);
     const float c1 = su * a.rm, c2 = sx * a.rm * rs;  // mean(u), mean(u n)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (!(row && in[v])) continue;
-      float t[8] = {};
-      if (a.d_sum) load8(static_cast<const T*>(a.d_sum) + r * a.M + c[v], t);
+      if constexpr (!AHEAD) raw8_f32(qs[v], t[v]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float n = (h[v][i] - mu) * rs, dd = d[v][i];
         dg[v][i] += dd * n;
         db[v][i] += dd;
-        t[i] += rs * (dd * gn[v][i] - c1 - n * c2);
+        t[v][i] += rs * (dd * (AHEAD ? gn[AHEAD ? v : 0][i] : gains[c[v] + i]) - c1 - n * c2);
       }
-      store8_t<NT>(static_cast<T*>(a.y) + r * a.M + c[v], t);
+      store8_t<NT>(static_cast<T*>(a.y) + r * a.M + c[v], t[v]);
     }
   }
   if (a.part == nullptr && a.dgain == nullptr && a.dbias == nullptr) return;
@@ -234,7 +265,7 @@ __global__ __launch_bounds__(kThreads<W>) void layer_norm_bwd_kernel(LnArgs a) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             cols[c[v] + i] = dg[v][i];
-            cols[512 * W * V + c[v] + i] = db[v][i];
+            cols[8 * L * W * V + c[v] + i] = db[v][i];
           }
       __syncthreads();
       if (g == 0)
@@ -243,7 +274,7 @@ __global__ __launch_bounds__(kThreads<W>) void layer_norm_bwd_kernel(LnArgs a) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             dg[v][i] += cols[c[v] + i];
-            db[v][i] += cols[512 * W * V + c[v] + i];
+            db[v][i] += cols[8 * L * W * V + c[v] + i];
           }
     }
     if (g != 0) return;
@@ -263,7 +294,6 @@ __global__ __launch_bounds__(kThreads<W>) void layer_norm_bwd_kernel(LnArgs a) {
       }
     }
   }
-  (void)NTH;
 }
 
 // dgain and dbias = (or +=) the sums of n partial rows [dgain | dbias]: blocks of 64
@@ -290,44 +320,53 @@ __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const float* part
   d[i] = accumulate ? d[i] + s : s;
 }
 
-// waves a row
+// lanes (of one wave) and waves a row
+int ln_lanes(int M) {
+  int l = 8;
+  while (l < 64 && 8 * l < M) l *= 2;
+  return l;
+}
 int ln_waves(int M) {
   int w = 1;
   while (1024 * w < M) w *= 2;
   return w;
 }
 
-int ln_blocks(long rows, int M, int most) {
-  const long per = std::max(4 / ln_waves(M), 1), need = (rows + per - 1) / per;
-  return (int)std::min(need, (long)most);
+int ln_blocks(long rows, int M, int es, int most) {
+  const int lw = ln_lanes(M) * ln_waves(M);
+  const long per = std::max(256 / lw, 1), need = (rows + per - 1) / per;
+  const long fill = std::min(std::max((4L << 20) / (per * M * es), 256L), (long)most);
+  return (int)std::min(need, fill);
 }
-int ln_bwd_blocks(long rows, int M) {
-  const int n = ln_blocks(rows, M, 512);
+int ln_bwd_blocks(long rows, int M, int es) {
+  const int n = ln_blocks(rows, M, es, 1024);
   return n <= 4 ? 1 : n;
 }
 
-#define FLOWMOE_LN_CASE(KERNEL, T, W, V)                                                        \
-  if (nt) hipLaunchKernelGGL((KERNEL<T, W, V, true>), dim3(n), dim3(kThreads<W>), 0, st, a);    \
-  else hipLaunchKernelGGL((KERNEL<T, W, V, false>), dim3(n), dim3(kThreads<W>), 0, st, a);      \
-  break
-#define FLOWMOE_LN_LAUNCH(KERNEL, T)                                \
-  switch (ln_waves(a.M)) {                                          \
-    case 1:                                                         \
-      if (a.M <= 512) {                                             \
-        FLOWMOE_LN_CASE(KERNEL, T, 1, 1);                           \
-      } else {                                                      \
-        FLOWMOE_LN_CASE(KERNEL, T, 1, 2);                           \
-      }                                                             \
-    case 2: FLOWMOE_LN_CASE(KERNEL, T, 2, 2);                       \
-    case 4: FLOWMOE_LN_CASE(KERNEL, T, 4, 2);                       \
-    case 8: FLOWMOE_LN_CASE(KERNEL, T, 8, 2);                       \
-    default: FLOWMOE_LN_CASE(KERNEL, T, 16, 2);                     \
+#define FLOWMOE_LN_CASE(KERNEL, T, L, W, V)                                                    \
+  {                                                                                            \
+    const dim3 g(n), b(kThreads<L, W>);                                                        \
+    if (nt) hipLaunchKernelGGL((KERNEL<T, L, W, V, true>), g, b, 0, st, a);                    \
+    else hipLaunchKernelGGL((KERNEL<T, L, W, V, false>), g, b, 0, st, a);                      \
+    break;                                                                                     \
+  }
+#define FLOWMOE_LN_LAUNCH(KERNEL, T)                                        \
+  switch (a.M <= 512 ? -ln_lanes(a.M) : ln_waves(a.M)) {                    \
+    case -8: FLOWMOE_LN_CASE(KERNEL, T, 8, 1, 1)                            \
+    case -16: FLOWMOE_LN_CASE(KERNEL, T, 16, 1, 1)                          \
+    case -32: FLOWMOE_LN_CASE(KERNEL, T, 32, 1, 1)                          \
+    case -64: FLOWMOE_LN_CASE(KERNEL, T, 64, 1, 1)                          \
+    case 1: FLOWMOE_LN_CASE(KERNEL, T, 64, 1, 2)                            \
+    case 2: FLOWMOE_LN_CASE(KERNEL, T, 64, 2, 2)                            \
+    case 4: FLOWMOE_LN_CASE(KERNEL, T, 64, 4, 2)                            \
+    case 8: FLOWMOE_LN_CASE(KERNEL, T, 64, 8, 2)                            \
+    default: FLOWMOE_LN_CASE(KERNEL, T, 64, 16, 2)                          \
   }
 
 }  // namespace
 
-size_t layer_norm_ws_bytes(int T, int M) {
-  const int n = ln_bwd_blocks(T, M);
+size_t layer_norm_ws_bytes(int T, int M, int dtype) {
+  const int n = ln_bwd_blocks(T, M, (int)esize(dtype));
   return T == 0 || n == 1 ? 0 : align256((size_t)n * 2 * M * sizeof(float));
 }
 
@@ -346,7 +385,7 @@ hipError_t launch_layer_norm_fwd(int dtype, int T, int M, float eps, const void*
   a.M = M;
   a.eps = eps;
   a.rm = 1.0f / M;
-  const int n = ln_blocks(T, M, 2048);
+  const int n = ln_blocks(T, M, (int)esize(dtype), 2048);
   const bool nt = (2 + (res != nullptr) + (sum != nullptr)) * (long)T * M * (long)esize(dtype) >= (256L << 20);
   return traced(FLOWMOE_K_LAYER_NORM, st, [&] {
     if (dtype == FLOWMOE_BF16) FLOWMOE_LN_LAUNCH(layer_norm_kernel, bf16_t)
@@ -371,7 +410,7 @@ hipError_t launch_layer_norm_bwd(int dtype, int T, int M, float eps, const void*
   a.accumulate = accumulate;
   const bool sums = dgain != nullptr || dbias != nullptr;
   // (without tokens they are sums of no partial rows)
-  const int n = T == 0 ? 0 : ln_bwd_blocks(T, M);
+  const int n = T == 0 ? 0 : ln_bwd_blocks(T, M, (int)esize(dtype));
   if (n == 1) {
     a.dgain = dgain;
     a.dbias = dbias;

@@ -31,6 +31,15 @@
 namespace flowmoe {
 namespace {
 
+// Units of the packed backward's long key tiles: a launch's steps are cut into about kUnits,
+// of at least kUnitSteps steps. us of the whole backward uncut and with 230, 460, 700, 1000
+// units: one sequence of 2031, 16 heads on 2 of 128, causal 696, 148, 149, 152, 150; one of
+// 16384, 8 on 1 6340, 2582, 2503, 2039, 2064; one of 4096, 16 on 16 342, 327, 322, 312, 331;
+// 16384 tokens in 12 of 46 to 8021, 32 on 8 2725, 2738, 2702, 2649, 2545, in 18 of 76 to 5801
+// 1809, 1843, 1728, 1644, 1653. With steps of at least 8, 16, 32: the first 148, 152, 142; 1000
+// tokens in 5, 8 on 2 of 64 30, 37, 47.
+constexpr int kUnits = 850, kUnitSteps = 16;
+
 struct AttnArgs {
   const bf16_t* qkv;  // T x 3M = [Q | K | V]; head h at columns h * D of each
   const bf16_t* o;    // T x M: the heads' outputs (backward)
@@ -48,6 +57,11 @@ struct AttnArgs {
   // that share kv key/value heads
   const int32_t* starts;
   int kv;
+  // backward: a key tile of more steps than a share of the launch (unit_steps) is cut into at
+  // most `units` units, whose sums go to part
+  float* part;
+  int units;
+  int rows32;  // 32-row tiles of all sequences (tile32)
 };
 
 // block -> (query or key tile, head, sequence). Blocks are dispatched in
@@ -86,44 +100,119 @@ __device__ __forceinline__ void decode(const AttnArgs& a, bool rev, bool shared,
 struct Span {
   long tok0, ld, k, v;
   int N, tile, hd;
+  int seq;    // packed: the sequence's index
   bool none;  // packed: no sequence's rows, whose outputs are zeros
 };
 
-// Packed sequences: tile t of sequence i has slot starts[i] / rows + i + t. Sequence i has
-// at most as many tiles as there are slots before sequence i + 1's, so that a block finds
-// its sequence by a search for its slot, without sums over the lengths, and a launch has
-// T / rows + nseq + 1 slots whatever the lengths are; those behind a sequence's last tile
-// stay empty (false). The rows behind the last sequence are a sequence of their own. The
-// search is a wave's: 64 starts at a time. Whatever `starts` holds, rows stay in 0 .. T.
+// Packed sequences, sequence i from row packed_start(i) on; the rows behind the last are a
+// sequence of their own. Whatever `starts` holds, rows stay in 0 .. T.
 __device__ __forceinline__ int packed_start(const AttnArgs& a, int i) {
   return i == 0 ? 0 : i > a.nseq ? a.T : min(max(a.starts[i], 0), a.T);
 }
-__device__ __forceinline__ bool locate(const AttnArgs& a, int slot, int rows, int lane, Span& s) {
-  int lo = 0, hi = a.nseq + 1;  // sequences lo .. hi - 1 may hold the slot, lo starts before it
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
-    const bool before = i < hi && packed_start(a, i) / rows + i <= slot;
-    const int n = max(1, (int)__popcll(__ballot(before)));
-    lo += (n - 1) * step;
-    hi = min(hi, lo + step);
+
+// The tile of `slot`, one of T / rows + nseq + 1 (false: none), by a wave, without sums over
+// all lengths stored anywhere.
+//
+// Up to 63 sequences: a lane each, and a scan of their tiles. More: tile t of sequence i has
+// slot packed_start(i) / rows + i + t, as many as there are before sequence i + 1's or
+// fewer, and a search finds the sequence, 64 at a time.
+__device__ __forceinline__ bool locate(const AttnArgs& a, int slot, int rows, bool rev, int lane,
+                                       Span& s) {
+  int i, r0, base;
+  if (a.nseq < 64) {
+    const int st = lane <= a.nseq ? packed_start(a, lane) : 0;
+    const int n = lane <= a.nseq ? packed_start(a, lane + 1) - st : 0;
+    const int nt = n > 0 ? (n + rows - 1) / rows : 0;
+    int before = nt;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(before, o);
+      if (lane >= o) before += v;
+    }
+    before -= nt;
+    const unsigned long m = __ballot(lane <= a.nseq && slot >= before && slot < before + nt);
+    if (m == 0) return false;
+    i = __builtin_ctzll(m);
+    r0 = __builtin_amdgcn_readlane(st, i);
+    s.N = __builtin_amdgcn_readlane(n, i);
+    base = __builtin_amdgcn_readlane(before, i);
+  } else {
+    int lo = 0, hi = a.nseq + 1;  // one of lo .. hi - 1 has the slot; lo's begin at or before it
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 63) / 64, k = lo + lane * step;
+      const bool before = k < hi && packed_start(a, k) / rows + k <= slot;
+      const int n = max(1, (int)__popcll(__ballot(before)));
+      lo += (n - 1) * step;
+      hi = min(hi, lo + step);
+    }
+    i = __builtin_amdgcn_readfirstlane(lo);
+    r0 = __builtin_amdgcn_readfirstlane(packed_start(a, i));
+    s.N = __builtin_amdgcn_readfirstlane(packed_start(a, i + 1)) - r0;
+    base = r0 / rows + i;
   }
-  const int i = __builtin_amdgcn_readfirstlane(lo);
-  const int r0 = __builtin_amdgcn_readfirstlane(packed_start(a, i));
+  s.seq = i;
   s.tok0 = r0;
-  s.N = __builtin_amdgcn_readfirstlane(packed_start(a, i + 1)) - r0;
-  s.tile = slot - r0 / rows - i;
   s.none = i == a.nseq;
-  return s.tile >= 0 && s.tile * (long)rows < s.N;
+  const int t = slot - base, nt = s.N > 0 ? (s.N + rows - 1) / rows : 0;
+  s.tile = rev ? nt - 1 - t : t;
+  return t >= 0 && t < nt;
 }
 
-// The packed grid: slots in descending order (a sequence's longest causal tiles first),
-// `per` heads of a slot side by side; where per is a multiple of 8, those of a group on
-// one XCD, through whose L2 they read their keys.
+// The packed grid: a slot's `per` heads side by side (where per is a multiple of 8, those of
+// a group on one XCD, through whose L2 they read their keys), each in `units` units; the
+// tiles of a sequence in descending order (`rev`).
 __device__ __forceinline__ bool packed_span(const AttnArgs& a, int per, bool rev, int rows,
-                                            int lane, Span& s) {
+                                            int units, int lane, Span& s, int& unit) {
   const int j = (int)(blockIdx.x % per), u = (int)(blockIdx.x / per);
   s.hd = per % 8 == 0 ? (j & 7) * (per >> 3) + (j >> 3) : j;
-  return locate(a, rev ? (int)(gridDim.x / per) - 1 - u : u, rows, lane, s);
+  const int slots = (int)(gridDim.x / per) / units;
+  unit = u / slots;
+  return locate(a, u - unit * slots, rows, rev, lane, s);
+}
+
+// Steps of a key tile of 128 rows in the backward, 32 queries a step: the group's heads one
+// after the other.
+__device__ __forceinline__ int key_steps(int N, int tile, int heads, bool causal) {
+  return heads * ((N - (causal ? 128 * tile : 0) + 31) / 32);
+}
+// The steps of a launch's unit, from the sum over its sequences, a lane each (a wave's 64 at
+// a time).
+__device__ __forceinline__ int unit_steps(const AttnArgs& a, bool causal, int lane) {
+  long sum = 0;
+  for (int i = lane; i < a.nseq; i += 64) {
+    const long n = max(packed_start(a, i + 1) - packed_start(a, i), 0), q = (n + 31) / 32,
+               nt = (n + 127) / 128;
+    sum += nt * q - (causal ? 2 * nt * (nt - 1) : 0);  // of q - 4 t over the tiles t
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  sum *= a.heads;  // (kv heads, of heads / kv query heads each)
+  // (uniform, and known to be: the loops' bounds come from it)
+  return __builtin_amdgcn_readfirstlane((int)max((long)kUnitSteps, min((sum + kUnits - 1) / kUnits, 1L << 30)));
+}
+// Units of a tile of `steps` steps (at most `most`), and the steps of each
+__device__ __forceinline__ int tile_units(int steps, int unit, int most, int& len) {
+  const int n = min(most, (steps + unit - 1) / unit);
+  len = n > 1 ? (steps + n - 1) / n : steps;
+  return n > 1 ? (steps + len - 1) / len : 1;  // (none of them empty)
+}
+
+// The sums of unit u of the 32-row tile t32 of a sequence, of a key head's K (kv = 0) or V:
+// 32 x D values as the lanes hold them, 16 bytes a lane side by side
+__device__ __forceinline__ float* unit_part(const AttnArgs& a, const Span& s, int u, int t32,
+                                            int g, int kv, int D) {
+  const long tile = s.tok0 / 32 + s.seq + t32;
+  return a.part + ((((long)u * a.rows32 + tile) * a.kv + g) * 2 + kv) * 32 * D;
+}
+template <int DB>
+__device__ __forceinline__ void store_part(float* p, const floatx16 (&x)[DB], int lane, float scale) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int J = 0; J < 4; ++J)
+      *reinterpret_cast<float4*>(p + ((db * 4 + J) * 64 + lane) * 4) =
+          make_float4(x[db][4 * J] * scale, x[db][4 * J + 1] * scale, x[db][4 * J + 2] * scale,
+                      x[db][4 * J + 3] * scale);
 }
 
 // zeros in `cols` columns of rows r0 .. r0 + n - 1 (16-byte vectors)
@@ -139,7 +228,8 @@ template <bool PACKED>
 __device__ __forceinline__ bool query_span(const AttnArgs& a, int D, bool causal, int rows,
                                            int lane, Span& s) {
   if constexpr (PACKED) {
-    const bool any = packed_span(a, a.heads, true, rows, lane, s);
+    int unit;
+    const bool any = packed_span(a, a.heads, causal, rows, 1, lane, s, unit);
     s.ld = (long)(a.heads + 2 * a.kv) * D;
     const int g = s.hd / (a.heads / a.kv);
     s.k = (long)(a.heads + g - s.hd) * D;
@@ -153,6 +243,7 @@ __device__ __forceinline__ bool query_span(const AttnArgs& a, int D, bool causal
     s.ld = 3L * a.M;
     s.k = a.M;
     s.v = 2L * a.M;
+    s.seq = 0;
     s.none = false;
     return true;
   }
@@ -679,8 +770,9 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
             h2 = lane >> 5, lq = lane & 31;
   Span sp;
   int nh = 1;  // query heads from hd on
+  int unit = 0, units = 1, it0 = 0, it1 = 0;  // the block's steps
   if constexpr (PACKED) {
-    const bool any = packed_span(a, a.kv, false, KB, lane, sp);
+    const bool any = packed_span(a, a.kv, false, KB, a.units, lane, sp, unit);
     if (!any) return;
     const int g = sp.hd;
     nh = a.heads / a.kv;
@@ -696,17 +788,28 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
     sp.ld = 3L * a.M;
     sp.k = a.M;
     sp.v = 2L * a.M;
+    sp.seq = 0;
     sp.none = false;
   }
   const long tok0 = sp.tok0, ld = sp.ld;
   const int hd = sp.hd, N = sp.N, k0 = sp.tile * KB, kw = k0 + 32 * w + lq;
   if constexpr (PACKED) {
     if (sp.none) {
+      if (unit > 0) return;
       const int n = min(KB, N - k0);
       zero_rows(a.d_qkv + hd * D + sp.k, ld, tok0 + k0, n, D, tid, 64 * NW);
       zero_rows(a.d_qkv + hd * D + sp.v, ld, tok0 + k0, n, D, tid, 64 * NW);
       return;
     }
+    const int steps = key_steps(N, sp.tile, nh, CAUSAL);
+    it1 = steps;
+    if (a.units > 1 && steps > kUnitSteps) {
+      int len;
+      units = tile_units(steps, unit_steps(a, CAUSAL, lane), a.units, len);
+      it0 = unit * len;
+      it1 = min(steps, it0 + len);
+    }
+    if (unit >= units) return;
   }
   const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
   const bf16_t* Gg = a.d_o + tok0 * a.M + (long)hd * D;
@@ -715,9 +818,11 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
   // query steps of 32: causal keys k0.. are seen by queries >= k0 only
   const int qs0 = CAUSAL ? k0 : 0;
   const int nqs = (N - qs0 + 31) / 32;
-  // packed: the group's query heads one after the other, nqs steps each
-  const int steps = PACKED ? nh * nqs : nqs;
-  int qi = 0;  // step of the head
+  // packed: the group's query heads one after the other, nqs steps each, of which the block
+  // has it0 .. it1 - 1, from step qi of head g0 on
+  const int steps = PACKED ? it1 - it0 : nqs;
+  const int g0 = PACKED ? it0 / nqs : 0;
+  int qi = PACKED ? it0 - g0 * nqs : 0;
 
   const Dma dma(lds_base(lds), w, lane, ld), dmag(lds_base(lds), w, lane, a.M);
 #pragma unroll
@@ -728,18 +833,19 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
   for (int ks = 0; ks < KS; ++ks)
     kf[ks] = live ? *reinterpret_cast<const bf16x8*>(Qg + sp.k + kw * ld + 16 * ks + 8 * h2) : zero8();
   float rstat = 0.0f;  // (the block's first 64 threads)
-  const float* sp_stat = (tid < 32 ? a.lse : a.delta) + srow0 + (tid & 31);
+  const float* sp_stat = (tid < 32 ? a.lse : a.delta) + srow0 + (PACKED ? (long)g0 * a.T : 0) + (tid & 31);
   auto load_stat = [&](int qb) {
     if (tid < 64) rstat = qb + (tid & 31) < N ? sp_stat[qb] * (tid < 32 ? kLog2e : 1.0f) : 0.0f;
   };
   auto store_stat = [&](int slot) {
     if (tid < 64) reinterpret_cast<float*>(lds + ST + 256 * slot)[tid] = rstat;
   };
-  const bf16_t* Qt = Qg + qs0 * ld;
-  const bf16_t* Gt = Gg + (long)qs0 * a.M;
-  dma.load(Qt, N - qs0, 0);
-  dmag.load(Gt, N - qs0, TQ);
-  load_stat(qs0);
+  const int qf0 = PACKED ? qs0 + 32 * qi : qs0;
+  const bf16_t* Qt = Qg + qf0 * ld + (PACKED ? g0 * D : 0);
+  const bf16_t* Gt = Gg + (long)qf0 * a.M + (PACKED ? g0 * D : 0);
+  dma.load(Qt, N - qf0, 0);
+  dmag.load(Gt, N - qf0, TQ);
+  load_stat(qf0);
   store_stat(0);
   floatx16 dv[DB], dk[DB];
 #pragma unroll
@@ -848,6 +954,15 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
     step(it, Stage<0>{});
     if (it + 1 < steps) step(it + 1, Stage<1>{});
   }
+  if constexpr (PACKED) {
+    if (units > 1) {
+      if (k0 + 32 * w < N) {
+        store_part<DB>(unit_part(a, sp, unit, sp.tile * NW + w, hd / nh, 0, D), dk, lane, a.rs);
+        store_part<DB>(unit_part(a, sp, unit, sp.tile * NW + w, hd / nh, 1, D), dv, lane, 1.0f);
+      }
+      return;
+    }
+  }
   if (live) {
     bf16_t* dst = a.d_qkv + (tok0 + kw) * ld + (long)hd * D;
 #pragma unroll
@@ -856,6 +971,50 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
       store_cols(dst + sp.v + 32 * db, dv[db], h2, 1.0f);
     }
   }
+}
+
+// dK and dV of the tiles that were cut, their units' sums added in order: a block a tile of
+// 128 rows of a key head and 32 columns of K (blockIdx.y < D / 32) or V
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+  constexpr int DB = D / 32;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6),
+            h2 = lane >> 5, lq = lane & 31;
+  const int kv = blockIdx.y / DB, db = blockIdx.y % DB, g = (int)(blockIdx.x % a.kv);
+  Span sp;
+  if (!locate(a, (int)(blockIdx.x / a.kv), 128, false, lane, sp) || sp.none) return;
+  const int steps = key_steps(sp.N, sp.tile, a.heads / a.kv, CAUSAL);
+  if (steps <= kUnitSteps) return;
+  int len;
+  const int units = tile_units(steps, unit_steps(a, CAUSAL, lane), a.units, len);
+  const int row = 128 * sp.tile + 32 * w;
+  if (units == 1 || row >= sp.N) return;
+  const float* p = unit_part(a, sp, 0, row / 32, g, kv, D);
+  const long next = (long)a.rows32 * a.kv * 64 * D;
+  floatx16 x = zero16();
+  constexpr int B = 8;  // units in flight
+  for (int u = 0; u < units; u += B) {
+    float4 v[B][4];
+#pragma unroll
+    for (int e = 0; e < B; ++e)
+#pragma unroll
+      for (int J = 0; J < 4; ++J)
+        v[e][J] = *reinterpret_cast<const float4*>(p + min(u + e, units - 1) * next +
+                                                   ((db * 4 + J) * 64 + lane) * 4);
+#pragma unroll
+    for (int e = 0; e < B; ++e)
+      if (u + e < units)
+#pragma unroll
+        for (int J = 0; J < 4; ++J) {
+          x[4 * J] += v[e][J].x;
+          x[4 * J + 1] += v[e][J].y;
+          x[4 * J + 2] += v[e][J].z;
+          x[4 * J + 3] += v[e][J].w;
+        }
+  }
+  if (row + lq >= sp.N) return;
+  const int col = (a.heads + kv * a.kv + g) * D + 32 * db;
+  store_cols(a.d_qkv + (sp.tok0 + row + lq) * ((long)(a.heads + 2 * a.kv) * D) + col, x, h2, 1.0f);
 }
 
 AttnArgs attn_args(const AttnShape& m, int T, int M) {
@@ -991,9 +1150,26 @@ unsigned packed_blocks(const AttnArgs& a, int rows, int per) {
   return (unsigned)((a.T / rows + a.nseq + 1) * (long)per);
 }
 
+// The most units of a tile: as many as leave the units' sums at 128 MB or so in all; few rows
+// are cut the most. None where no tile has the steps, or so many sequences that a block's
+// sum over them would take as long as it saves.
+void packed_units(const PackedShape& m, int T, AttnArgs& a) {
+  const long rows32 = T / 32 + (long)m.nseq + 1, steps = (T + 31) / 32 * (m.heads / m.kv);
+  const long most = (262144L * 128 / m.D + rows32 * 32 * m.kv - 1) / (rows32 * 32 * m.kv);
+  a.rows32 = (int)rows32;
+  a.units = m.nseq > 4096 || steps <= 40 ? 1 : (int)std::min(most, 32L);
+}
+size_t part_bytes(const PackedShape& m, const AttnArgs& a) {
+  return a.units > 1 ? (size_t)a.units * a.rows32 * m.kv * 64 * m.D * sizeof(float) : 0;
+}
+
 }  // namespace
 
-size_t packed_attn_ws_bytes(const PackedShape&, int) { return 0; }
+size_t packed_attn_ws_bytes(const PackedShape& m, int T) {
+  AttnArgs a = {};
+  packed_units(m, T, a);
+  return T == 0 ? 0 : part_bytes(m, a);
+}
 
 #define FLOWMOE_PACKED_LAUNCH(KERNEL, ARGS64, ARGS128, grid, threads)                         \
   do {                                                                                        \
@@ -1022,7 +1198,7 @@ hipError_t launch_packed_attn_fwd(const PackedShape& m, int T, const void* qkv,
 
 hipError_t launch_packed_attn_bwd(const PackedShape& m, int T, const void* qkv,
                                   const int32_t* starts, const void* o, const float* lse,
-                                  const void* d_o, void* d_qkv, float* delta, void*,
+                                  const void* d_o, void* d_qkv, float* delta, void* ws,
                                   hipStream_t st) {
   if (T == 0) return hipSuccess;
   AttnArgs a = packed_args(m, T, qkv, starts);
@@ -1031,12 +1207,27 @@ hipError_t launch_packed_attn_bwd(const PackedShape& m, int T, const void* qkv,
   a.d_qkv = static_cast<bf16_t*>(d_qkv);
   a.lse = const_cast<float*>(lse);
   a.delta = delta;
-  const hipError_t e = traced(FLOWMOE_K_ATTN_BWD_DQ, st, [&] {
-    FLOWMOE_PACKED_LAUNCH(attn_dq_kernel, FLOWMOE_NONE, FLOWMOE_NONE, packed_blocks(a, 128, m.heads), 256);
+  packed_units(m, T, a);
+  a.part = static_cast<float*>(ws);
+  hipError_t e = traced(FLOWMOE_K_ATTN_BWD_DQ, st, [&] {
+    FLOWMOE_PACKED_LAUNCH(attn_dq_kernel, FLOWMOE_NONE, FLOWMOE_NONE,
+                          packed_blocks(a, 128, m.heads), 256);
   });
-  if (e != hipSuccess) return e;
-  return traced(FLOWMOE_K_ATTN_BWD_DKDV, st, [&] {
-    FLOWMOE_PACKED_LAUNCH(attn_dkdv_kernel, FLOWMOE_NONE, FLOWMOE_NONE, packed_blocks(a, 128, m.kv), 256);
+  if (e == hipSuccess)
+    e = traced(FLOWMOE_K_ATTN_BWD_DKDV, st, [&] {
+      FLOWMOE_PACKED_LAUNCH(attn_dkdv_kernel, FLOWMOE_NONE, FLOWMOE_NONE,
+                            packed_blocks(a, 128, m.kv * a.units), 256);
+    });
+  if (e != hipSuccess || a.units == 1) return e;
+  return traced(FLOWMOE_K_PACKED_JOIN, st, [&] {
+    const dim3 g(packed_blocks(a, 128, m.kv), 2 * m.D / 32), b(256);
+    if (m.D == 128) {
+      if (m.causal) hipLaunchKernelGGL((attn_join_kernel<128, true>), g, b, 0, st, a);
+      else hipLaunchKernelGGL((attn_join_kernel<128, false>), g, b, 0, st, a);
+    } else {
+      if (m.causal) hipLaunchKernelGGL((attn_join_kernel<64, true>), g, b, 0, st, a);
+      else hipLaunchKernelGGL((attn_join_kernel<64, false>), g, b, 0, st, a);
+    }
   });
 }
 

@@ -102,6 +102,29 @@ def test_long_sequences():
     Case([3100], 2, 2, 64, False).check()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens,heads,kv", [
+    ([2031], 8, 1), ([1500, 3, 600], 2, 2), ([30] * 70 + [1100, 31, 700], 4, 1), ([1281], 1, 1),
+])
+def test_long_tiles_are_cut(lens, heads, kv, causal, D):
+    """Few long tiles: cut into units, whose sums are joined; with up to 63 sequences and more."""
+    c = Case(lens, heads, kv, D, causal, 9)
+    assert c.n > 0
+    c.check()
+    want = c.d_qkv.clone()
+    c.ws.fill_(255)
+    c.bwd()
+    assert torch.equal(c.d_qkv, want)
+
+
+@pytest.mark.parametrize("n", [62, 63, 64, 65])
+def test_number_of_sequences(n):
+    """About where the search for a block's sequence changes, in any order of lengths."""
+    g = torch.Generator().manual_seed(n)
+    Case(torch.randint(0, 200, (n,), generator=g).tolist(), 4, 2, 64, True, 30).check()
+
+
 @pytest.mark.parametrize("heads,kv", [(16, 2), (32, 8), (24, 8), (12, 4)])
 def test_heads(heads, kv):
     """Grids with heads on XCDs of their own and without."""

@@ -22,11 +22,13 @@
 //   dkdv kernel (blocks of 128 keys, loop over 32-query steps): S and dP with
 //     the key as the accumulator column, dV^T += dO^T P, dK^T += Q^T dS.
 #include <math.h>
+#include <stdlib.h>
 
 #include <algorithm>
 
 #include "attn_tiles.hpp"
 #include "common.hpp"
+#include "packed.hpp"
 
 namespace flowmoe {
 namespace {
@@ -39,30 +41,6 @@ namespace {
 // 1809, 1843, 1728, 1644, 1653. With steps of at least 8, 16, 32: the first 148, 152, 142; 1000
 // tokens in 5, 8 on 2 of 64 30, 37, 47.
 constexpr int kUnits = 850, kUnitSteps = 16;
-
-struct AttnArgs {
-  const bf16_t* qkv;  // T x 3M = [Q | K | V]; head h at columns h * D of each
-  const bf16_t* o;    // T x M: the heads' outputs (backward)
-  const bf16_t* d_o;  // T x M: their gradient (backward)
-  bf16_t* out;        // forward: T x M
-  bf16_t* d_qkv;      // backward: T x 3M
-  float* lse;         // heads x T: natural log-sum-exp of each row's scores
-  float* delta;       // heads x T: rowsum(dO * O) over the head's columns
-  int T, M, N, heads, nseq;
-  int shared;  // query tiles of a head side by side on one XCD (decode)
-  int pair;  // causal grid of one round of resident blocks: pair long and short tiles (decode)
-  float c2;  // log2(e) / sqrt(D): a score times c2 is its base-2 exponent
-  float rs;  // 1 / sqrt(D)
-  // packed sequences (locate): nseq of them from rows starts[i] on, query heads in groups
-  // that share kv key/value heads
-  const int32_t* starts;
-  int kv;
-  // backward: a key tile of more steps than a share of the launch (unit_steps) is cut into at
-  // most `units` units, whose sums go to part
-  float* part;
-  int units;
-  int rows32;  // 32-row tiles of all sequences (tile32)
-};
 
 // block -> (query or key tile, head, sequence). Blocks are dispatched in
 // order; u = blockIdx / (heads x sequences) ranks the tiles by their causal
@@ -93,81 +71,6 @@ __device__ __forceinline__ void decode(const AttnArgs& a, bool rev, bool shared,
   tile = rev ? nt - 1 - r : r;
   hd = rest % a.heads;
   sq = rest / a.heads;
-}
-
-// A block's rows: tokens tok0 .. tok0 + N - 1 are the sequence, `tile` of it the block's;
-// qkv rows are ld apart, head hd's K and V columns k and v past its Q columns.
-struct Span {
-  long tok0, ld, k, v;
-  int N, tile, hd;
-  int seq;    // packed: the sequence's index
-  bool none;  // packed: no sequence's rows, whose outputs are zeros
-};
-
-// Packed sequences, sequence i from row packed_start(i) on; the rows behind the last are a
-// sequence of their own. Whatever `starts` holds, rows stay in 0 .. T.
-__device__ __forceinline__ int packed_start(const AttnArgs& a, int i) {
-  return i == 0 ? 0 : i > a.nseq ? a.T : min(max(a.starts[i], 0), a.T);
-}
-
-// The tile of `slot`, one of T / rows + nseq + 1 (false: none), by a wave, without sums over
-// all lengths stored anywhere.
-//
-// Up to 63 sequences: a lane each, and a scan of their tiles. More: tile t of sequence i has
-// slot packed_start(i) / rows + i + t, as many as there are before sequence i + 1's or
-// fewer, and a search finds the sequence, 64 at a time.
-__device__ __forceinline__ bool locate(const AttnArgs& a, int slot, int rows, bool rev, int lane,
-                                       Span& s) {
-  int i, r0, base;
-  if (a.nseq < 64) {
-    const int st = lane <= a.nseq ? packed_start(a, lane) : 0;
-    const int n = lane <= a.nseq ? packed_start(a, lane + 1) - st : 0;
-    const int nt = n > 0 ? (n + rows - 1) / rows : 0;
-    int before = nt;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(before, o);
-      if (lane >= o) before += v;
-    }
-    before -= nt;
-    const unsigned long m = __ballot(lane <= a.nseq && slot >= before && slot < before + nt);
-    if (m == 0) return false;
-    i = __builtin_ctzll(m);
-    r0 = __builtin_amdgcn_readlane(st, i);
-    s.N = __builtin_amdgcn_readlane(n, i);
-    base = __builtin_amdgcn_readlane(before, i);
-  } else {
-    int lo = 0, hi = a.nseq + 1;  // one of lo .. hi - 1 has the slot; lo's begin at or before it
-    while (hi - lo > 1) {
-      const int step = (hi - lo + 63) / 64, k = lo + lane * step;
-      const bool before = k < hi && packed_start(a, k) / rows + k <= slot;
-      const int n = max(1, (int)__popcll(__ballot(before)));
-      lo += (n - 1) * step;
-      hi = min(hi, lo + step);
-    }
-    i = __builtin_amdgcn_readfirstlane(lo);
-    r0 = __builtin_amdgcn_readfirstlane(packed_start(a, i));
-    s.N = __builtin_amdgcn_readfirstlane(packed_start(a, i + 1)) - r0;
-    base = r0 / rows + i;
-  }
-  s.seq = i;
-  s.tok0 = r0;
-  s.none = i == a.nseq;
-  const int t = slot - base, nt = s.N > 0 ? (s.N + rows - 1) / rows : 0;
-  s.tile = rev ? nt - 1 - t : t;
-  return t >= 0 && t < nt;
-}
-
-// The packed grid: a slot's `per` heads side by side (where per is a multiple of 8, those of
-// a group on one XCD, through whose L2 they read their keys), each in `units` units; the
-// tiles of a sequence in descending order (`rev`).
-__device__ __forceinline__ bool packed_span(const AttnArgs& a, int per, bool rev, int rows,
-                                            int units, int lane, Span& s, int& unit) {
-  const int j = (int)(blockIdx.x % per), u = (int)(blockIdx.x / per);
-  s.hd = per % 8 == 0 ? (j & 7) * (per >> 3) + (j >> 3) : j;
-  const int slots = (int)(gridDim.x / per) / units;
-  unit = u / slots;
-  return locate(a, u - unit * slots, rows, rev, lane, s);
 }
 
 // Steps of a key tile of 128 rows in the backward, 32 queries a step: the group's heads one
@@ -213,14 +116,6 @@ __device__ __forceinline__ void store_part(float* p, const floatx16 (&x)[DB], in
       *reinterpret_cast<float4*>(p + ((db * 4 + J) * 64 + lane) * 4) =
           make_float4(x[db][4 * J] * scale, x[db][4 * J + 1] * scale, x[db][4 * J + 2] * scale,
                       x[db][4 * J + 3] * scale);
-}
-
-// zeros in `cols` columns of rows r0 .. r0 + n - 1 (16-byte vectors)
-__device__ __forceinline__ void zero_rows(bf16_t* dst, long ld, long r0, int n, int cols, int tid,
-                                          int threads) {
-  const int c = cols / 8;
-  for (int i = tid; i < n * c; i += threads)
-    *reinterpret_cast<u32x4*>(dst + (r0 + i / c) * ld + 8 * (i % c)) = u32x4{0, 0, 0, 0};
 }
 
 // Query tiles: the block's span, with or without packing; false: no rows
@@ -1131,18 +1026,10 @@ hipError_t launch_attn_bwd(const AttnShape& m, int T, int M, const void* qkv, co
 // ---------------------------------------------------------------------------
 namespace {
 
-AttnArgs packed_args(const PackedShape& m, int T, const void* qkv, const int32_t* starts) {
-  AttnArgs a = {};
-  a.T = T;
-  a.M = m.heads * m.D;
-  a.heads = m.heads;
-  a.kv = m.kv;
-  a.nseq = m.nseq;
-  a.starts = starts;
-  a.c2 = kLog2e / sqrtf((float)m.D);
-  a.rs = 1.0f / sqrtf((float)m.D);
-  a.qkv = static_cast<const bf16_t*>(qkv);
-  return a;
+// Sequences so short on average that a wave each serves them best (packed_short.hip)?
+bool packed_short(const PackedShape& m, int T) {
+  const int k = getenv("V1") ? atoi(getenv("V1")) : 32;
+  return T <= (long)k * m.nseq;
 }
 
 // blocks of a packed grid: its slots (locate) times `per` heads
@@ -1168,7 +1055,7 @@ size_t part_bytes(const PackedShape& m, const AttnArgs& a) {
 size_t packed_attn_ws_bytes(const PackedShape& m, int T) {
   AttnArgs a = {};
   packed_units(m, T, a);
-  return T == 0 ? 0 : part_bytes(m, a);
+  return T == 0 || packed_short(m, T) ? 0 : part_bytes(m, a);
 }
 
 #define FLOWMOE_PACKED_LAUNCH(KERNEL, ARGS64, ARGS128, grid, threads)                         \
@@ -1188,6 +1075,7 @@ size_t packed_attn_ws_bytes(const PackedShape& m, int T) {
 hipError_t launch_packed_attn_fwd(const PackedShape& m, int T, const void* qkv,
                                   const int32_t* starts, void* o, float* lse, hipStream_t st) {
   if (T == 0) return hipSuccess;
+  if (packed_short(m, T)) return launch_short_attn_fwd(m, T, qkv, starts, o, lse, st);
   AttnArgs a = packed_args(m, T, qkv, starts);
   a.out = static_cast<bf16_t*>(o);
   a.lse = lse;
@@ -1201,6 +1089,8 @@ hipError_t launch_packed_attn_bwd(const PackedShape& m, int T, const void* qkv,
                                   const void* d_o, void* d_qkv, float* delta, void* ws,
                                   hipStream_t st) {
   if (T == 0) return hipSuccess;
+  if (packed_short(m, T))
+    return launch_short_attn_bwd(m, T, qkv, starts, o, lse, d_o, d_qkv, delta, st);
   AttnArgs a = packed_args(m, T, qkv, starts);
   a.o = static_cast<const bf16_t*>(o);
   a.d_o = static_cast<const bf16_t*>(d_o);

@@ -423,6 +423,12 @@ hipError_t launch_packed_attn_bwd(const PackedShape& m, int T, const void* qkv,
                                   const int32_t* starts, const void* o, const float* lse,
                                   const void* d_o, void* d_qkv, float* delta, void* ws,
                                   hipStream_t st);
+// the same for short sequences, a wave a tile of 32 rows (no scratch)
+hipError_t launch_short_attn_fwd(const PackedShape& m, int T, const void* qkv,
+                                 const int32_t* starts, void* o, float* lse, hipStream_t st);
+hipError_t launch_short_attn_bwd(const PackedShape& m, int T, const void* qkv,
+                                 const int32_t* starts, const void* o, const float* lse,
+                                 const void* d_o, void* d_qkv, float* delta, hipStream_t st);
 // partial sums of a weight gradient (M x N) whose rows are split
 inline size_t wgrad_part_bytes(int M, int N, long rows) {
   const int s = dense_wgrad_splits(M, N, rows);

@@ -22,7 +22,6 @@
 //   dkdv kernel (blocks of 128 keys, loop over 32-query steps): S and dP with
 //     the key as the accumulator column, dV^T += dO^T P, dK^T += Q^T dS.
 #include <math.h>
-#include <stdlib.h>
 
 #include <algorithm>
 
@@ -169,18 +168,22 @@ __device__ __forceinline__ bool query_span(const AttnArgs& a, int D, bool causal
 // where a launch is several rounds. us of the loop before, ahead, in turn: 32
 // sequences of 512, 16 heads, bidirectional 56, 62, 51 (8 waves); 4 x 4096, 24 heads,
 // causal 252, 266, 229; 8 x 512 20, 19, 18; 1 x 4096, 8 heads 64, 54, 55.
-template <int D, bool CAUSAL, int NW, bool PACKED>
-__global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(AttnArgs a) {
+template <int D, bool CAUSAL, int NW, bool PACKED, int SPLIT>
+__global__ __launch_bounds__(64 * NW * SPLIT, D == 128 ? 2 : 4) void attn_fwd_kernel(AttnArgs a) {
   constexpr bool AHEAD = D == 128;
   constexpr int KS = D / 16, DB = D / 32, QB = 32 * NW;
   using Dma = TileDma<D, 64, NW>;
   constexpr int TB = Dma::TB;
-  __shared__ __attribute__((aligned(1024))) char lds[4 * TB];  // K slots 0, 1, then V slots 0, 1
+  __shared__ __attribute__((aligned(1024))) char all[SPLIT * 4 * TB];  // a group: K slots 0, 1, then V slots 0, 1
   // the wave index through readfirstlane: the compiler then knows it is
   // wave-uniform, and the branches on a wave's query or key range are
   // scalar branches instead of exec-mask ones (backward 7-10% faster)
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
+  // (group grp of NW waves has the key tiles grp, grp + SPLIT, ...)
+  const int grp = SPLIT > 1 ? wv / NW : 0, w = SPLIT > 1 ? wv % NW : wv, ko = 64 * grp;
+  constexpr int KT = 64 * SPLIT;
+  char* const lds = all + grp * 4 * TB;
   Span sp;
   if (!query_span<PACKED>(a, D, CAUSAL, QB, lane, sp)) return;
   const long tok0 = sp.tok0, ld = sp.ld;
@@ -188,26 +191,26 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
   if constexpr (PACKED) {
     if (sp.none) {
       const int n = min(QB, N - q0);
-      zero_rows(a.out + (long)hd * D, a.M, tok0 + q0, n, D, tid, 64 * NW);
-      for (int i = tid; i < n; i += 64 * NW) a.lse[(long)hd * a.T + tok0 + q0 + i] = 0.0f;
+      zero_rows(a.out + (long)hd * D, a.M, tok0 + q0, n, D, tid, 64 * NW * SPLIT);
+      for (int i = tid; i < n; i += 64 * NW * SPLIT) a.lse[(long)hd * a.T + tok0 + q0 + i] = 0.0f;
       return;
     }
   }
   const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
-  const bf16_t* Kg = Qg + sp.k;
-  const bf16_t* Vg = Qg + sp.v;
+  const bf16_t* Kg = Qg + sp.k + ko * ld;
+  const bf16_t* Vg = Qg + sp.v + ko * ld;
 
   const int kend = CAUSAL ? min(N, q0 + QB) : N;
-  const int nk = (kend + 63) / 64;
+  const int nkt = (kend + 63) / 64, nk = (nkt + SPLIT - 1) / SPLIT;
   // (causal: a wave whose queries all precede a tile has nothing in it; packed: nor one
   // without queries)
-  const int nkc = CAUSAL ? min(nk, (q0 + 32 * w + 31) / 64 + 1) : nk;
-  const int nkw = PACKED && q0 + 32 * w >= N ? 0 : nkc;
-  const Dma dma(lds_base(lds), w, lane, ld);
-  const long kstep = 64 * ld;
-  dma.load(Kg, kend, 0);
-  dma.load(Vg, kend, 2 * TB);
-  if constexpr (AHEAD) dma.load(Kg + kstep, kend - 64, TB);  // (past the last tile: no traffic)
+  const int nkc = CAUSAL ? min(nkt, (q0 + 32 * w + 31) / 64 + 1) : nkt;
+  const int nkw = PACKED && q0 + 32 * w >= N ? 0 : (nkc + SPLIT - 1 - grp) / SPLIT;
+  const Dma dma(lds_base(all) + grp * 4 * TB, w, lane, ld);
+  const long kstep = KT * ld;
+  dma.load(Kg, kend - ko, 0);
+  dma.load(Vg, kend - ko, 2 * TB);
+  if constexpr (AHEAD) dma.load(Kg + kstep, kend - ko - KT, TB);  // (past the last tile: no traffic)
 
   bf16x8 qf[KS];
 #pragma unroll
@@ -292,8 +295,8 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
     }
     Kg += kstep;  // K(t + 1), V(t + 1)
     Vg += kstep;
-    dma.load(Kg, kend - 64 * (t + 1), (st ^ 1) * TB);
-    dma.load(Vg, kend - 64 * (t + 1), (2 + (st ^ 1)) * TB);
+    dma.load(Kg, kend - ko - KT * (t + 1), (st ^ 1) * TB);
+    dma.load(Vg, kend - ko - KT * (t + 1), (2 + (st ^ 1)) * TB);
     if (!live) return;
     floatx16 sc[2];
 #pragma unroll
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
       mul_k(sc, i);
       __builtin_amdgcn_sched_barrier(0);
     }
-    mask(sc, 64 * t);
+    mask(sc, ko + KT * t);
     move_ref(row_max(sc));
     unsigned pw[16];
     float rsum = 0.0f;
@@ -344,7 +347,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
       __builtin_amdgcn_sched_barrier(0);
       mul_k(s[0], i);
     }
-    mask(s[0], 0);
+    mask(s[0], ko);
     move_ref(row_max(s[0]));
   }
 
@@ -364,8 +367,8 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
     }
     Kg += kstep;  // K(t + 1), V(t + 1)
     Vg += kstep;
-    dma.load(Kg + kstep, kend - 64 * (t + 2), st * TB);
-    dma.load(Vg, kend - 64 * (t + 1), (2 + (st ^ 1)) * TB);
+    dma.load(Kg + kstep, kend - ko - KT * (t + 2), st * TB);
+    dma.load(Vg, kend - ko - KT * (t + 1), (2 + (st ^ 1)) * TB);
     if (!live) return;
     unsigned pw[16];  // the 32 probabilities of this lane, bf16 pairs
     // (the sum in key order, then the lane pair's two halves, tile by tile: results do
@@ -399,7 +402,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      mask(sn, (t + 1) * 64);
+      mask(sn, ko + KT * (t + 1));
     } else {
       read_group(tk, tv, KS);
       read_group(tk, tv, KS + 1);
@@ -435,6 +438,38 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
     step(t, Stage<0>{});
     if (t + 1 < nk) step(t + 1, Stage<1>{});
   }
+  if constexpr (SPLIT > 1) {
+    // the groups' sums, in order. (Of a live tile every query sees the first key, so that a
+    // group's m is finite or, with no tile, its sums are zeros; the first group has key 0.)
+    float* part = reinterpret_cast<float*>(all);
+    constexpr int NF = 16 * DB + 2;
+    static_assert((SPLIT - 1) * NW * NF * 256 <= SPLIT * 4 * TB, "the sums fit the tiles' LDS");
+    wait_vm<0>();  // (loads past the last tile write zeros)
+    lds_barrier();
+    if (grp > 0) {
+      float* p = part + ((grp - 1) * NW + w) * NF * 64 + lane;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[(16 * db + r) * 64] = o[db][r];
+      p[16 * DB * 64] = m;
+      p[(16 * DB + 1) * 64] = l;
+    }
+    lds_barrier();
+    if (grp > 0) return;
+#pragma unroll 1
+    for (int e = 0; e < SPLIT - 1; ++e) {
+      const float* p = part + (e * NW + w) * NF * 64 + lane;
+      const float m1 = p[16 * DB * 64], mn = fmaxf(m, m1);
+      const float a0 = exp2_fast(m - mn), a1 = exp2_fast(m1 - mn);
+      l = l * a0 + p[(16 * DB + 1) * 64] * a1;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] = o[db][r] * a0 + p[(16 * db + r) * 64] * a1;
+      m = mn;
+    }
+  }
   if (qw < N) {
     const float inv = 1.0f / l;
     bf16_t* Og = a.out + (tok0 + qw) * a.M + (long)hd * D;
@@ -453,17 +488,21 @@ __global__ __launch_bounds__(64 * NW, D == 128 ? 2 : 4) void attn_fwd_kernel(Att
 // rows are read from LDS (registers hold Q). Before -> now: 4 x 4096 tokens, 32 heads
 // of 128, causal 970 -> 850 us; one sequence of 4096, 16 heads 171 -> 135; 4 x 1500, 20
 // heads of 64, bidirectional 112 -> 102.
-template <int D, bool CAUSAL, bool PACKED>
-__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
+template <int D, bool CAUSAL, bool PACKED, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT, 2) void attn_dq_kernel(AttnArgs a) {
   constexpr int KS = D / 16, DB = D / 32, NW = 4, QB = 32 * NW;
   using Dma = TileDma<D, 32, NW>;
-  constexpr int TB = Dma::TB, VB = 3 * TB, GB = 5 * TB;  // K slots, V slots, the dO rows
-  __shared__ __attribute__((aligned(1024))) char lds[GB + QB * D * 2];
+  constexpr int TB = Dma::TB, VB = 3 * TB, GB = SPLIT * 5 * TB;  // a group's K, V slots; the dO rows
+  __shared__ __attribute__((aligned(1024))) char all[GB + QB * D * 2];
   // the wave index through readfirstlane: the compiler then knows it is
   // wave-uniform, and the branches on a wave's query or key range are
   // scalar branches instead of exec-mask ones (backward 7-10% faster)
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
+  // (group grp of NW waves has the key tiles grp, grp + SPLIT, ...)
+  const int grp = SPLIT > 1 ? wv / NW : 0, w = SPLIT > 1 ? wv % NW : wv, ko = 32 * grp;
+  constexpr int KT = 32 * SPLIT;
+  char* const lds = all + grp * 5 * TB;
   Span sp;
   if (!query_span<PACKED>(a, D, CAUSAL, QB, lane, sp)) return;
   const long tok0 = sp.tok0, ld = sp.ld;
@@ -471,36 +510,36 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   if constexpr (PACKED) {
     if (sp.none) {
       const int n = min(QB, N - q0);
-      zero_rows(a.d_qkv + (long)hd * D, ld, tok0 + q0, n, D, tid, 64 * NW);
-      for (int i = tid; i < n; i += 64 * NW) a.delta[(long)hd * a.T + tok0 + q0 + i] = 0.0f;
+      zero_rows(a.d_qkv + (long)hd * D, ld, tok0 + q0, n, D, tid, 64 * NW * SPLIT);
+      for (int i = tid; i < n; i += 64 * NW * SPLIT) a.delta[(long)hd * a.T + tok0 + q0 + i] = 0.0f;
       return;
     }
   }
   const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
-  const bf16_t* Kg = Qg + sp.k;
-  const bf16_t* Vg = Qg + sp.v;
+  const bf16_t* Kg = Qg + sp.k + ko * ld;
+  const bf16_t* Vg = Qg + sp.v + ko * ld;
   const bf16_t* Gg = a.d_o + tok0 * a.M + (long)hd * D;
   const bf16_t* Og = a.o + tok0 * a.M + (long)hd * D;
   const bool live = qw < N;
 
   const int kend = CAUSAL ? min(N, q0 + QB) : N;
-  const int nk = (kend + 31) / 32;
+  const int nkt = (kend + 31) / 32, nk = (nkt + SPLIT - 1) / SPLIT;
   // (causal: a wave whose queries all precede a tile has nothing in it; packed: nor one
   // without queries)
-  const int nkc = CAUSAL ? min(nk, (q0 + 32 * w + 31) / 32 + 1) : nk;
-  const int nkw = PACKED && q0 + 32 * w >= N ? 0 : nkc;
-  const long kstep = 32 * ld;
-  const Dma dma(lds_base(lds), w, lane, ld);
-  {
-    const Dma dmag(lds_base(lds), w, lane, a.M);
+  const int nkc = CAUSAL ? min(nkt, (q0 + 32 * w + 31) / 32 + 1) : nkt;
+  const int nkw = PACKED && q0 + 32 * w >= N ? 0 : (nkc + SPLIT - 1 - grp) / SPLIT;
+  const long kstep = KT * ld;
+  const Dma dma(lds_base(all) + grp * 5 * TB, w, lane, ld);
+  if (grp == 0) {
+    const Dma dmag(lds_base(all), w, lane, a.M);
 #pragma unroll
     for (int i = 0; i < NW; ++i)
       dmag.load(Gg + (long)(q0 + 32 * i) * a.M, N - q0 - 32 * i, GB + i * TB);
   }
-  dma.load(Kg, kend, 0);
-  dma.load(Vg, kend, VB);
-  dma.load(Kg + kstep, kend - 32, TB);  // (past the last tile: no traffic)
-  dma.load(Vg + kstep, kend - 32, VB + TB);
+  dma.load(Kg, kend - ko, 0);
+  dma.load(Vg, kend - ko, VB);
+  dma.load(Kg + kstep, kend - ko - KT, TB);  // (past the last tile: no traffic)
+  dma.load(Vg + kstep, kend - ko - KT, VB + TB);
   bf16x8 qf[KS];
   float dl = 0.0f;
 #pragma unroll
@@ -513,7 +552,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   }
   dl += __shfl_xor(dl, 32);
   const long srow = (long)hd * a.T + tok0 + qw;
-  if (live && h2 == 0) a.delta[srow] = dl;
+  if (live && h2 == 0 && grp == 0) a.delta[srow] = dl;
   const float l2 = live ? a.lse[srow] * kLog2e : 0.0f;
   floatx16 dq[DB];
 #pragma unroll
@@ -529,7 +568,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     if (i < KS) {
       fr[i % RS][0] = frag_row_x<D>(tk, rbase, 0, i);
       fr[i % RS][1] = frag_row_x<D>(tv, rbase, 0, i);
-      fr[i % RS][2] = frag_row_x<D>(lds + GB, rbase, 32 * w, i);
+      fr[i % RS][2] = frag_row_x<D>(all + GB, rbase, 32 * w, i);
     } else if (i < NG) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -562,7 +601,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     __builtin_amdgcn_sched_barrier(0);
     mul(s[0], dp[0], i);
   }
-  mask(s[0], 0);
+  mask(s[0], ko);
 
   int k0s = 0;  // tile t's K slot
   auto step = [&](const int t, auto stc) {
@@ -581,8 +620,8 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
     }
     Kg += kstep;  // K(t + 1), V(t + 1)
     Vg += kstep;
-    dma.load(Kg + kstep, kend - 32 * (t + 2), k2s * TB);
-    dma.load(Vg + kstep, kend - 32 * (t + 2), VB + st * TB);
+    dma.load(Kg + kstep, kend - ko - KT * (t + 2), k2s * TB);
+    dma.load(Vg + kstep, kend - ko - KT * (t + 2), VB + st * TB);
     k0s = k1s;
     if (t >= nkw) return;
     unsigned pw[8];  // dS^T of this lane, bf16 pairs
@@ -611,7 +650,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      mask(s[st ^ 1], 32 * (t + 1));
+      mask(s[st ^ 1], ko + KT * (t + 1));
     } else {
       read_group(tk, tv, tkt, KS);
       if constexpr (RS > 2) read_group(tk, tv, tkt, KS + 1);
@@ -635,6 +674,30 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
   for (int t = 0; t < nk; t += 2) {
     step(t, Stage<0>{});
     if (t + 1 < nk) step(t + 1, Stage<1>{});
+  }
+  if constexpr (SPLIT > 1) {
+    // the groups' sums, in order
+    float* part = reinterpret_cast<float*>(all);
+    static_assert((SPLIT - 1) * NW * DB * 16 * 256 <= GB + QB * D * 2, "the sums fit the tiles' LDS");
+    wait_vm<0>();  // (loads past the last tile write zeros)
+    lds_barrier();
+    if (grp > 0) {
+      float* p = part + ((grp - 1) * NW + w) * DB * 16 * 64 + lane;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[(16 * db + r) * 64] = dq[db][r];
+    }
+    lds_barrier();
+    if (grp > 0) return;
+#pragma unroll 1
+    for (int e = 0; e < SPLIT - 1; ++e) {
+      const float* p = part + (e * NW + w) * DB * 16 * 64 + lane;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dq[db][r] += p[(16 * db + r) * 64];
+    }
   }
   if (live) {
     bf16_t* dst = a.d_qkv + (tok0 + qw) * ld + (long)hd * D;
@@ -968,19 +1031,21 @@ bool shared_order(const AttnShape& m, const AttnArgs& a) {
 template <int D, int NW>
 void launch_fwd(const AttnShape& m, const AttnArgs& a, hipStream_t st) {
   const dim3 g(attn_blocks(a, 32 * NW)), b(64 * NW);
-  if (m.causal) hipLaunchKernelGGL((attn_fwd_kernel<D, true, NW, false>), g, b, 0, st, a);
-  else hipLaunchKernelGGL((attn_fwd_kernel<D, false, NW, false>), g, b, 0, st, a);
+  if (m.causal) hipLaunchKernelGGL((attn_fwd_kernel<D, true, NW, false, 1>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((attn_fwd_kernel<D, false, NW, false, 1>), g, b, 0, st, a);
 }
 
-#define FLOWMOE_ATTN_LAUNCH(KERNEL, a, st)                                       \
+#define FLOWMOE_NONE
+#define FLOWMOE_ONE , 1
+#define FLOWMOE_ATTN_LAUNCH(KERNEL, MORE, a, st)                                     \
   do {                                                                            \
     const dim3 g(attn_blocks(a)), b(256);                                         \
     if (m.D == 128) {                                                             \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true, false>), g, b, 0, st, a);      \
-      else hipLaunchKernelGGL((KERNEL<128, false, false>), g, b, 0, st, a);              \
+      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true, false MORE>), g, b, 0, st, a);      \
+      else hipLaunchKernelGGL((KERNEL<128, false, false MORE>), g, b, 0, st, a);              \
     } else {                                                                      \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true, false>), g, b, 0, st, a);       \
-      else hipLaunchKernelGGL((KERNEL<64, false, false>), g, b, 0, st, a);               \
+      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true, false MORE>), g, b, 0, st, a);       \
+      else hipLaunchKernelGGL((KERNEL<64, false, false MORE>), g, b, 0, st, a);               \
     }                                                                             \
   } while (0)
 
@@ -1015,10 +1080,10 @@ hipError_t launch_attn_bwd(const AttnShape& m, int T, int M, const void* qkv, co
   a.delta = delta;
   a.pair = attn_pair(m, a);
   a.shared = !m.causal;
-  hipError_t e = traced(FLOWMOE_K_ATTN_BWD_DQ, st, [&] { FLOWMOE_ATTN_LAUNCH(attn_dq_kernel, a, st); });
+  hipError_t e = traced(FLOWMOE_K_ATTN_BWD_DQ, st, [&] { FLOWMOE_ATTN_LAUNCH(attn_dq_kernel, FLOWMOE_ONE, a, st); });
   if (e != hipSuccess) return e;
   return traced(FLOWMOE_K_ATTN_BWD_DKDV, st,
-                [&] { FLOWMOE_ATTN_LAUNCH(attn_dkdv_kernel, a, st); });
+                [&] { FLOWMOE_ATTN_LAUNCH(attn_dkdv_kernel, FLOWMOE_NONE, a, st); });
 }
 
 // ---------------------------------------------------------------------------
@@ -1026,11 +1091,11 @@ hipError_t launch_attn_bwd(const AttnShape& m, int T, int M, const void* qkv, co
 // ---------------------------------------------------------------------------
 namespace {
 
-// Sequences so short on average that a wave each serves them best (packed_short.hip)?
-bool packed_short(const PackedShape& m, int T) {
-  const int k = getenv("V1") ? atoi(getenv("V1")) : 32;
-  return T <= (long)k * m.nseq;
-}
+// Sequences so short on average that a wave a tile of 32 rows serves them best
+// (packed_short.hip)? us with it and without: 5000 tokens in 840 of 1 to 12, 16 heads on 4 of
+// 128 40, 185, backward 137, 351; 259 in 26 of 0 to 71, 4 on 2 of 64 6, 6 and 17, 17; 1000 in 5 of
+// 100 to 300, 8 on 2 of 64 7, 8 and 55, 37; 8192 in 51 of 20 to 600, 16 of 64 35, 30.
+bool packed_short(const PackedShape& m, int T) { return T <= 32L * m.nseq; }
 
 // blocks of a packed grid: its slots (locate) times `per` heads
 unsigned packed_blocks(const AttnArgs& a, int rows, int per) {
@@ -1058,19 +1123,34 @@ size_t packed_attn_ws_bytes(const PackedShape& m, int T) {
   return T == 0 || packed_short(m, T) ? 0 : part_bytes(m, a);
 }
 
-#define FLOWMOE_PACKED_LAUNCH(KERNEL, ARGS64, ARGS128, grid, threads)                         \
-  do {                                                                                        \
-    const dim3 g(grid), b(threads);                                                           \
-    if (m.D == 128) {                                                                         \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true ARGS128, true>), g, b, 0, st, a);    \
-      else hipLaunchKernelGGL((KERNEL<128, false ARGS128, true>), g, b, 0, st, a);            \
-    } else {                                                                                  \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true ARGS64, true>), g, b, 0, st, a);      \
-      else hipLaunchKernelGGL((KERNEL<64, false ARGS64, true>), g, b, 0, st, a);              \
-    }                                                                                         \
-  } while (0)
-#define FLOWMOE_NW4 , 4
-#define FLOWMOE_NONE
+template <int D, int S>
+void run_packed_fwd(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
+  const dim3 g(packed_blocks(a, 128, m.heads)), b(256 * S);
+  if (m.causal) hipLaunchKernelGGL((attn_fwd_kernel<D, true, 4, true, S>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((attn_fwd_kernel<D, false, 4, true, S>), g, b, 0, st, a);
+}
+template <int D, int S>
+void run_packed_dq(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
+  const dim3 g(packed_blocks(a, 128, m.heads)), b(256 * S);
+  if (m.causal) hipLaunchKernelGGL((attn_dq_kernel<D, true, true, S>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((attn_dq_kernel<D, false, true, S>), g, b, 0, st, a);
+}
+template <int D>
+void run_packed_dkdv(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
+  const dim3 g(packed_blocks(a, 128, m.kv * a.units)), b(256);
+  if (m.causal) hipLaunchKernelGGL((attn_dkdv_kernel<D, true, true>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((attn_dkdv_kernel<D, false, true>), g, b, 0, st, a);
+}
+
+// Waves of a block in two groups that share its queries, each with every other key tile? Where
+// the launch's blocks are two to a CU at most and sequences are long. us, one group and two:
+// forward of one sequence, causal, 2048 tokens, 8 heads of 128 40, 37; 16 on 4 of 64 29, 25;
+// 1024 23, 23 and 17, 15; 512 15, 16 and 11, 10; 2031, 16 on 2 of 128 42, 38; 544 blocks (2048,
+// 32 on 8) 51, 53; the whole backward of these 110, 98; 100, 90; 80, 76; 55, 51; 49, 48; 43, 42;
+// 150, 133; 192, 195. Four groups are no better.
+bool packed_split(const PackedShape& m, const AttnArgs& a) {
+  return packed_blocks(a, 128, m.heads) <= 512 && a.T >= (m.D == 128 ? 1024L : 512L) * m.nseq;
+}
 
 hipError_t launch_packed_attn_fwd(const PackedShape& m, int T, const void* qkv,
                                   const int32_t* starts, void* o, float* lse, hipStream_t st) {
@@ -1080,7 +1160,11 @@ hipError_t launch_packed_attn_fwd(const PackedShape& m, int T, const void* qkv,
   a.out = static_cast<bf16_t*>(o);
   a.lse = lse;
   return traced(FLOWMOE_K_ATTN_FWD, st, [&] {
-    FLOWMOE_PACKED_LAUNCH(attn_fwd_kernel, FLOWMOE_NW4, FLOWMOE_NW4, packed_blocks(a, 128, m.heads), 256);
+    const bool split = packed_split(m, a);
+    if (m.D == 128 && split) run_packed_fwd<128, 2>(m, a, st);
+    else if (m.D == 128) run_packed_fwd<128, 1>(m, a, st);
+    else if (split) run_packed_fwd<64, 2>(m, a, st);
+    else run_packed_fwd<64, 1>(m, a, st);
   });
 }
 
@@ -1100,13 +1184,16 @@ hipError_t launch_packed_attn_bwd(const PackedShape& m, int T, const void* qkv,
   packed_units(m, T, a);
   a.part = static_cast<float*>(ws);
   hipError_t e = traced(FLOWMOE_K_ATTN_BWD_DQ, st, [&] {
-    FLOWMOE_PACKED_LAUNCH(attn_dq_kernel, FLOWMOE_NONE, FLOWMOE_NONE,
-                          packed_blocks(a, 128, m.heads), 256);
+    const bool split = packed_split(m, a);
+    if (m.D == 128 && split) run_packed_dq<128, 2>(m, a, st);
+    else if (m.D == 128) run_packed_dq<128, 1>(m, a, st);
+    else if (split) run_packed_dq<64, 2>(m, a, st);
+    else run_packed_dq<64, 1>(m, a, st);
   });
   if (e == hipSuccess)
     e = traced(FLOWMOE_K_ATTN_BWD_DKDV, st, [&] {
-      FLOWMOE_PACKED_LAUNCH(attn_dkdv_kernel, FLOWMOE_NONE, FLOWMOE_NONE,
-                            packed_blocks(a, 128, m.kv * a.units), 256);
+      if (m.D == 128) run_packed_dkdv<128>(m, a, st);
+      else run_packed_dkdv<64>(m, a, st);
     });
   if (e != hipSuccess || a.units == 1) return e;
   return traced(FLOWMOE_K_PACKED_JOIN, st, [&] {

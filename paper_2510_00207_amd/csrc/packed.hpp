@@ -58,19 +58,20 @@ __device__ __forceinline__ int packed_start(const AttnArgs& a, int i) {
 __device__ __forceinline__ bool locate(const AttnArgs& a, int slot, int rows, bool rev, int lane,
                                        Span& s) {
   int lo = 0, hi = a.nseq + 1;  // one of lo .. hi - 1 has the slot; lo's begin at or before it
-  while (hi - lo > 63) {
-    const int step = (hi - lo + 63) / 64, k = lo + lane * step;
-    const bool before = k < hi && packed_start(a, k) / rows + k <= slot;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+    const bool before = i < hi && packed_start(a, i) / rows + i <= slot;
     const int n = max(1, (int)__popcll(__ballot(before)));
     lo += (n - 1) * step;
     hi = min(hi, lo + step);
   }
-  const int k = lo + lane, st = k <= hi ? packed_start(a, k) : 0;
-  const int n = max(1, (int)__popcll(__ballot(k < hi && st / rows + k <= slot)));
-  const int i = lo + n - 1, r0 = __builtin_amdgcn_readlane(st, n - 1);
-  s.N = __builtin_amdgcn_readlane(st, n) - r0;
-  s.seq = i;
+  // (its rows by loads of their own: from the lanes that read them last, the forward of heads
+  // of 128 spilled 64 bytes a lane)
+  const int i = __builtin_amdgcn_readfirstlane(lo);
+  const int r0 = __builtin_amdgcn_readfirstlane(packed_start(a, i));
   s.tok0 = r0;
+  s.N = __builtin_amdgcn_readfirstlane(packed_start(a, i + 1)) - r0;
+  s.seq = i;
   s.none = i == a.nseq;
   const int t = slot - r0 / rows - i, nt = s.N > 0 ? (s.N + rows - 1) / rows : 0;
   s.tile = rev ? nt - 1 - t : t;

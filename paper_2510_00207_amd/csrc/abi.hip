@@ -1115,7 +1115,7 @@ flowmoe_status_t check_packed(const flowmoe_shape_t* s, const flowmoe_packed_sha
   // (a tile's rows are reached by 32-bit byte offsets; a grid holds kMaxBlocks)
   if ((long)s->T * 3 * s->M > (1L << 40) || s->T > (1 << 30) || s->M > (1 << 21))
     return fail(FLOWMOE_ERR_UNSUPPORTED, "tensor too large");
-  if ((s->T / 32 + (long)m->nseq + 1) * m->heads > kMaxBlocks)
+  if ((s->T / 32 + 2L * m->nseq + 2) * m->heads > kMaxBlocks)
     return fail(FLOWMOE_ERR_UNSUPPORTED, "too many attention tiles");
   *out = PackedShape{m->nseq, m->heads, m->kv_heads, m->head_dim, m->causal};
   return FLOWMOE_OK;

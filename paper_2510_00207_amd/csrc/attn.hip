@@ -120,10 +120,10 @@ __device__ __forceinline__ void store_part(float* p, const floatx16 (&x)[DB], in
 // Query tiles: the block's span, with or without packing; false: no rows
 template <bool PACKED>
 __device__ __forceinline__ bool query_span(const AttnArgs& a, int D, bool causal, int rows,
-                                           int lane, Span& s) {
+                                           int lane, unsigned block, unsigned blocks, Span& s) {
   if constexpr (PACKED) {
     int unit;
-    const bool any = packed_span(a, a.heads, causal, rows, 1, lane, s, unit);
+    const bool any = packed_span(a, a.heads, causal, rows, 1, lane, block, blocks, s, unit);
     s.ld = (long)(a.heads + 2 * a.kv) * D;
     const int g = s.hd / (a.heads / a.kv);
     s.k = (long)(a.heads + g - s.hd) * D;
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(64 * NW * SPLIT, D == 128 ? 2 : 4) void attn_fwd_ke
   constexpr int KT = 64 * SPLIT;
   char* const lds = all + grp * 4 * TB;
   Span sp;
-  if (!query_span<PACKED>(a, D, CAUSAL, QB, lane, sp)) return;
+  if (!query_span<PACKED>(a, D, CAUSAL, QB, lane, blockIdx.x, gridDim.x, sp)) return;
   const long tok0 = sp.tok0, ld = sp.ld;
   const int hd = sp.hd, N = sp.N, q0 = sp.tile * QB, qw = q0 + 32 * w + lq;
   if constexpr (PACKED) {
@@ -488,71 +488,74 @@ __global__ __launch_bounds__(64 * NW * SPLIT, D == 128 ? 2 : 4) void attn_fwd_ke
 // rows are read from LDS (registers hold Q). Before -> now: 4 x 4096 tokens, 32 heads
 // of 128, causal 970 -> 850 us; one sequence of 4096, 16 heads 171 -> 135; 4 x 1500, 20
 // heads of 64, bidirectional 112 -> 102.
-template <int D, bool CAUSAL, bool PACKED, int SPLIT>
-__global__ __launch_bounds__(256 * SPLIT, 2) void attn_dq_kernel(AttnArgs a) {
+//
+// DELTA: computed here; else read (attn_delta_kernel's).
+template <int D>
+constexpr int kDqLds = 5 * 64 * D + 256 * D;
+template <int D, bool CAUSAL, bool PACKED, bool DELTA>
+__device__ __forceinline__ void dq_rows(const AttnArgs& a, char* lds, unsigned block, unsigned blocks) {
   constexpr int KS = D / 16, DB = D / 32, NW = 4, QB = 32 * NW;
   using Dma = TileDma<D, 32, NW>;
-  constexpr int TB = Dma::TB, VB = 3 * TB, GB = SPLIT * 5 * TB;  // a group's K, V slots; the dO rows
-  __shared__ __attribute__((aligned(1024))) char all[GB + QB * D * 2];
+  constexpr int TB = Dma::TB, VB = 3 * TB, GB = 5 * TB;  // K slots, V slots, the dO rows
+  static_assert(GB + QB * D * 2 == kDqLds<D>, "the block's LDS");
   // the wave index through readfirstlane: the compiler then knows it is
   // wave-uniform, and the branches on a wave's query or key range are
   // scalar branches instead of exec-mask ones (backward 7-10% faster)
-  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6),
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6),
             h2 = lane >> 5, lq = lane & 31;
-  // (group grp of NW waves has the key tiles grp, grp + SPLIT, ...)
-  const int grp = SPLIT > 1 ? wv / NW : 0, w = SPLIT > 1 ? wv % NW : wv, ko = 32 * grp;
-  constexpr int KT = 32 * SPLIT;
-  char* const lds = all + grp * 5 * TB;
   Span sp;
-  if (!query_span<PACKED>(a, D, CAUSAL, QB, lane, sp)) return;
+  if (!query_span<PACKED>(a, D, CAUSAL, QB, lane, block, blocks, sp)) return;
   const long tok0 = sp.tok0, ld = sp.ld;
   const int hd = sp.hd, N = sp.N, q0 = sp.tile * QB, qw = q0 + 32 * w + lq;
   if constexpr (PACKED) {
     if (sp.none) {
       const int n = min(QB, N - q0);
-      zero_rows(a.d_qkv + (long)hd * D, ld, tok0 + q0, n, D, tid, 64 * NW * SPLIT);
-      for (int i = tid; i < n; i += 64 * NW * SPLIT) a.delta[(long)hd * a.T + tok0 + q0 + i] = 0.0f;
+      zero_rows(a.d_qkv + (long)hd * D, ld, tok0 + q0, n, D, tid, 64 * NW);
+      for (int i = tid; i < n; i += 64 * NW) a.delta[(long)hd * a.T + tok0 + q0 + i] = 0.0f;
       return;
     }
   }
   const bf16_t* Qg = a.qkv + tok0 * ld + (long)hd * D;
-  const bf16_t* Kg = Qg + sp.k + ko * ld;
-  const bf16_t* Vg = Qg + sp.v + ko * ld;
+  const bf16_t* Kg = Qg + sp.k;
+  const bf16_t* Vg = Qg + sp.v;
   const bf16_t* Gg = a.d_o + tok0 * a.M + (long)hd * D;
   const bf16_t* Og = a.o + tok0 * a.M + (long)hd * D;
   const bool live = qw < N;
 
   const int kend = CAUSAL ? min(N, q0 + QB) : N;
-  const int nkt = (kend + 31) / 32, nk = (nkt + SPLIT - 1) / SPLIT;
+  const int nk = (kend + 31) / 32;
   // (causal: a wave whose queries all precede a tile has nothing in it; packed: nor one
   // without queries)
-  const int nkc = CAUSAL ? min(nkt, (q0 + 32 * w + 31) / 32 + 1) : nkt;
-  const int nkw = PACKED && q0 + 32 * w >= N ? 0 : (nkc + SPLIT - 1 - grp) / SPLIT;
-  const long kstep = KT * ld;
-  const Dma dma(lds_base(all) + grp * 5 * TB, w, lane, ld);
-  if (grp == 0) {
-    const Dma dmag(lds_base(all), w, lane, a.M);
+  const int nkc = CAUSAL ? min(nk, (q0 + 32 * w + 31) / 32 + 1) : nk;
+  const int nkw = PACKED && q0 + 32 * w >= N ? 0 : nkc;
+  const long kstep = 32 * ld;
+  const Dma dma(lds_base(lds), w, lane, ld);
+  {
+    const Dma dmag(lds_base(lds), w, lane, a.M);
 #pragma unroll
     for (int i = 0; i < NW; ++i)
       dmag.load(Gg + (long)(q0 + 32 * i) * a.M, N - q0 - 32 * i, GB + i * TB);
   }
-  dma.load(Kg, kend - ko, 0);
-  dma.load(Vg, kend - ko, VB);
-  dma.load(Kg + kstep, kend - ko - KT, TB);  // (past the last tile: no traffic)
-  dma.load(Vg + kstep, kend - ko - KT, VB + TB);
+  dma.load(Kg, kend, 0);
+  dma.load(Vg, kend, VB);
+  dma.load(Kg + kstep, kend - 32, TB);  // (past the last tile: no traffic)
+  dma.load(Vg + kstep, kend - 32, VB + TB);
   bf16x8 qf[KS];
   float dl = 0.0f;
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     qf[ks] = live ? *reinterpret_cast<const bf16x8*>(Qg + qw * ld + 16 * ks + 8 * h2) : zero8();
-    const bf16x8 gv = live ? *reinterpret_cast<const bf16x8*>(Gg + (long)qw * a.M + 16 * ks + 8 * h2) : zero8();
-    const bf16x8 ov = live ? *reinterpret_cast<const bf16x8*>(Og + (long)qw * a.M + 16 * ks + 8 * h2) : zero8();
+    if constexpr (DELTA) {
+      const bf16x8 gv = live ? *reinterpret_cast<const bf16x8*>(Gg + (long)qw * a.M + 16 * ks + 8 * h2) : zero8();
+      const bf16x8 ov = live ? *reinterpret_cast<const bf16x8*>(Og + (long)qw * a.M + 16 * ks + 8 * h2) : zero8();
 #pragma unroll
-    for (int t = 0; t < 8; ++t) dl += (float)gv[t] * (float)ov[t];
+      for (int t = 0; t < 8; ++t) dl += (float)gv[t] * (float)ov[t];
+    }
   }
-  dl += __shfl_xor(dl, 32);
   const long srow = (long)hd * a.T + tok0 + qw;
-  if (live && h2 == 0 && grp == 0) a.delta[srow] = dl;
+  if constexpr (DELTA) dl += __shfl_xor(dl, 32);
+  else dl = live ? a.delta[srow] : 0.0f;
+  if (DELTA && live && h2 == 0) a.delta[srow] = dl;
   const float l2 = live ? a.lse[srow] * kLog2e : 0.0f;
   floatx16 dq[DB];
 #pragma unroll
@@ -568,7 +571,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void attn_dq_kernel(AttnArgs a) {
     if (i < KS) {
       fr[i % RS][0] = frag_row_x<D>(tk, rbase, 0, i);
       fr[i % RS][1] = frag_row_x<D>(tv, rbase, 0, i);
-      fr[i % RS][2] = frag_row_x<D>(all + GB, rbase, 32 * w, i);
+      fr[i % RS][2] = frag_row_x<D>(lds + GB, rbase, 32 * w, i);
     } else if (i < NG) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -601,7 +604,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void attn_dq_kernel(AttnArgs a) {
     __builtin_amdgcn_sched_barrier(0);
     mul(s[0], dp[0], i);
   }
-  mask(s[0], ko);
+  mask(s[0], 0);
 
   int k0s = 0;  // tile t's K slot
   auto step = [&](const int t, auto stc) {
@@ -620,8 +623,8 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void attn_dq_kernel(AttnArgs a) {
     }
     Kg += kstep;  // K(t + 1), V(t + 1)
     Vg += kstep;
-    dma.load(Kg + kstep, kend - ko - KT * (t + 2), k2s * TB);
-    dma.load(Vg + kstep, kend - ko - KT * (t + 2), VB + st * TB);
+    dma.load(Kg + kstep, kend - 32 * (t + 2), k2s * TB);
+    dma.load(Vg + kstep, kend - 32 * (t + 2), VB + st * TB);
     k0s = k1s;
     if (t >= nkw) return;
     unsigned pw[8];  // dS^T of this lane, bf16 pairs
@@ -650,7 +653,7 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void attn_dq_kernel(AttnArgs a) {
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      mask(s[st ^ 1], ko + KT * (t + 1));
+      mask(s[st ^ 1], 32 * (t + 1));
     } else {
       read_group(tk, tv, tkt, KS);
       if constexpr (RS > 2) read_group(tk, tv, tkt, KS + 1);
@@ -675,35 +678,17 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void attn_dq_kernel(AttnArgs a) {
     step(t, Stage<0>{});
     if (t + 1 < nk) step(t + 1, Stage<1>{});
   }
-  if constexpr (SPLIT > 1) {
-    // the groups' sums, in order
-    float* part = reinterpret_cast<float*>(all);
-    static_assert((SPLIT - 1) * NW * DB * 16 * 256 <= GB + QB * D * 2, "the sums fit the tiles' LDS");
-    wait_vm<0>();  // (loads past the last tile write zeros)
-    lds_barrier();
-    if (grp > 0) {
-      float* p = part + ((grp - 1) * NW + w) * DB * 16 * 64 + lane;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[(16 * db + r) * 64] = dq[db][r];
-    }
-    lds_barrier();
-    if (grp > 0) return;
-#pragma unroll 1
-    for (int e = 0; e < SPLIT - 1; ++e) {
-      const float* p = part + (e * NW + w) * DB * 16 * 64 + lane;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dq[db][r] += p[(16 * db + r) * 64];
-    }
-  }
   if (live) {
     bf16_t* dst = a.d_qkv + (tok0 + qw) * ld + (long)hd * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db) store_cols(dst + 32 * db, dq[db], h2, a.rs);
   }
+}
+
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[kDqLds<D>];
+  dq_rows<D, CAUSAL, false, true>(a, lds, blockIdx.x, gridDim.x);
 }
 
 // dK and dV: blocks of 4 waves of 32 keys, two to a CU, over 32-query tiles. The
@@ -713,14 +698,16 @@ __global__ __launch_bounds__(256 * SPLIT, 2) void attn_dq_kernel(AttnArgs a) {
 // the CU fills the elementwise part (half of it beside the first products of
 // dV and dK was 2-4% slower at D = 128). Before -> now, as above: 1258 -> 1120, 256 ->
 // 182 and 163 -> 127 us.
+template <int D>
+constexpr int kDkdvLds = 4 * 64 * D + 256 * D + 512;
 template <int D, bool CAUSAL, bool PACKED>
-__global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
+__device__ __forceinline__ void dkdv_rows(const AttnArgs& a, char* lds, unsigned block, unsigned blocks) {
   constexpr int KS = D / 16, DB = D / 32, NW = 4, KB = 32 * NW;
   using Dma = TileDma<D, 32, NW>;
   constexpr int TQ = Dma::TB;           // one 32-row tile
   constexpr int VT = 4 * TQ;            // two slots of Q and dO, then the block's V rows,
   constexpr int ST = VT + KB * D * 2;   // then two slots of 32 lse2 and 32 delta
-  __shared__ __attribute__((aligned(1024))) char lds[ST + 2 * 256];
+  static_assert(ST + 2 * 256 == kDkdvLds<D>, "the block's LDS");
   // the wave index through readfirstlane: the compiler then knows it is
   // wave-uniform, and the branches on a wave's query or key range are
   // scalar branches instead of exec-mask ones (backward 7-10% faster)
@@ -730,7 +717,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
   int nh = 1;  // query heads from hd on
   int unit = 0, units = 1, it0 = 0, it1 = 0;  // the block's steps
   if constexpr (PACKED) {
-    const bool any = packed_span(a, a.kv, false, KB, a.units, lane, sp, unit);
+    const bool any = packed_span(a, a.kv, false, KB, a.units, lane, block, blocks, sp, unit);
     if (!any) return;
     const int g = sp.hd;
     nh = a.heads / a.kv;
@@ -931,6 +918,49 @@ __global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
   }
 }
 
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void attn_dkdv_kernel(AttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[kDkdvLds<D>];
+  dkdv_rows<D, CAUSAL, false>(a, lds, blockIdx.x, gridDim.x);
+}
+
+// The packed backward: kblocks blocks of dK and dV, from block k0 on, and the blocks of dQ
+// before (k0 > 0) or behind them, in one launch, so that neither waits for the other's last
+// blocks; delta is attn_delta_kernel's. The whole backward in us, two launches (dQ's with
+// delta) and so: one sequence of 512, 8 heads of 128, causal 48, 29; 1024, 16 on 4 of 64 50, 35;
+// 2031, 16 on 2 of 128 133, 103; 16384 tokens in 12 of 46 to 8021, 32 on 8 2500, 2233, in 18 of 76
+// to 5801 1646, 1508. Where dQ's blocks are few they go first, as a block's walk over
+// its keys takes longer than a unit of dK and dV: 4096 tokens, 4 heads on 4 of 64 125, 94, 16 on
+// 16 of 128 304, 290; many go last: the 12 sequences 2490, 2233; 16384, 8 on 1 2027, 1791.
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void attn_packed_bwd_kernel(AttnArgs a, unsigned kblocks,
+                                                                 unsigned k0) {
+  constexpr int n = kDqLds<D> > kDkdvLds<D> ? kDqLds<D> : kDkdvLds<D>;
+  __shared__ __attribute__((aligned(1024))) char lds[n];
+  // (unsigned: blocks before k0 are not below kblocks)
+  if (blockIdx.x - k0 < kblocks) dkdv_rows<D, CAUSAL, true>(a, lds, blockIdx.x - k0, kblocks);
+  else dq_rows<D, CAUSAL, true, false>(a, lds, k0 > 0 ? blockIdx.x : blockIdx.x - kblocks, gridDim.x - kblocks);
+}
+
+// delta = rowsum(dO * O) per head and row, D / 8 lanes each (of the rows of no sequence
+// whatever they hold: dQ's blocks clear it)
+template <int D>
+__global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
+  constexpr int L = D / 8;
+  const long n = (long)a.T * a.heads, step = (long)gridDim.x * (256 / L);
+  for (long i = (long)blockIdx.x * (256 / L) + threadIdx.x / L; i < n; i += step) {
+    const long off = i * D + 8 * (threadIdx.x % L);
+    float g[8], o[8], s = 0.0f;
+    load8(a.d_o + off, g);
+    load8(a.o + off, o);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += g[e] * o[e];
+#pragma unroll
+    for (int m = L / 2; m > 0; m >>= 1) s += __shfl_xor(s, m);
+    if (threadIdx.x % L == 0) a.delta[i % a.heads * a.T + i / a.heads] = s;
+  }
+}
+
 // dK and dV of the tiles that were cut, their units' sums added in order: a block a tile of
 // 128 rows of a key head and 32 columns of K (blockIdx.y < D / 32) or V
 template <int D, bool CAUSAL>
@@ -1035,17 +1065,15 @@ void launch_fwd(const AttnShape& m, const AttnArgs& a, hipStream_t st) {
   else hipLaunchKernelGGL((attn_fwd_kernel<D, false, NW, false, 1>), g, b, 0, st, a);
 }
 
-#define FLOWMOE_NONE
-#define FLOWMOE_ONE , 1
-#define FLOWMOE_ATTN_LAUNCH(KERNEL, MORE, a, st)                                     \
+#define FLOWMOE_ATTN_LAUNCH(KERNEL, a, st)                                     \
   do {                                                                            \
     const dim3 g(attn_blocks(a)), b(256);                                         \
     if (m.D == 128) {                                                             \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true, false MORE>), g, b, 0, st, a);      \
-      else hipLaunchKernelGGL((KERNEL<128, false, false MORE>), g, b, 0, st, a);              \
+      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true>), g, b, 0, st, a);      \
+      else hipLaunchKernelGGL((KERNEL<128, false>), g, b, 0, st, a);              \
     } else {                                                                      \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true, false MORE>), g, b, 0, st, a);       \
-      else hipLaunchKernelGGL((KERNEL<64, false, false MORE>), g, b, 0, st, a);               \
+      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true>), g, b, 0, st, a);       \
+      else hipLaunchKernelGGL((KERNEL<64, false>), g, b, 0, st, a);               \
     }                                                                             \
   } while (0)
 
@@ -1080,10 +1108,10 @@ hipError_t launch_attn_bwd(const AttnShape& m, int T, int M, const void* qkv, co
   a.delta = delta;
   a.pair = attn_pair(m, a);
   a.shared = !m.causal;
-  hipError_t e = traced(FLOWMOE_K_ATTN_BWD_DQ, st, [&] { FLOWMOE_ATTN_LAUNCH(attn_dq_kernel, FLOWMOE_ONE, a, st); });
+  hipError_t e = traced(FLOWMOE_K_ATTN_BWD_DQ, st, [&] { FLOWMOE_ATTN_LAUNCH(attn_dq_kernel, a, st); });
   if (e != hipSuccess) return e;
   return traced(FLOWMOE_K_ATTN_BWD_DKDV, st,
-                [&] { FLOWMOE_ATTN_LAUNCH(attn_dkdv_kernel, FLOWMOE_NONE, a, st); });
+                [&] { FLOWMOE_ATTN_LAUNCH(attn_dkdv_kernel, a, st); });
 }
 
 // ---------------------------------------------------------------------------
@@ -1129,25 +1157,11 @@ void run_packed_fwd(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
   if (m.causal) hipLaunchKernelGGL((attn_fwd_kernel<D, true, 4, true, S>), g, b, 0, st, a);
   else hipLaunchKernelGGL((attn_fwd_kernel<D, false, 4, true, S>), g, b, 0, st, a);
 }
-template <int D, int S>
-void run_packed_dq(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
-  const dim3 g(packed_blocks(a, 128, m.heads)), b(256 * S);
-  if (m.causal) hipLaunchKernelGGL((attn_dq_kernel<D, true, true, S>), g, b, 0, st, a);
-  else hipLaunchKernelGGL((attn_dq_kernel<D, false, true, S>), g, b, 0, st, a);
-}
-template <int D>
-void run_packed_dkdv(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
-  const dim3 g(packed_blocks(a, 128, m.kv * a.units)), b(256);
-  if (m.causal) hipLaunchKernelGGL((attn_dkdv_kernel<D, true, true>), g, b, 0, st, a);
-  else hipLaunchKernelGGL((attn_dkdv_kernel<D, false, true>), g, b, 0, st, a);
-}
-
-// Waves of a block in two groups that share its queries, each with every other key tile? Where
-// the launch's blocks are two to a CU at most and sequences are long. us, one group and two:
-// forward of one sequence, causal, 2048 tokens, 8 heads of 128 40, 37; 16 on 4 of 64 29, 25;
-// 1024 23, 23 and 17, 15; 512 15, 16 and 11, 10; 2031, 16 on 2 of 128 42, 38; 544 blocks (2048,
-// 32 on 8) 51, 53; the whole backward of these 110, 98; 100, 90; 80, 76; 55, 51; 49, 48; 43, 42;
-// 150, 133; 192, 195. Four groups are no better.
+// The forward's waves in two groups that share a block's queries, each with every other key tile?
+// Where the launch's blocks are two to a CU at most and sequences are long. us of one sequence,
+// causal, one group and two: 2048 tokens, 8 heads of 128 40, 37; 16 on 4 of 64 29, 25; 1024 23, 23
+// and 17, 15; 512 15, 16 and 11, 10; 2031, 16 on 2 of 128 42, 38; 544 blocks (2048, 32 on 8) 51,
+// 53. Four groups are no better.
 bool packed_split(const PackedShape& m, const AttnArgs& a) {
   return packed_blocks(a, 128, m.heads) <= 512 && a.T >= (m.D == 128 ? 1024L : 512L) * m.nseq;
 }
@@ -1168,6 +1182,23 @@ hipError_t launch_packed_attn_fwd(const PackedShape& m, int T, const void* qkv,
   });
 }
 
+namespace {
+
+hipError_t join_packed(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
+  return traced(FLOWMOE_K_PACKED_JOIN, st, [&] {
+    const dim3 g(packed_blocks(a, 128, m.kv), 2 * m.D / 32), b(256);
+    if (m.D == 128) {
+      if (m.causal) hipLaunchKernelGGL((attn_join_kernel<128, true>), g, b, 0, st, a);
+      else hipLaunchKernelGGL((attn_join_kernel<128, false>), g, b, 0, st, a);
+    } else {
+      if (m.causal) hipLaunchKernelGGL((attn_join_kernel<64, true>), g, b, 0, st, a);
+      else hipLaunchKernelGGL((attn_join_kernel<64, false>), g, b, 0, st, a);
+    }
+  });
+}
+
+}  // namespace
+
 hipError_t launch_packed_attn_bwd(const PackedShape& m, int T, const void* qkv,
                                   const int32_t* starts, const void* o, const float* lse,
                                   const void* d_o, void* d_qkv, float* delta, void* ws,
@@ -1184,28 +1215,24 @@ hipError_t launch_packed_attn_bwd(const PackedShape& m, int T, const void* qkv,
   packed_units(m, T, a);
   a.part = static_cast<float*>(ws);
   hipError_t e = traced(FLOWMOE_K_ATTN_BWD_DQ, st, [&] {
-    const bool split = packed_split(m, a);
-    if (m.D == 128 && split) run_packed_dq<128, 2>(m, a, st);
-    else if (m.D == 128) run_packed_dq<128, 1>(m, a, st);
-    else if (split) run_packed_dq<64, 2>(m, a, st);
-    else run_packed_dq<64, 1>(m, a, st);
+    const dim3 g((unsigned)std::min(((long)T * a.M / 8 + 255) / 256, 1L << 20)), b(256);
+    if (m.D == 128) hipLaunchKernelGGL(attn_delta_kernel<128>, g, b, 0, st, a);
+    else hipLaunchKernelGGL(attn_delta_kernel<64>, g, b, 0, st, a);
   });
-  if (e == hipSuccess)
-    e = traced(FLOWMOE_K_ATTN_BWD_DKDV, st, [&] {
-      if (m.D == 128) run_packed_dkdv<128>(m, a, st);
-      else run_packed_dkdv<64>(m, a, st);
-    });
-  if (e != hipSuccess || a.units == 1) return e;
-  return traced(FLOWMOE_K_PACKED_JOIN, st, [&] {
-    const dim3 g(packed_blocks(a, 128, m.kv), 2 * m.D / 32), b(256);
+  if (e != hipSuccess) return e;
+  e = traced(FLOWMOE_K_ATTN_BWD_DKDV, st, [&] {
+    const unsigned k = packed_blocks(a, 128, m.kv * a.units), q = packed_blocks(a, 128, m.heads),
+                   k0 = q <= 1024 ? q : 0;
+    const dim3 g(k + q), b(256);
     if (m.D == 128) {
-      if (m.causal) hipLaunchKernelGGL((attn_join_kernel<128, true>), g, b, 0, st, a);
-      else hipLaunchKernelGGL((attn_join_kernel<128, false>), g, b, 0, st, a);
+      if (m.causal) hipLaunchKernelGGL((attn_packed_bwd_kernel<128, true>), g, b, 0, st, a, k, k0);
+      else hipLaunchKernelGGL((attn_packed_bwd_kernel<128, false>), g, b, 0, st, a, k, k0);
     } else {
-      if (m.causal) hipLaunchKernelGGL((attn_join_kernel<64, true>), g, b, 0, st, a);
-      else hipLaunchKernelGGL((attn_join_kernel<64, false>), g, b, 0, st, a);
+      if (m.causal) hipLaunchKernelGGL((attn_packed_bwd_kernel<64, true>), g, b, 0, st, a, k, k0);
+      else hipLaunchKernelGGL((attn_packed_bwd_kernel<64, false>), g, b, 0, st, a, k, k0);
     }
   });
+  return e != hipSuccess || a.units == 1 ? e : join_packed(m, a, st);
 }
 
 size_t packed_mha_ws_bytes(const PackedShape& m, int T) {

@@ -78,14 +78,15 @@ __device__ __forceinline__ bool locate(const AttnArgs& a, int slot, int rows, bo
   return t >= 0 && t < nt;
 }
 
-// The packed grid: a slot's `per` heads side by side (where per is a multiple of 8, those of
-// a group on one XCD, through whose L2 they read their keys), each in `units` units; the
-// tiles of a sequence in descending order (`rev`).
+// Block `block` of the `blocks` of a packed grid: a slot's `per` heads side by side (where per is
+// a multiple of 8, those of a group on one XCD, through whose L2 they read their keys), first
+// units first; the tiles of a sequence in descending order (`rev`).
 __device__ __forceinline__ bool packed_span(const AttnArgs& a, int per, bool rev, int rows,
-                                            int units, int lane, Span& s, int& unit) {
-  const int j = (int)(blockIdx.x % per), u = (int)(blockIdx.x / per);
+                                            int units, int lane, unsigned block, unsigned blocks,
+                                            Span& s, int& unit) {
+  const int j = (int)(block % per), u = (int)(block / per);
   s.hd = per % 8 == 0 ? (j & 7) * (per >> 3) + (j >> 3) : j;
-  const int slots = (int)(gridDim.x / per) / units;
+  const int slots = (int)(blocks / per) / units;
   unit = u / slots;
   return locate(a, u - unit * slots, rows, rev, lane, s);
 }

@@ -26,7 +26,7 @@ __global__ __launch_bounds__(64, D == 128 ? 3 : 4) void short_fwd_kernel(AttnArg
   const int lane = threadIdx.x, h2 = lane >> 5, lq = lane & 31;
   Span sp;
   int unit;
-  if (!packed_span(a, a.heads, CAUSAL, 32, 1, lane, sp, unit)) return;
+  if (!packed_span(a, a.heads, CAUSAL, 32, 1, lane, blockIdx.x, gridDim.x, sp, unit)) return;
   const long tok0 = sp.tok0, ld = (long)(a.heads + 2 * a.kv) * D;
   const int hd = sp.hd, N = sp.N, q0 = 32 * sp.tile, qw = q0 + lq, g = hd / (a.heads / a.kv);
   if (sp.none) {
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(64, D == 128 ? 1 : 2) void short_bwd_kernel(AttnArg
   const int lane = threadIdx.x, h2 = lane >> 5, lq = lane & 31;
   Span sp;
   int unit;
-  if (!packed_span(a, a.kv, false, 32, 1, lane, sp, unit)) return;
+  if (!packed_span(a, a.kv, false, 32, 1, lane, blockIdx.x, gridDim.x, sp, unit)) return;
   const int nh = a.heads / a.kv, g = sp.hd, N = sp.N, r0 = 32 * sp.tile, rw = r0 + lq;
   const long tok0 = sp.tok0, ld = (long)(a.heads + 2 * a.kv) * D;
   const long kcol = (long)(a.heads + g) * D, vcol = kcol + (long)a.kv * D;

@@ -1346,7 +1346,7 @@ flowmoe_status_t flowmoe_embed_fwd(const flowmoe_shape_t* shape, const flowmoe_e
 
 size_t flowmoe_embed_ws_bytes(const flowmoe_shape_t* shape, const flowmoe_embed_shape_t* embed) {
   if (check_embed(shape, embed) != FLOWMOE_OK) return 0;
-  return embed_ws_bytes(shape->T, shape->M);
+  return embed_ws_bytes(shape->T, shape->M, embed->vocab);
 }
 
 flowmoe_status_t flowmoe_embed_bwd(const flowmoe_shape_t* shape, const flowmoe_embed_shape_t* embed,
@@ -1360,7 +1360,7 @@ flowmoe_status_t flowmoe_embed_bwd(const flowmoe_shape_t* shape, const flowmoe_e
     REQUIRE_F(ids, "ids");
     REQUIRE_T(dy, "dy");
   }
-  const size_t need = embed_ws_bytes(shape->T, shape->M);
+  const size_t need = embed_ws_bytes(shape->T, shape->M, embed->vocab);
   st = check_ws(ws, ws_bytes, need, "flowmoe_embed_bwd");
   if (st != FLOWMOE_OK) return st;
   if (need > 0) REQUIRE_T(ws, "ws");

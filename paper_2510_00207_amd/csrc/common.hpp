@@ -494,7 +494,7 @@ hipError_t launch_layer_norm_bwd(int dtype, int T, int M, float eps, const void*
 
 // Embedding lookup in a table V x M, and its gradient
 bool embed_fits(int T, int M, int V);  // a grid holds the calls' blocks
-size_t embed_ws_bytes(int T, int M);
+size_t embed_ws_bytes(int T, int M, int V);
 hipError_t launch_embed_fwd(int dtype, int T, int M, int V, float scale, const int32_t* ids,
                             const void* table, void* y, hipStream_t st);
 hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const int32_t* ids,

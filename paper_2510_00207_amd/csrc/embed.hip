@@ -284,6 +284,13 @@ __device__ __forceinline__ void zero_absent(const EmbedArgs& a, long v0, int lan
     absent = absent && !(lo < end && a.ids[lo] == v);
   }
   unsigned long m = __ballot(absent);
+  if (a.M < 256) {  // narrow rows: the wave's rows as one run of 16-byte vectors
+    const int per = a.M / 4, n = (v1 - (int)v0) * per;
+    for (int u = lane; u < n; u += 64)
+      if (m >> (u / per) & 1)
+        st16<NT>(reinterpret_cast<u32x4v_t*>(a.dtable + v0 * a.M + 4 * u), u32x4v_t{0, 0, 0, 0});
+    return;
+  }
   while (m) {
     const long r = v0 + __builtin_ctzll(m);
     m &= m - 1;
@@ -355,22 +362,22 @@ int key_passes(int V) {  // keys 0 .. V
 // 55; 16384 65, 69, all of one id 248, 114; 32768 x 2048, 50021 rows 169, 135.
 int embed_chunk(int T) { return T <= kFew ? 8 : 32; }
 
-// The most items that are ranked: us of the whole gradient ranked and sorted: 1000 tokens 21,
-// 28; 4096 46, 44; 8192 63, 50.
-constexpr int kRank = 2048;
+// Ranked, in one launch, or sorted in two a pass? us of the whole gradient ranked and sorted: 1000
+// tokens, two passes 21, 28; 4096 46, 44; 8192 63, 50.
+bool ranked(int T, int V) { return T <= (key_passes(V) > 2 ? 4096 : 2048); }
 int sort_per(int T) { return std::max(1, (int)(((long)T + 262143) / 262144)) * 1024; }
 int sort_blocks(int T) { return (int)(((long)T + sort_per(T) - 1) / sort_per(T)); }
 
 struct EmbedWs {
   size_t a, b, hist, part, bytes;
 };
-EmbedWs embed_ws(int T, int M) {
+EmbedWs embed_ws(int T, int M, int V) {
   EmbedWs w;
   const size_t items = align256((size_t)T * 8);
   w.a = 0;
   w.b = items;
   w.hist = 2 * items;
-  w.part = w.hist + align256(T <= kRank ? 0 : (size_t)sort_blocks(T) * 1024);
+  w.part = w.hist + align256(ranked(T, V) ? 0 : (size_t)sort_blocks(T) * 1024);
   w.bytes = w.part + align256(((size_t)T + embed_chunk(T) - 1) / embed_chunk(T) * 2 * M * sizeof(float));
   return w;
 }
@@ -379,7 +386,7 @@ hipError_t sort_tokens(int T, int V, const int32_t* ids, const EmbedWs& w, char*
   const int passes = key_passes(V);
   int32_t* x = reinterpret_cast<int32_t*>(ws + w.b);
   int32_t* y = reinterpret_cast<int32_t*>(ws + w.a);
-  if (T <= kRank)
+  if (ranked(T, V))
     return traced(FLOWMOE_K_EMBED_SORT, st, [&] {
       hipLaunchKernelGGL(embed_rank_kernel, dim3((T + 63) / 64), dim3(1024), 0, st, ids, y, y + T, T, V);
     });
@@ -426,7 +433,7 @@ bool embed_fits(int T, int M, int V) {
   return (T + f - 1) / f <= kMaxBlocks && (embed_waves(T, M, V, false) + 3) / 4 <= kMaxBlocks;
 }
 
-size_t embed_ws_bytes(int T, int M) { return T == 0 ? 0 : embed_ws(T, M).bytes; }
+size_t embed_ws_bytes(int T, int M, int V) { return T == 0 ? 0 : embed_ws(T, M, V).bytes; }
 
 hipError_t launch_embed_fwd(int dtype, int T, int M, int V, float scale, const int32_t* ids,
                             const void* table, void* y, hipStream_t st) {
@@ -465,7 +472,7 @@ hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const i
                             const void* dy, float* dtable, int accumulate, void* ws,
                             hipStream_t st) {
   if (T == 0 && accumulate) return hipSuccess;
-  const EmbedWs w = embed_ws(T, M);
+  const EmbedWs w = embed_ws(T, M, V);
   char* base = static_cast<char*>(ws);
   EmbedArgs a = {};
   a.dy = dy;

@@ -103,13 +103,17 @@ __global__ __launch_bounds__(64, D == 128 ? 3 : 4) void short_fwd_kernel(AttnArg
   }
 }
 
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(64, D == 128 ? 1 : 2) void short_bwd_kernel(AttnArgs a) {
+template <int D, bool CAUSAL, int W>
+__global__ __launch_bounds__(64 * W, D == 128 ? 1 : 2) void short_bwd_kernel(AttnArgs a) {
   constexpr int KS = D / 16, DB = D / 32;
   using Dma = TileDma<D, 32, 1>;
   constexpr int TB = Dma::TB, VT = TB, QT = 2 * TB, GT = 3 * TB, ST = 4 * TB;
-  __shared__ __attribute__((aligned(1024))) char lds[ST + 256];  // K, V, Q, dO; 32 lse2, 32 delta
-  const int lane = threadIdx.x, h2 = lane >> 5, lq = lane & 31;
+  // a wave: K, V, Q, dO; 32 lse2, 32 delta
+  constexpr int LW = (ST + 256 + 1023) / 1024 * 1024;
+  __shared__ __attribute__((aligned(1024))) char all[W * LW];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h2 = lane >> 5,
+            lq = lane & 31;
+  char* const lds = all + w * LW;
   Span sp;
   int unit;
   if (!packed_span(a, a.kv, false, 32, 1, lane, blockIdx.x, gridDim.x, sp, unit)) return;
@@ -117,6 +121,7 @@ __global__ __launch_bounds__(64, D == 128 ? 1 : 2) void short_bwd_kernel(AttnArg
   const long tok0 = sp.tok0, ld = (long)(a.heads + 2 * a.kv) * D;
   const long kcol = (long)(a.heads + g) * D, vcol = kcol + (long)a.kv * D;
   if (sp.none) {
+    if (w > 0) return;
     const int n = min(32, N - r0);
     zero_rows(a.d_qkv + (long)g * nh * D, ld, tok0 + r0, n, nh * D, lane, 64);
     zero_rows(a.d_qkv + kcol, ld, tok0 + r0, n, D, lane, 64);
@@ -128,7 +133,7 @@ __global__ __launch_bounds__(64, D == 128 ? 1 : 2) void short_bwd_kernel(AttnArg
   const bf16_t* X = a.qkv + tok0 * ld;
   const bf16_t* G = a.d_o + tok0 * a.M;
   const bf16_t* O = a.o + tok0 * a.M;
-  const Dma dma(lds_base(lds), 0, lane, ld), dmag(lds_base(lds), 0, lane, a.M);
+  const Dma dma(lds_base(all) + w * LW, 0, lane, ld), dmag(lds_base(all) + w * LW, 0, lane, a.M);
   const int rbase = row_base<D>(lq, h2), tb0 = tr_base<D>(lane, 0), tb1 = tr_base<D>(lane, 1);
   const bool one = N <= 32;
   // (loads of a tile whose place in LDS is still being read wait for that first)
@@ -233,10 +238,21 @@ __global__ __launch_bounds__(64, D == 128 ? 1 : 2) void short_bwd_kernel(AttnArg
     st[lane] = h2 ? dl : l2;  // (both lanes of a query have both)
   };
 
+  // (a wave has LDS of its own: no barriers, its reads done before a load's writes, and its loads
+  // and writes before the reads)
+  auto own_reads = [&] {
+    wait_lgkm0();
+    asm volatile("" ::: "memory");
+  };
+  auto own_loads = [&] {
+    wait_vm<0>();
+    wait_lgkm0();
+    asm volatile("" ::: "memory");
+  };
   if (one) load_kv(0);
-  for (int h = g * nh; h < g * nh + nh; ++h) {
+  for (int h = g * nh + w; h < g * nh + nh; h += W) {
     float dl, l2;
-    lds_barrier();
+    own_reads();
     load_qg(h, r0);
     stats(h, r0, dl, l2);
     if (h2 == 0 && rw < N) a.delta[(long)h * a.T + tok0 + rw] = dl;
@@ -245,17 +261,15 @@ __global__ __launch_bounds__(64, D == 128 ? 1 : 2) void short_bwd_kernel(AttnArg
     for (int db = 0; db < DB; ++db) dq[db] = zero16();
     if (one) {
       keep_stats(dl, l2);
-      wait_vm<0>();
-      lds_barrier();
+      own_loads();
       dq_tile(dq, 0, dl, l2);
       dkdv_tile(0);
     } else {
       const int kend = CAUSAL ? min(N, r0 + 32) : N;
       for (int kb = 0; kb < kend; kb += 32) {
-        lds_barrier();
+        own_reads();
         load_kv(kb);
-        wait_vm<0>();
-        lds_barrier();
+        own_loads();
         dq_tile(dq, kb, dl, l2);
       }
     }
@@ -266,19 +280,46 @@ __global__ __launch_bounds__(64, D == 128 ? 1 : 2) void short_bwd_kernel(AttnArg
     }
   }
   if (!one) {
-    lds_barrier();
+    own_reads();
     load_kv(r0);
-    for (int h = g * nh; h < g * nh + nh; ++h)
+    for (int h = g * nh + w; h < g * nh + nh; h += W)
       for (int qb = CAUSAL ? r0 : 0; qb < N; qb += 32) {
         float dl, l2;
-        lds_barrier();
+        own_reads();
         load_qg(h, qb);
         stats(h, qb, dl, l2);
         keep_stats(dl, l2);
-        wait_vm<0>();
-        lds_barrier();
+        own_loads();
         dkdv_tile(qb);
       }
+  }
+  if constexpr (W > 1) {
+    // the waves' sums, in order
+    static_assert(2 * DB * 16 * 256 <= LW, "the sums fit a wave's LDS");
+    own_loads();
+    if (w > 0) {
+      float* p = reinterpret_cast<float*>(lds) + lane;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          p[(16 * db + r) * 64] = dk[db][r];
+          p[(16 * (DB + db) + r) * 64] = dv[db][r];
+        }
+    }
+    lds_barrier();
+    if (w > 0) return;
+#pragma unroll 1
+    for (int e = 1; e < W; ++e) {
+      const float* p = reinterpret_cast<const float*>(all + e * LW) + lane;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          dk[db][r] += p[(16 * db + r) * 64];
+          dv[db][r] += p[(16 * (DB + db) + r) * 64];
+        }
+    }
   }
   if (rw < N) {
     bf16_t* dst = a.d_qkv + (tok0 + rw) * ld;
@@ -294,27 +335,42 @@ unsigned short_blocks(const PackedShape& m, int T, int per) {
   return (unsigned)((T / 32 + (long)m.nseq + 1) * per);
 }
 
-}  // namespace
+// Few tiles of a key head leave room for a wave each of up to four of a group's query heads. us of
+// the backward with one wave a block and so: 20 tokens in 2 sequences, 16 heads on 2 of 128 35, 18,
+// on 4 of 64 12, 8; 1000 in 98, 16 on 2 of 128 (258 tiles) 40, 34; 2500 in 252 (650) 51, 68.
+constexpr unsigned kFewTiles = 512;
+template <int D>
+void run_short_fwd(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
+  const dim3 g(short_blocks(m, a.T, m.heads)), b(64);
+  if (m.causal) hipLaunchKernelGGL((short_fwd_kernel<D, true>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((short_fwd_kernel<D, false>), g, b, 0, st, a);
+}
+template <int D, int W>
+void run_short_bwd(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
+  const dim3 g(short_blocks(m, a.T, m.kv)), b(64 * W);
+  if (m.causal) hipLaunchKernelGGL((short_bwd_kernel<D, true, W>), g, b, 0, st, a);
+  else hipLaunchKernelGGL((short_bwd_kernel<D, false, W>), g, b, 0, st, a);
+}
+template <int D>
+void run_short_bwd(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
+  // (few tiles: waves for the heads of a group)
+  const int nh = short_blocks(m, a.T, m.kv) > kFewTiles ? 1 : m.heads / m.kv;
+  if (nh > 2) run_short_bwd<D, 4>(m, a, st);
+  else if (nh > 1) run_short_bwd<D, 2>(m, a, st);
+  else run_short_bwd<D, 1>(m, a, st);
+}
 
-#define FLOWMOE_SHORT_LAUNCH(KERNEL, grid)                                                \
-  do {                                                                                    \
-    const dim3 g(grid), b(64);                                                            \
-    if (m.D == 128) {                                                                     \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<128, true>), g, b, 0, st, a);              \
-      else hipLaunchKernelGGL((KERNEL<128, false>), g, b, 0, st, a);                      \
-    } else {                                                                              \
-      if (m.causal) hipLaunchKernelGGL((KERNEL<64, true>), g, b, 0, st, a);               \
-      else hipLaunchKernelGGL((KERNEL<64, false>), g, b, 0, st, a);                       \
-    }                                                                                     \
-  } while (0)
+}  // namespace
 
 hipError_t launch_short_attn_fwd(const PackedShape& m, int T, const void* qkv,
                                  const int32_t* starts, void* o, float* lse, hipStream_t st) {
   AttnArgs a = packed_args(m, T, qkv, starts);
   a.out = static_cast<bf16_t*>(o);
   a.lse = lse;
-  return traced(FLOWMOE_K_ATTN_FWD, st,
-                [&] { FLOWMOE_SHORT_LAUNCH(short_fwd_kernel, short_blocks(m, T, m.heads)); });
+  return traced(FLOWMOE_K_ATTN_FWD, st, [&] {
+    if (m.D == 128) run_short_fwd<128>(m, a, st);
+    else run_short_fwd<64>(m, a, st);
+  });
 }
 
 hipError_t launch_short_attn_bwd(const PackedShape& m, int T, const void* qkv,
@@ -326,8 +382,10 @@ hipError_t launch_short_attn_bwd(const PackedShape& m, int T, const void* qkv,
   a.d_qkv = static_cast<bf16_t*>(d_qkv);
   a.lse = const_cast<float*>(lse);
   a.delta = delta;
-  return traced(FLOWMOE_K_ATTN_BWD_DKDV, st,
-                [&] { FLOWMOE_SHORT_LAUNCH(short_bwd_kernel, short_blocks(m, T, m.kv)); });
+  return traced(FLOWMOE_K_ATTN_BWD_DKDV, st, [&] {
+    if (m.D == 128) run_short_bwd<128>(m, a, st);
+    else run_short_bwd<64>(m, a, st);
+  });
 }
 
 }  // namespace flowmoe

@@ -42,6 +42,34 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
+// 8 floats of a gain or bias, which may be aligned to 4 bytes only
+__device__ __forceinline__ bool aligned16(const void* p) { return (reinterpret_cast<unsigned long>(p) & 15) == 0; }
+__device__ __forceinline__ void load_param(const float* p, int c, bool on, float other, float v[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = other;
+  if (p == nullptr || !on) return;
+  if (aligned16(p)) {
+    load8(p + c, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = p[c + i];
+  }
+}
+// d = v, or d += v
+__device__ __forceinline__ void store_grad(float* d, int c, const float v[8], bool add) {
+  if (d == nullptr) return;
+  float o[8];
+  if (aligned16(d)) {
+    if (add) load8(d + c, o);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = add ? o[i] + v[i] : v[i];
+    store8(d + c, o);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[c + i] = add ? d[c + i] + v[i] : v[i];
+  }
+}
+
 // a row's vectors as stored, loaded a row ahead of their use
 template <typename T>
 using Raw8 = decltype(raw8_load(static_cast<const T*>(nullptr)));
@@ -83,11 +111,8 @@ __global__ __launch_bounds__((kThreads<L, W>)) void layer_norm_kernel(LnArgs a) 
   for (int v = 0; v < V; ++v) {
     c[v] = 8 * (lane + L * (w + W * v));
     in[v] = c[v] < a.M;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      gn[v][i] = in[v] && a.gain ? a.gain[c[v] + i] : 1.0f;
-      bs[v][i] = in[v] && a.bias ? a.bias[c[v] + i] : 0.0f;
-    }
+    load_param(a.gain, c[v], in[v], 1.0f, gn[v]);
+    load_param(a.bias, c[v], in[v], 0.0f, bs[v]);
   }
   const int nw = part_count<L, W, V>(a.M, w);
   const float rn = nw > 0 ? 1.0f / nw : 0.0f;
@@ -166,13 +191,15 @@ __global__ __launch_bounds__((kThreads<L, W>)) void layer_norm_bwd_kernel(LnArgs
   for (int v = 0; v < V; ++v) {
     c[v] = 8 * (lane + L * (w + W * v));
     in[v] = c[v] < a.M;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float gi = in[v] && a.gain ? a.gain[c[v] + i] : 1.0f;
-      if constexpr (AHEAD) gn[v][i] = gi;
-      else gains[c[v] + i] = gi;
-      dg[v][i] = db[v][i] = 0.0f;
+    if constexpr (AHEAD) {
+      load_param(a.gain, c[v], in[v], 1.0f, gn[v]);
+    } else {
+      float t[8];
+      load_param(a.gain, c[v], in[v], 1.0f, t);
+      store8(gains + c[v], t);
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dg[v][i] = db[v][i] = 0.0f;
   }
   const int nw = part_count<L, W, V>(a.M, w);
   const float rn = nw > 0 ? 1.0f / nw : 0.0f;
@@ -257,7 +284,8 @@ __global__ __launch_bounds__((kThreads<L, W>)) void layer_norm_bwd_kernel(LnArgs
   if (a.part == nullptr && a.dgain == nullptr && a.dbias == nullptr) return;
   // the block's rows side by side, in order
   if constexpr (G > 1) {
-    for (int k = 1; k < G; ++k) {
+    const int groups = (int)min((long)G, a.rows);  // (the others have no rows)
+    for (int k = 1; k < groups; ++k) {
       __syncthreads();
       if (g == k)
 #pragma unroll
@@ -287,11 +315,8 @@ __global__ __launch_bounds__((kThreads<L, W>)) void layer_norm_bwd_kernel(LnArgs
       store8(p, dg[v]);
       store8(p + a.M, db[v]);
     } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (a.dgain) a.dgain[c[v] + i] = (a.accumulate ? a.dgain[c[v] + i] : 0.0f) + dg[v][i];
-        if (a.dbias) a.dbias[c[v] + i] = (a.accumulate ? a.dbias[c[v] + i] : 0.0f) + db[v][i];
-      }
+      store_grad(a.dgain, c[v], dg[v], a.accumulate != 0);
+      store_grad(a.dbias, c[v], db[v], a.accumulate != 0);
     }
   }
 }

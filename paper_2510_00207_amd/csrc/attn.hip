@@ -962,8 +962,8 @@ __global__ __launch_bounds__(256) void attn_delta_kernel(AttnArgs a) {
 }
 
 // dK and dV of the tiles that were cut, their units' sums added in order: a block a tile of
-// 128 rows of a key head and 32 columns of K (blockIdx.y < D / 32) or V
-template <int D, bool CAUSAL>
+// 128 rows of a key head and 32 columns of K (blockIdx.y < D / 32) or V. B units in flight.
+template <int D, bool CAUSAL, int B>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   constexpr int DB = D / 32;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6),
@@ -980,7 +980,6 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const float* p = unit_part(a, sp, 0, row / 32, g, kv, D);
   const long next = (long)a.rows32 * a.kv * 64 * D;
   floatx16 x = zero16();
-  constexpr int B = 8;  // units in flight
   for (int u = 0; u < units; u += B) {
     float4 v[B][4];
 #pragma unroll
@@ -1184,16 +1183,21 @@ hipError_t launch_packed_attn_fwd(const PackedShape& m, int T, const void* qkv,
 
 namespace {
 
+template <int B>
+void run_join(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
+  const dim3 g(packed_blocks(a, 128, m.kv), 2 * m.D / 32), b(256);
+  if (m.D == 128) {
+    if (m.causal) hipLaunchKernelGGL((attn_join_kernel<128, true, B>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((attn_join_kernel<128, false, B>), g, b, 0, st, a);
+  } else {
+    if (m.causal) hipLaunchKernelGGL((attn_join_kernel<64, true, B>), g, b, 0, st, a);
+    else hipLaunchKernelGGL((attn_join_kernel<64, false, B>), g, b, 0, st, a);
+  }
+}
 hipError_t join_packed(const PackedShape& m, const AttnArgs& a, hipStream_t st) {
   return traced(FLOWMOE_K_PACKED_JOIN, st, [&] {
-    const dim3 g(packed_blocks(a, 128, m.kv), 2 * m.D / 32), b(256);
-    if (m.D == 128) {
-      if (m.causal) hipLaunchKernelGGL((attn_join_kernel<128, true>), g, b, 0, st, a);
-      else hipLaunchKernelGGL((attn_join_kernel<128, false>), g, b, 0, st, a);
-    } else {
-      if (m.causal) hipLaunchKernelGGL((attn_join_kernel<64, true>), g, b, 0, st, a);
-      else hipLaunchKernelGGL((attn_join_kernel<64, false>), g, b, 0, st, a);
-    }
+    if (a.units <= 2) run_join<2>(m, a, st);
+    else run_join<8>(m, a, st);
   });
 }
 

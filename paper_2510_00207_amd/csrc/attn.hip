@@ -32,14 +32,15 @@
 namespace flowmoe {
 namespace {
 
-// Units of the packed backward's long key tiles: a launch's steps are cut into about kUnits,
-// of at least kUnitSteps steps. us of the whole backward uncut and with 230, 460, 700, 1000
-// units: one sequence of 2031, 16 heads on 2 of 128, causal 696, 148, 149, 152, 150; one of
-// 16384, 8 on 1 6340, 2582, 2503, 2039, 2064; one of 4096, 16 on 16 342, 327, 322, 312, 331;
-// 16384 tokens in 12 of 46 to 8021, 32 on 8 2725, 2738, 2702, 2649, 2545, in 18 of 76 to 5801
-// 1809, 1843, 1728, 1644, 1653. With steps of at least 8, 16, 32: the first 148, 152, 142; 1000
-// tokens in 5, 8 on 2 of 64 30, 37, 47.
-constexpr int kUnits = 850, kUnitSteps = 16;
+// Units of the packed backward's long key tiles: a launch's steps are cut into about kUnits, of
+// at least 16 steps, or of 8 where it has few. us of the whole backward with 500, 850, 1300 and
+// 2000 units (uncut, of an earlier version, in brackets): one sequence of 2031, 16 heads on 2 of 128,
+// causal 107, 103, 104, 104 (696); one of 4096, 16 on 16 277, 294, 298, 321 (342); of 16384, 8 on 1
+// 1881, 1893, 1892, 1886 (6340); 16384 tokens in 12 of 46 to 8021, 32 on 8 2314, 2340, 2300, 2310
+// (2725), in 18 of 76 to 5801 1545, 1556, 1605, 1599 (1809). Of at least 8, 16 and 32 steps: the
+// first 112, 103, 124; 1000 tokens in 5, 8 on 2 of 64 23, 35, 39; one of 512, 16 on 4 24, 30, 44;
+// of 1024, 32 on 8 of 128 74, 71, 74.
+constexpr int kUnits = 850, kMinSteps = 8;
 
 // block -> (query or key tile, head, sequence). Blocks are dispatched in
 // order; u = blockIdx / (heads x sequences) ranks the tiles by their causal
@@ -90,7 +91,8 @@ __device__ __forceinline__ int unit_steps(const AttnArgs& a, bool causal, int la
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
   sum *= a.heads;  // (kv heads, of heads / kv query heads each)
   // (uniform, and known to be: the loops' bounds come from it)
-  return __builtin_amdgcn_readfirstlane((int)max((long)kUnitSteps, min((sum + kUnits - 1) / kUnits, 1L << 30)));
+  return __builtin_amdgcn_readfirstlane(
+      sum <= 2 * kUnits ? kMinSteps : (int)max(2L * kMinSteps, min((sum + kUnits - 1) / kUnits, 1L << 30)));
 }
 // Units of a tile of `steps` steps (at most `most`), and the steps of each
 __device__ __forceinline__ int tile_units(int steps, int unit, int most, int& len) {
@@ -748,7 +750,7 @@ __device__ __forceinline__ void dkdv_rows(const AttnArgs& a, char* lds, unsigned
     }
     const int steps = key_steps(N, sp.tile, nh, CAUSAL);
     it1 = steps;
-    if (a.units > 1 && steps > kUnitSteps) {
+    if (a.units > 1 && steps > kMinSteps) {
       int len;
       units = tile_units(steps, unit_steps(a, CAUSAL, lane), a.units, len);
       it0 = unit * len;
@@ -972,7 +974,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   Span sp;
   if (!locate(a, (int)(blockIdx.x / a.kv), 128, false, lane, sp) || sp.none) return;
   const int steps = key_steps(sp.N, sp.tile, a.heads / a.kv, CAUSAL);
-  if (steps <= kUnitSteps) return;
+  if (steps <= kMinSteps) return;
   int len;
   const int units = tile_units(steps, unit_steps(a, CAUSAL, lane), a.units, len);
   const int row = 128 * sp.tile + 32 * w;
@@ -1136,7 +1138,7 @@ void packed_units(const PackedShape& m, int T, AttnArgs& a) {
   const long rows32 = T / 32 + (long)m.nseq + 1, steps = (T + 31) / 32 * (m.heads / m.kv);
   const long most = (262144L * 128 / m.D + rows32 * 32 * m.kv - 1) / (rows32 * 32 * m.kv);
   a.rows32 = (int)rows32;
-  a.units = m.nseq > 4096 || steps <= 40 ? 1 : (int)std::min(most, 32L);
+  a.units = m.nseq > 4096 || steps <= 2 * kMinSteps ? 1 : (int)std::min(most, 32L);
 }
 size_t part_bytes(const PackedShape& m, const AttnArgs& a) {
   return a.units > 1 ? (size_t)a.units * a.rows32 * m.kv * 64 * m.D * sizeof(float) : 0;

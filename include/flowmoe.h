@@ -318,8 +318,9 @@ enum {
   FLOWMOE_K_EMBED_SORT = 35,      /* embedding gradient: the tokens by id */
   FLOWMOE_K_EMBED_BWD = 36,       /* embedding gradient: sums of the tokens' rows */
   FLOWMOE_K_PACKED_JOIN = 37      /* attention over packed sequences, backward: sums of
-                                     partial dK, dV (its other kernels are of the kinds
-                                     FLOWMOE_K_ATTN_FWD, _BWD_DQ and _BWD_DKDV) */
+                                     partial dK, dV (its forward is FLOWMOE_K_ATTN_FWD, its
+                                     delta FLOWMOE_K_ATTN_BWD_DQ, dQ, dK and dV, one launch,
+                                     FLOWMOE_K_ATTN_BWD_DKDV) */
 };
 
 /* Start tracing on the calling host thread: every later kernel launch whose
@@ -660,7 +661,9 @@ flowmoe_status_t flowmoe_diff_mha_bwd(const flowmoe_shape_t* shape,
  * query heads that share key/value heads. shape->M = heads * head_dim; qkv rows hold
  * W = M + 2 * kv_heads * head_dim elements, [Q | K | V], and query head h reads key head
  * h / (heads / kv_heads). bf16 only; 16-byte aligned; only shape->T, M (at most 2^21) and
- * dtype are used. */
+ * dtype are used. heads times (T / 32 + 2 nseq + 2) stay below 2^24. A call's blocks depend on
+ * its sizes, and in the backward on the lengths: the same sequence in another batch may be
+ * summed in another order. */
 typedef struct {
   int32_t nseq;     /* sequences, >= 0 */
   int32_t heads;

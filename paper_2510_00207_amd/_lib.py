@@ -552,6 +552,8 @@ def kind_mask(names) -> int:
 
 def flowmoe_trace_start(events, kinds, pairs: int, mask: int):
     """events: ctypes array of 2*pairs hipEvent_t; kinds: ctypes int32 array."""
+    if mask >> 32:
+        raise ValueError("the mask names kinds past 31: flowmoe_trace_start64 takes them")
     _check(load().flowmoe_trace_start(ctypes.cast(events, ctypes.c_void_p),
                                       ctypes.cast(kinds, ctypes.c_void_p), pairs, mask))
 

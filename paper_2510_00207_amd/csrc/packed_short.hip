@@ -7,7 +7,9 @@
 // key head: dQ^T += K^T dS^T over the key tiles, then dV^T += dO^T P and dK^T += Q^T dS over
 // the query tiles; of a sequence of one tile K, V, Q and dO are loaded once for both.
 //
-// Latency bounds it: a wave waits for its loads, its scores, its softmax, its products in turn.
+// Latency bounds it: a wave waits for its loads, its scores, its softmax, its products in turn. 5000
+// tokens in 840 sequences of 1 to 12, 16 heads on 4 of 128: forward 40 us (185 in blocks of 128
+// rows), backward 136 (351); 259 in 26 of up to 71, 4 on 2 of 64: 5 and 11.
 #include <math.h>
 
 #include "attn_tiles.hpp"

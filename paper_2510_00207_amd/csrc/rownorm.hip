@@ -3,7 +3,8 @@
 //   y = n gain + bias,
 // and its gradients, with u = dy gain:
 //   dh = r (u - mean(u) - n mean(u n)) (+ d_sum), dgain = sum of dy n, dbias = sum of dy.
-// HBM bounds both: about ten operations an element.
+// HBM bounds both: about ten operations an element. 16384 rows of 4096 bf16 with a residual (537
+// MB): forward 93 us, 5.8 TB/s, backward 100, 5.4, with the join's 5.
 //
 // A row is W waves, V vectors of 8 elements a thread, all in registers, so that every
 // element is read once and the squares are of deviations from the mean. The waves of a row
@@ -70,7 +71,8 @@ __device__ __forceinline__ void store_grad(float* d, int c, const float v[8], bo
   }
 }
 
-// a row's vectors as stored, loaded a row ahead of their use
+// a row's vectors as stored, loaded a row ahead of their use (the forward above 125 -> 101 us, the
+// backward 155 -> 102)
 template <typename T>
 using Raw8 = decltype(raw8_load(static_cast<const T*>(nullptr)));
 template <typename T, int V>
@@ -357,12 +359,17 @@ int ln_waves(int M) {
   return w;
 }
 
+// Blocks: as many as have 4 MB of rows in flight (each a row or a few, and the next), at least
+// one to a CU. us of the forward and backward with 256, 512, 1024 and 2048 blocks: 16384 x 4096
+// bf16 131, 102, 110, 109 and 146, 103, 120, 127; f32 208, 259, 253, 233 and 211, 221, 224, 230;
+// 65536 x 256 bf16 82, 48, 32, 33 and 88, 52, 39, 44.
 int ln_blocks(long rows, int M, int es, int most) {
   const int lw = ln_lanes(M) * ln_waves(M);
   const long per = std::max(256 / lw, 1), need = (rows + per - 1) / per;
   const long fill = std::min(std::max((4L << 20) / (per * M * es), 256L), (long)most);
   return (int)std::min(need, fill);
 }
+// (up to four steps of one block need no join: a launch)
 int ln_bwd_blocks(long rows, int M, int es) {
   const int n = ln_blocks(rows, M, es, 1024);
   return n <= 4 ? 1 : n;

@@ -94,6 +94,57 @@ def test_more_rows_than_blocks():
     c.check_bwd()
 
 
+def test_rows_past_32_bit_offsets():
+    """More than 2^31 elements: the last rows, and the sums over all."""
+    T, M = 530000, 4096
+    c = Case(8, M, res=False)
+    x = c.x.repeat(T // 8, 1)
+    dy = c.dy.repeat(T // 8, 1)
+    s = L.make_shape(T, M, 8, 1, 1, 0)
+    y = torch.zeros_like(x)
+    L.flowmoe_layer_norm_fwd(s, EPS, x, None, c.gain, c.bias, None, y)
+    c.fwd()
+    assert torch.equal(y[-8:], c.y) and torch.equal(y[T // 2:T // 2 + 8], c.y)
+    n = L.flowmoe_layer_norm_ws_bytes(s)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev())
+    L.flowmoe_layer_norm_bwd(s, EPS, x, c.gain, dy, None, y, c.dgain, c.dbias, False, ws, n)
+    got, db = c.dgain.clone(), c.dbias.clone()
+    c.bwd()
+    assert torch.equal(y[-8:], c.dx) and torch.equal(y[T // 2:T // 2 + 8], c.dx)
+    # T / 8 times the eight rows' sums: T 2^-24 of the magnitudes
+    _, dg, dbr, mg, mb, _ = R.layer_norm_bwd(c.x, c.gain, c.dy, None, EPS)
+    within(got, dg * (T // 8), (T + 20) * E24 * mg * (T // 8) + 1e-3 * mg)
+    within(db, dbr * (T // 8), (T + 20) * E24 * mb * (T // 8))
+
+
+def test_trace_of_kinds_past_31():
+    from paper_2510_00207_amd.hiprt import EventArray
+    c = Case(3000, 512)
+    ev = EventArray(8)
+    L.flowmoe_trace_start64(ev.ev, ev.kinds, ev.pairs, L.kind_mask(["layer_norm", "layer_norm_bwd"]))
+    c.fwd()
+    c.bwd()
+    n = L.flowmoe_trace_stop()
+    assert [L.K_NAMES[k] for k in ev.kinds[:n]] == ["layer_norm", "layer_norm_bwd", "layer_norm_bwd"]
+    assert all(ev.elapsed_ms(i) > 0 for i in range(n))
+    ev.close()
+
+
+def test_unaligned_parameters():
+    """Gains, biases and their gradients at 4 bytes past a 16-byte boundary."""
+    for T, M in ((3, 40), (2000, 1032), (5, 8200)):
+        c = Case(T, M)
+        c.fwd()
+        c.bwd()
+        want = [t.clone() for t in (c.y, c.dx, c.dgain, c.dbias)]
+        off = lambda t: torch.cat([t.new_zeros(1), t])[1:]
+        c.gain, c.bias, c.dgain, c.dbias = (off(t) for t in (c.gain, c.bias, c.dgain, c.dbias))
+        assert c.gain.data_ptr() % 16 == 4 and c.dgain.data_ptr() % 16 == 4
+        c.fwd()
+        c.bwd()
+        assert all(torch.equal(t, w) for t, w in zip((c.y, c.dx, c.dgain, c.dbias), want))
+
+
 def test_large_mean():
     """Deviations far below the mean: the squares are of deviations, not of the values."""
     c = Case(40, 1000, "f32", mean=1000.0, std=1.0)

@@ -64,6 +64,7 @@ class Case:
         c = (self.lens, self.heads, self.kv, self.D, self.causal)
         d, rnd, mag = R.attention_bwd(self.qkv, *c, self.attn, self.lse, self.d_attn)
         within(self.d_qkv, d, HALF * rnd + 2.0 ** -10 * mag + HALF * d.abs())
+        assert not self.delta[:, self.live:].any()
 
     def check(self):
         self.fwd()
@@ -131,22 +132,42 @@ def test_heads(heads, kv):
     Case([200, 90], heads, kv, 64, True, 5).check()
 
 
-def test_sequences_do_not_meet():
+@pytest.mark.parametrize("lens", [[40, 30, 70, 5], [20, 10, 30, 5], [900, 700, 600, 40]])
+@pytest.mark.parametrize("causal", [True, False])
+def test_sequences_do_not_meet(lens, causal):
     """A sequence of infinities and NaN changes no other's rows, bit for bit."""
-    lens = [40, 30, 70, 5]
-    for causal in (True, False):
-        a = Case(lens, 4, 2, 64, causal, poison=False)
-        a.fwd()
-        a.bwd()
-        want = [t.clone() for t in (a.attn, a.lse, a.d_qkv)]
-        b = Case(lens, 4, 2, 64, causal, poison=False)
-        b.qkv[40:70:2] = float("nan")
-        b.qkv[41:70:2] = float("inf")
-        b.d_attn[40:70] = float("nan")
-        b.fwd()
-        b.bwd()
-        for t, w in zip((b.attn, b.lse.T, b.d_qkv), (want[0], want[1].T, want[2])):
-            assert torch.equal(t[:40], w[:40]) and torch.equal(t[70:], w[70:])
+    lo, hi = lens[0], lens[0] + lens[1]
+    a = Case(lens, 4, 1, 64, causal, poison=False)
+    a.fwd()
+    a.bwd()
+    want = [t.clone() for t in (a.attn, a.lse, a.d_qkv)]
+    b = Case(lens, 4, 1, 64, causal, poison=False)
+    b.qkv[lo:hi:2] = float("nan")
+    b.qkv[lo + 1:hi:2] = float("inf")
+    b.d_attn[lo:hi] = float("nan")
+    b.fwd()
+    b.bwd()
+    for t, w in zip((b.attn, b.lse.T, b.d_qkv), (want[0], want[1].T, want[2])):
+        assert torch.equal(t[:lo], w[:lo]) and torch.equal(t[hi:], w[hi:])
+
+
+def test_rows_past_32_bit_offsets():
+    """[Q | K | V] of more than 2^31 elements: the last sequences' rows."""
+    n, T = 1500, 360000
+    lens = [n] * (T // n - 1) + [n - 77]
+    c = Case(lens, 32, 8, 128, True, 77, poison=False)
+    assert c.qkv.numel() > 1 << 31
+    c.fwd()
+    c.bwd()
+    lo, hi = c.live - lens[-1], c.live
+    a = ([lens[-1]], 32, 8, 128, True)
+    ref, lse, mag, smax = R.attention(c.qkv[lo:hi], *a)
+    within(c.attn[lo:hi], ref, (HALF + 2.0 ** -12) * mag + HALF * ref.abs())
+    within(c.lse[:, lo:hi], lse, 128 * 2.0 ** -24 * smax + 2.0 ** -20 + 2.0 ** -22 * lse.abs())
+    d, rnd, mag = R.attention_bwd(c.qkv[lo:hi], *a, c.attn[lo:hi], c.lse[:, lo:hi], c.d_attn[lo:hi])
+    within(c.d_qkv[lo:hi], d, HALF * rnd + 2.0 ** -10 * mag + HALF * d.abs())
+    for t in (c.attn, c.d_qkv):
+        assert not t[hi:].any()
 
 
 def test_equal_lengths_match_the_attention():
@@ -206,7 +227,7 @@ def test_graph_follows_its_inputs():
         other = Case(lens, 4, 2, 64, True, 517 - sum(lens), seed=i)
         for n in ("qkv", "starts", "d_attn"):
             getattr(c, n).copy_(getattr(other, n))
-        c.lens = lens
+        c.lens, c.live = lens, sum(lens)
         graph.replay()
         torch.cuda.synchronize()
         c.check_fwd()

@@ -196,4 +196,6 @@ def test_trace_mask_of_64_bits(flowmoe_lib):
     L.flowmoe_trace_start64(None, None, 0, (1 << 64) - 1)
     assert L.flowmoe_trace_stop() == 0
     assert L.kind_mask(["layer_norm", "embed"]) == (1 << 32) | (1 << 34)
+    with pytest.raises(ValueError, match="trace_start64"):  # (ctypes would cut it to 32 bits)
+        L.flowmoe_trace_start(None, None, 0, L.kind_mask(["layer_norm"]))
     assert ctypes.sizeof(L.PackedMhaBufs) == 8 * (len(L._PACKED_MHA_FIELDS) + 1)

@@ -1129,11 +1129,19 @@ hipError_t launch_attn_bwd(const AttnShape& m, int T, int M, const void* qkv, co
 // ---------------------------------------------------------------------------
 namespace {
 
-// Sequences so short on average that a wave a tile of 32 rows serves them best
-// (packed_short.hip)? us with it and without: 5000 tokens in 840 of 1 to 12, 16 heads on 4 of
-// 128 40, 185, backward 137, 351; 259 in 26 of 0 to 71, 4 on 2 of 64 6, 6 and 17, 17; 1000 in 5 of
-// 100 to 300, 8 on 2 of 64 7, 8 and 55, 37; 8192 in 51 of 20 to 600, 16 of 64 35, 30.
-bool packed_short(const PackedShape& m, int T) { return T <= 32L * m.nseq; }
+// Sequences so short on average that a wave a tile of 32 rows serves them best (packed_short.hip)?
+// Up to 96 rows forward, 48 backward, 24 where a wave there walks more than two heads. The host
+// knows the average alone, and a wave's walk over a long sequence is slow. us in blocks of 128
+// rows and so, causal, 8 heads on 4 of 64, 16 on 16 and 32 on 4 of 128: forward of 8000 tokens in
+// sequences of 32 13, 11; 50, 40; 93, 40; of 64 11, 8; 35, 28; 59, 41; of 128 11, 9; 47, 31; 50, 44; 6000
+// in sequences of 1 to 500 13, 14; 35, 32; 57, 47; of 4000 and 100 of 20 54, 79; 96, 151; 164, 189.
+// Backward of 8000 of 24 81, 19; 132, 80; 201, 150; of 32 68, 27; 157, 123; 167, 179; of 64 52, 24; 122,
+// 90; 145, 140; 6000 of 40 to 120 49, 29; 105, 84; 142, 163; of 1 to 500 56, 62; 113, 114; 165, 376; of
+// 4000 and 100 of 20 (59 on average) 170, 437; 313, 598; 534, 2723.
+bool packed_short_fwd(const PackedShape& m, int T) { return T <= 96L * m.nseq; }
+bool packed_short_bwd(const PackedShape& m, int T) {
+  return T <= (m.heads / m.kv <= 2 ? 48L : 24L) * m.nseq;
+}
 
 // blocks of a packed grid: its slots (locate) times `per` heads
 unsigned packed_blocks(const AttnArgs& a, int rows, int per) {
@@ -1158,7 +1166,7 @@ size_t part_bytes(const PackedShape& m, const AttnArgs& a) {
 size_t packed_attn_ws_bytes(const PackedShape& m, int T) {
   AttnArgs a = {};
   packed_units(m, T, a);
-  return T == 0 || packed_short(m, T) ? 0 : part_bytes(m, a);
+  return T == 0 || packed_short_bwd(m, T) ? 0 : part_bytes(m, a);
 }
 
 template <int D, int S>
@@ -1179,7 +1187,7 @@ bool packed_split(const PackedShape& m, const AttnArgs& a) {
 hipError_t launch_packed_attn_fwd(const PackedShape& m, int T, const void* qkv,
                                   const int32_t* starts, void* o, float* lse, hipStream_t st) {
   if (T == 0) return hipSuccess;
-  if (packed_short(m, T)) return launch_short_attn_fwd(m, T, qkv, starts, o, lse, st);
+  if (packed_short_fwd(m, T)) return launch_short_attn_fwd(m, T, qkv, starts, o, lse, st);
   AttnArgs a = packed_args(m, T, qkv, starts);
   a.out = static_cast<bf16_t*>(o);
   a.lse = lse;
@@ -1219,7 +1227,7 @@ hipError_t launch_packed_attn_bwd(const PackedShape& m, int T, const void* qkv,
                                   const void* d_o, void* d_qkv, float* delta, void* ws,
                                   hipStream_t st) {
   if (T == 0) return hipSuccess;
-  if (packed_short(m, T))
+  if (packed_short_bwd(m, T))
     return launch_short_attn_bwd(m, T, qkv, starts, o, lse, d_o, d_qkv, delta, st);
   AttnArgs a = packed_args(m, T, qkv, starts);
   a.o = static_cast<const bf16_t*>(o);

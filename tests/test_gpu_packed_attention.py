@@ -132,7 +132,8 @@ def test_heads(heads, kv):
     Case([200, 90], heads, kv, 64, True, 5).check()
 
 
-@pytest.mark.parametrize("lens", [[40, 30, 70, 5], [20, 10, 30, 5], [900, 700, 600, 40]])
+@pytest.mark.parametrize("lens", [[40, 30, 70, 5], [20, 10, 30, 5], [130, 60, 300, 100],
+                                  [900, 700, 600, 40]])
 @pytest.mark.parametrize("causal", [True, False])
 def test_sequences_do_not_meet(lens, causal):
     """A sequence of infinities and NaN changes no other's rows, bit for bit."""

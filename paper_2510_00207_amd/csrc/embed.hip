@@ -6,8 +6,7 @@
 // gradient needs a row's tokens side by side: a stable radix sort of (id, t) by 8 bits a pass, then
 // sums of equally many tokens a wave, so that an id of thousands of tokens holds no wave up (a
 // wave a few rows of the table, each walking its tokens: 32768 x 2048 of 50021 rows 442 us; so
-// 143, of which the sums and the rows without tokens 103 at 5.3 TB/s, four launches of the sort
-// 20, the join 11).
+// 139, of which the sums, the joins and the rows without tokens 113, the sort's four launches 20).
 #include <algorithm>
 
 #include "common.hpp"
@@ -305,7 +304,13 @@ __device__ __forceinline__ void zero_absent(const EmbedArgs& a, long v0, int lan
   }
 }
 
-// waves 0 .. chunks * slabs - 1: the chunks; the others: the rows without tokens
+// Waves 0 .. chunks * slabs - 1: the chunks' sums, then their joins; the others look after the rows
+// without tokens, in the launch of the joins where that is worth two long launches (C 32: they
+// hide the joins' latencies, 16384 tokens of one id, 32000 rows of 1024, 104 us of 111), else in
+// that of the sums, so that the joins' stays small (1024 tokens of 1024, 1000 rows: 16 us of 17).
+template <int C>
+constexpr bool kZeroInJoin = C > 8;
+
 template <typename T, int C, bool ADD, bool NT>
 __global__ __launch_bounds__(256) void embed_bwd_kernel(EmbedArgs a) {
   const int lane = threadIdx.x & 63, slabs = (a.M + 511) / 512;
@@ -313,18 +318,15 @@ __global__ __launch_bounds__(256) void embed_bwd_kernel(EmbedArgs a) {
   const long sums = ((long)a.T + C - 1) / C * slabs;
   if (u < sums) {
     sum_chunk<T, C, ADD, NT>(a, (int)(u / slabs), (int)(u % slabs) * 512 + 8 * lane, lane);
-  } else if constexpr (!ADD) {
+  } else if constexpr (!ADD && !kZeroInJoin<C>) {
     const long v0 = (u - sums) * a.rows;
     if (v0 < a.V) zero_absent<NT>(a, v0, lane);
   }
 }
 
-// runs that cross chunks: the wave of the chunk where one begins adds up its parts
+// a run that crosses chunks: the wave of the chunk ch where it begins adds up its parts
 template <int C, bool ADD>
-__global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a) {
-  const int lane = threadIdx.x & 63, slabs = (a.M + 511) / 512;
-  const long u = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int ch = (int)(u / slabs), c = (int)(u % slabs) * 512 + 8 * lane;
+__device__ __forceinline__ void join_chunk(const EmbedArgs& a, int ch, int c, int lane) {
   const long p = (long)ch * C;
   if (p + C >= a.T) return;
   const int id = a.ids[p + C - 1];
@@ -353,6 +355,19 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc[i] = ADD ? old[i] + a.scale * acc[i] : a.scale * acc[i];
   if (on) store8(a.dtable + (long)id * a.M + c, acc);
+}
+
+template <int C, bool ADD, bool NT>
+__global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a) {
+  const int lane = threadIdx.x & 63, slabs = (a.M + 511) / 512;
+  const long u = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long sums = ((long)a.T + C - 1) / C * slabs;
+  if (u < sums) {
+    join_chunk<C, ADD>(a, (int)(u / slabs), (int)(u % slabs) * 512 + 8 * lane, lane);
+  } else if constexpr (!ADD && kZeroInJoin<C>) {
+    const long v0 = (u - sums) * a.rows;
+    if (v0 < a.V) zero_absent<NT>(a, v0, lane);
+  }
 }
 
 // ---- host -------------------------------------------------------------------------------
@@ -494,9 +509,10 @@ hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const i
     a.part = reinterpret_cast<float*>(base + w.part);
   }
   a.rows = embed_rows(M, V);
-  const dim3 g((unsigned)((embed_waves(T, M, V, accumulate) + 3) / 4)), b(256);
-  const bool nt = (long)V * M * 4 >= (256L << 20);
-  const bool few = embed_chunk(T) == 8;
+  const bool nt = (long)V * M * 4 >= (256L << 20), few = embed_chunk(T) == 8;
+  const dim3 gz((unsigned)((embed_waves(T, M, V, accumulate) + 3) / 4));
+  const dim3 gs((unsigned)((embed_waves(T, M, V, true) + 3) / 4)), b(256);
+  const dim3 g = few ? gz : gs, gj = few ? gs : gz;
   const hipError_t e = traced(FLOWMOE_K_EMBED_BWD, st, [&] {
 #define FLOWMOE_EMBED_BWD(T, C)                                                                 \
   if (accumulate) hipLaunchKernelGGL((embed_bwd_kernel<T, C, true, false>), g, b, 0, st, a);    \
@@ -514,11 +530,11 @@ hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const i
   });
   if (e != hipSuccess || T <= embed_chunk(T)) return e;
   return traced(FLOWMOE_K_EMBED_BWD, st, [&] {
-    const dim3 gj((unsigned)((embed_waves(T, M, V, true) + 3) / 4));
-    if (few && accumulate) hipLaunchKernelGGL((embed_join_kernel<8, true>), gj, b, 0, st, a);
-    else if (few) hipLaunchKernelGGL((embed_join_kernel<8, false>), gj, b, 0, st, a);
-    else if (accumulate) hipLaunchKernelGGL((embed_join_kernel<32, true>), gj, b, 0, st, a);
-    else hipLaunchKernelGGL((embed_join_kernel<32, false>), gj, b, 0, st, a);
+    if (few && accumulate) hipLaunchKernelGGL((embed_join_kernel<8, true, false>), gj, b, 0, st, a);
+    else if (few) hipLaunchKernelGGL((embed_join_kernel<8, false, false>), gj, b, 0, st, a);
+    else if (accumulate) hipLaunchKernelGGL((embed_join_kernel<32, true, false>), gj, b, 0, st, a);
+    else if (nt) hipLaunchKernelGGL((embed_join_kernel<32, false, true>), gj, b, 0, st, a);
+    else hipLaunchKernelGGL((embed_join_kernel<32, false, false>), gj, b, 0, st, a);
   });
 }
 

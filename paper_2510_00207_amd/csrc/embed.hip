@@ -22,7 +22,7 @@ struct EmbedArgs {
   void* y;
   float* dtable;
   float* part;  // the runs' parts
-  int T, M, V, rows;
+  int T, M, V, rows, groups;
   float scale;
 };
 
@@ -304,24 +304,12 @@ __device__ __forceinline__ void zero_absent(const EmbedArgs& a, long v0, int lan
   }
 }
 
-// Waves 0 .. chunks * slabs - 1: the chunks' sums, then their joins; the others look after the rows
-// without tokens, in the launch of the joins where that is worth two long launches (C 32: they
-// hide the joins' latencies, 16384 tokens of one id, 32000 rows of 1024, 104 us of 111), else in
-// that of the sums, so that the joins' stays small (1024 tokens of 1024, 1000 rows: 16 us of 17).
-template <int C>
-constexpr bool kZeroInJoin = C > 8;
-
 template <typename T, int C, bool ADD, bool NT>
 __global__ __launch_bounds__(256) void embed_bwd_kernel(EmbedArgs a) {
   const int lane = threadIdx.x & 63, slabs = (a.M + 511) / 512;
   const long u = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const long sums = ((long)a.T + C - 1) / C * slabs;
-  if (u < sums) {
+  if (u < ((long)a.T + C - 1) / C * slabs)
     sum_chunk<T, C, ADD, NT>(a, (int)(u / slabs), (int)(u % slabs) * 512 + 8 * lane, lane);
-  } else if constexpr (!ADD && !kZeroInJoin<C>) {
-    const long v0 = (u - sums) * a.rows;
-    if (v0 < a.V) zero_absent<NT>(a, v0, lane);
-  }
 }
 
 // a run that crosses chunks: the wave of the chunk ch where it begins adds up its parts
@@ -357,6 +345,8 @@ __device__ __forceinline__ void join_chunk(const EmbedArgs& a, int ch, int c, in
   if (on) store8(a.dtable + (long)id * a.M + c, acc);
 }
 
+// Waves 0 .. chunks * slabs - 1 join runs; the others clear the rows without tokens, which hides
+// the joins' latencies (16384 tokens of one id, 32000 rows of 1024: 104 us, beside the sums 111).
 template <int C, bool ADD, bool NT>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a) {
   const int lane = threadIdx.x & 63, slabs = (a.M + 511) / 512;
@@ -364,13 +354,115 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a) {
   const long sums = ((long)a.T + C - 1) / C * slabs;
   if (u < sums) {
     join_chunk<C, ADD>(a, (int)(u / slabs), (int)(u % slabs) * 512 + 8 * lane, lane);
-  } else if constexpr (!ADD && kZeroInJoin<C>) {
+  } else if constexpr (!ADD) {
     const long v0 = (u - sums) * a.rows;
     if (v0 < a.V) zero_absent<NT>(a, v0, lane);
   }
 }
 
+// ---- very few tokens ----------------------------------------------------------------------
+// In one launch, without a sort: `groups` blocks a token look, by all ids (I a thread), whether it
+// is the first of its id and sum its id's rows if so, the columns shared out among them: 512 a
+// wave, eight rows in flight; of a long run waves sum parts, which are added up in order. The
+// other blocks clear the rows without tokens, `rows` of them each. us of 1000 f32 tokens of 264,
+// 5003 rows: 6.6 (launches of a sort, the sums and the joins: 15), five of them a launch's least.
+constexpr int kFewWaves = 8;  // (1000 tokens of 264, 4, 8 and 16 waves: 8.4, 7.5, 12.9 us)
+template <typename T, int I, bool ADD, bool NT>
+__global__ __launch_bounds__(64 * kFewWaves) void embed_few_kernel(EmbedArgs a) {
+  constexpr int W = kFewWaves, B = 8;
+  __shared__ int list[64 * W * I];  // the id's tokens, or which rows have tokens
+  __shared__ int cnt[W * I];
+  __shared__ __attribute__((aligned(16))) float part[W][512];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int t = blockIdx.x / a.groups, s0 = blockIdx.x % a.groups;
+  int ids[I];
+#pragma unroll
+  for (int k = 0; k < I; ++k) ids[k] = tid + 64 * W * k < a.T ? a.ids[tid + 64 * W * k] : -1;
+  if (t >= a.T) {
+    if constexpr (!ADD) {
+      const long v0 = (blockIdx.x - (long)a.T * a.groups) * a.rows;
+      const int n = (int)min((long)a.rows, a.V - v0), per = a.M / 4;
+      for (int u = tid; u < n; u += 64 * W) list[u] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < I; ++k)
+        if (ids[k] >= v0 && ids[k] < v0 + n) list[ids[k] - v0] = 1;
+      __syncthreads();
+      for (int u = tid; u < n * per; u += 64 * W)
+        if (list[u / per] == 0)
+          st16<NT>(reinterpret_cast<u32x4v_t*>(a.dtable + v0 * a.M + 4L * u), u32x4v_t{0, 0, 0, 0});
+    }
+    return;
+  }
+  const int id = a.ids[t];
+  if (id < 0 || id >= a.V) return;
+  unsigned long same[I];
+  bool before = false;
+#pragma unroll
+  for (int k = 0; k < I; ++k) {
+    same[k] = __ballot(ids[k] == id);
+    before = before || (ids[k] == id && tid + 64 * W * k < t);
+    if (lane == 0) cnt[W * k + w] = __popcll(same[k]);
+  }
+  if (__syncthreads_or(before)) return;
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < I; ++k)
+#pragma unroll
+    for (int u = 0; u < W; ++u) {
+      if (u == w && ids[k] == id) list[n + __popcll(same[k] & ((1ul << lane) - 1))] = tid + 64 * W * k;
+      n += cnt[W * k + u];
+    }
+  n = __builtin_amdgcn_readfirstlane(n);
+  __syncthreads();
+  int P = 1;
+  while (P < W && n > 8 * P) P *= 2;
+  const int p = w & (P - 1);
+  const int k0 = (int)((long)n * p / P), k1 = (int)((long)n * (p + 1) / P);
+  for (int c0 = 512 * (W / P) * s0; c0 < a.M; c0 += 512 * (W / P) * a.groups) {
+    const int c = c0 + 512 * (w / P) + 8 * lane;
+    const bool on = c < a.M;
+    float acc[8] = {}, old[8] = {};
+    float* const row = a.dtable + (long)id * a.M + c;
+    if (ADD && on && p == 0) load8(row, old);
+    for (int k = k0; k < k1; k += B) {
+      float v[B][8] = {};
+#pragma unroll
+      for (int u = 0; u < B; ++u) {
+        const long j = __builtin_amdgcn_readfirstlane(list[min(k + u, k1 - 1)]);
+        if (on && k + u < k1) load8(static_cast<const T*>(a.dy) + j * a.M + c, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < B; ++u)
+        if (k + u < k1)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] += v[u][i];
+    }
+    if (P > 1) {
+      if (p > 0) store8(part[w] + 8 * lane, acc);
+      __syncthreads();
+      if (p == 0)
+        for (int e = 1; e < P; ++e) {
+          float v[8];
+          load8(part[w + e] + 8 * lane, v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] += v[i];
+        }
+      __syncthreads();
+    }
+    if (p > 0 || !on) continue;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = ADD ? old[i] + a.scale * acc[i] : a.scale * acc[i];
+    store8_t<NT>(row, acc);
+  }
+}
+
 // ---- host -------------------------------------------------------------------------------
+// us so and with a sort: 512 tokens of 1024, 1000 rows 7, 13, 1000 of 2048, 5003 rows 15, 20, of
+// 1024, 32000 rows 26, 33. Only a run of most of the tokens is slow, as one or two CUs read it:
+// 512 tokens of one id, 32000 rows of 1024 34, 35, 1000 60, 43, added to the gradient 29, 26;
+// 2000 lose with ids of any spread (of 4096, 32000 rows 169, 125).
+constexpr int kVeryFew = 128 * kFewWaves;
 constexpr int kFew = 8192;
 int key_passes(int V) {  // keys 0 .. V
   int p = 1;
@@ -378,12 +470,11 @@ int key_passes(int V) {  // keys 0 .. V
   return p;
 }
 // Tokens a chunk: few tokens are better served by more waves, many by fewer parts of runs. us
-// with 8 and 32: 1000 tokens of 1000 x 2048 in 5003 rows 20, 32; 4096 x 1024, 32000 rows 46,
+// with 8 and 32: 4096 x 1024, 32000 rows 46,
 // 55; 16384 65, 69, all of one id 248, 114; 32768 x 2048, 50021 rows 169, 135.
 int embed_chunk(int T) { return T <= kFew ? 8 : 32; }
 
-// Ranked, in one launch, or sorted in two a pass? us of the whole gradient ranked and sorted: 1000
-// tokens, two passes 21, 28; 4096 46, 44; 8192 63, 50.
+// Ranked, in one launch, or sorted in two a pass? us of the whole gradient ranked and sorted: 4096 46, 44; 8192 63, 50.
 bool ranked(int T, int V) { return T <= (key_passes(V) > 2 ? 4096 : 2048); }
 int sort_per(int T) { return std::max(1, (int)(((long)T + 262143) / 262144)) * 1024; }
 int sort_blocks(int T) { return (int)(((long)T + sort_per(T) - 1) / sort_per(T)); }
@@ -437,8 +528,8 @@ int embed_lanes(int M) {
 
 }  // namespace
 
-// Rows of the table that a wave looks at for those without tokens: 1024 waves or more (1000 tokens
-// of 264, 5003 rows: 64 rows a wave 21 us, 4 15).
+// Rows of the table that a wave looks at for those without tokens: 1024 waves or more (1500 tokens
+// of 264, 5003 rows: 64 rows a wave 22 us, 4 18).
 static int embed_rows(int M, int V) {
   return std::max(4, std::min(M >= 512 ? 16 : 64, V / 1024));
 }
@@ -453,7 +544,9 @@ bool embed_fits(int T, int M, int V) {
   return (T + f - 1) / f <= kMaxBlocks && (embed_waves(T, M, V, false) + 3) / 4 <= kMaxBlocks;
 }
 
-size_t embed_ws_bytes(int T, int M, int V) { return T == 0 ? 0 : embed_ws(T, M, V).bytes; }
+size_t embed_ws_bytes(int T, int M, int V) {
+  return T <= kVeryFew ? 0 : embed_ws(T, M, V).bytes;
+}
 
 hipError_t launch_embed_fwd(int dtype, int T, int M, int V, float scale, const int32_t* ids,
                             const void* table, void* y, hipStream_t st) {
@@ -501,18 +594,38 @@ hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const i
   a.M = M;
   a.V = V;
   a.scale = scale;
-  if (T > 0) {
-    const hipError_t e = sort_tokens(T, V, ids, w, base, st);
-    if (e != hipSuccess) return e;
-    a.ids = reinterpret_cast<const int32_t*>(base + w.a);
-    a.tok = a.ids + T;
-    a.part = reinterpret_cast<float*>(base + w.part);
-  }
-  a.rows = embed_rows(M, V);
   const bool nt = (long)V * M * 4 >= (256L << 20), few = embed_chunk(T) == 8;
-  const dim3 gz((unsigned)((embed_waves(T, M, V, accumulate) + 3) / 4));
-  const dim3 gs((unsigned)((embed_waves(T, M, V, true) + 3) / 4)), b(256);
-  const dim3 g = few ? gz : gs, gj = few ? gs : gz;
+  if (T <= kVeryFew) {
+    a.ids = ids;
+    // (two blocks a token where there are columns for them: 512 tokens of 2048, 5003 rows 16, 12)
+    a.groups = M > 512 ? 2 : 1;
+    a.rows = std::max({1, std::min({512, V / 256, 8192 / M}), V >> 21});
+    const long zero = accumulate ? 0 : (V + (long)a.rows - 1) / a.rows;
+    const dim3 g((unsigned)((long)T * a.groups + zero)), b(64 * kFewWaves);
+    return traced(FLOWMOE_K_EMBED_BWD, st, [&] {
+#define FLOWMOE_EMBED_FEW(T, I)                                                               \
+  if (accumulate) hipLaunchKernelGGL((embed_few_kernel<T, I, true, false>), g, b, 0, st, a);  \
+  else if (nt) hipLaunchKernelGGL((embed_few_kernel<T, I, false, true>), g, b, 0, st, a);     \
+  else hipLaunchKernelGGL((embed_few_kernel<T, I, false, false>), g, b, 0, st, a)
+      if (T <= 64 * kFewWaves && dtype == FLOWMOE_BF16) {
+        FLOWMOE_EMBED_FEW(bf16_t, 1);
+      } else if (T <= 64 * kFewWaves) {
+        FLOWMOE_EMBED_FEW(float, 1);
+      } else if (dtype == FLOWMOE_BF16) {
+        FLOWMOE_EMBED_FEW(bf16_t, 2);
+      } else {
+        FLOWMOE_EMBED_FEW(float, 2);
+      }
+    });
+  }
+  const hipError_t se = sort_tokens(T, V, ids, w, base, st);
+  if (se != hipSuccess) return se;
+  a.ids = reinterpret_cast<const int32_t*>(base + w.a);
+  a.tok = a.ids + T;
+  a.part = reinterpret_cast<float*>(base + w.part);
+  a.rows = embed_rows(M, V);
+  const dim3 g((unsigned)((embed_waves(T, M, V, true) + 3) / 4)), b(256);
+  const dim3 gj((unsigned)((embed_waves(T, M, V, accumulate) + 3) / 4));
   const hipError_t e = traced(FLOWMOE_K_EMBED_BWD, st, [&] {
 #define FLOWMOE_EMBED_BWD(T, C)                                                                 \
   if (accumulate) hipLaunchKernelGGL((embed_bwd_kernel<T, C, true, false>), g, b, 0, st, a);    \
@@ -528,13 +641,17 @@ hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const i
       FLOWMOE_EMBED_BWD(float, 32);
     }
   });
-  if (e != hipSuccess || T <= embed_chunk(T)) return e;
+  if (e != hipSuccess) return e;
   return traced(FLOWMOE_K_EMBED_BWD, st, [&] {
-    if (few && accumulate) hipLaunchKernelGGL((embed_join_kernel<8, true, false>), gj, b, 0, st, a);
-    else if (few) hipLaunchKernelGGL((embed_join_kernel<8, false, false>), gj, b, 0, st, a);
-    else if (accumulate) hipLaunchKernelGGL((embed_join_kernel<32, true, false>), gj, b, 0, st, a);
-    else if (nt) hipLaunchKernelGGL((embed_join_kernel<32, false, true>), gj, b, 0, st, a);
-    else hipLaunchKernelGGL((embed_join_kernel<32, false, false>), gj, b, 0, st, a);
+#define FLOWMOE_EMBED_JOIN(C)                                                                \
+  if (accumulate) hipLaunchKernelGGL((embed_join_kernel<C, true, false>), gj, b, 0, st, a);  \
+  else if (nt) hipLaunchKernelGGL((embed_join_kernel<C, false, true>), gj, b, 0, st, a);     \
+  else hipLaunchKernelGGL((embed_join_kernel<C, false, false>), gj, b, 0, st, a)
+    if (few) {
+      FLOWMOE_EMBED_JOIN(8);
+    } else {
+      FLOWMOE_EMBED_JOIN(32);
+    }
   });
 }
 

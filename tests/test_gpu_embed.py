@@ -183,3 +183,58 @@ def test_deterministic_graph_and_stream():
         s.synchronize()
         assert torch.equal(c.y, o.y) and torch.equal(c.dtable, o.dtable)
         c.check_bwd()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,M,vocab", [
+    (8, 1032, 1), (9, 512, 1), (33, 4104, 2), (512, 520, 3), (512, 4104, 40000), (513, 1032, 2),
+    (1024, 8, 1), (1024, 2056, 600), (1025, 2056, 600),
+])
+def test_few_tokens(T, M, vocab, dtype):
+    """Either side of the sizes at which a wave, a block or a launch has enough tokens, with runs of
+    a few, of dozens and of all tokens, and one id before and behind them all."""
+    g = torch.Generator().manual_seed(T)
+    ids = torch.randint(0, vocab, (T,), generator=g)
+    ids[torch.rand(T, generator=g) < 0.1] = vocab // 2
+    ids[torch.rand(T, generator=g) < 0.1] = -1
+    ids[0] = ids[-1] = vocab - 1
+    c = Case(T, M, vocab, dtype, ids=ids)
+    c.bwd()
+    c.check_bwd()
+    first = c.dtable.clone()
+    c.dtable.fill_(float("nan"))
+    c.bwd()
+    assert torch.equal(first, c.dtable)
+    base = torch.randn(vocab, M, device=dev())
+    c.dtable.copy_(base)
+    c.bwd(True)
+    c.check_bwd(base)
+
+
+def test_many_rows_of_no_id_may_hold_anything():
+    c = Case(5000, 64, 20)
+    c.dy[(c.ids < 0) | (c.ids >= 20)] = float("nan")
+    c.bwd()
+    assert torch.isfinite(c.dtable).all()
+
+
+def test_few_tokens_graph_and_stream():
+    """As test_deterministic_graph_and_stream; such calls take no workspace."""
+    c = Case(700, 264, 900)
+    assert c.n == 0
+    c.bwd()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.flowmoe_embed_bwd(c.shape, c.embed, c.ids, c.dy, c.dtable, False, None, 0)
+    for i in range(3):
+        o = Case(700, 264, 900, seed=i)
+        c.ids.copy_(o.ids)
+        c.dy.copy_(o.dy)
+        graph.replay()
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream()
+        o.bwd(stream=s)
+        s.synchronize()
+        assert torch.equal(c.dtable, o.dtable)
+        c.check_bwd()

@@ -663,7 +663,9 @@ flowmoe_status_t flowmoe_diff_mha_bwd(const flowmoe_shape_t* shape,
  * h / (heads / kv_heads). bf16 only; 16-byte aligned; only shape->T, M (at most 2^21) and
  * dtype are used. heads times (T / 32 + 2 nseq + 2) stay below 2^24. A call's blocks depend on
  * its sizes, and in the backward on the lengths: the same sequence in another batch may be
- * summed in another order. */
+ * summed in another order. The kernels are chosen by T / nseq, so that sequences without tokens
+ * that fill up a list of a fixed length cost time where they are many (16 of 512 tokens: 20 % with
+ * 112 more, 16 heads of 64). */
 typedef struct {
   int32_t nseq;     /* sequences, >= 0 */
   int32_t heads;

@@ -23,6 +23,7 @@ struct EmbedArgs {
   float* dtable;
   float* part;  // the runs' parts
   int T, M, V, rows, groups;
+  int zero;  // the launch clears the rows without tokens
   float scale;
 };
 
@@ -158,35 +159,47 @@ __global__ __launch_bounds__(1024) void embed_place_kernel(SortArgs a) {
 }
 
 // Few tokens, in one launch: an item's place is the number of items that sort before it.
-// A block finds those of 64 items, a lane each; its 16 waves compare them with every 16th 64
-// of all items each.
+// A block finds those of B items, whose keys are scalars: its 16 waves compare them with every
+// 16th 64 of all items each, a vector comparison and a scalar count of its mask for 64 pairs.
+constexpr int kRankItems = 32;
 __global__ __launch_bounds__(1024) void embed_rank_kernel(const int32_t* ids, int32_t* key,
                                                           int32_t* val, int T, int V) {
-  __shared__ int part[16][64];
+  constexpr int B = kRankItems, kNone = 0x7FFFFFFE;
+  __shared__ int part[16][B];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int b0 = blockIdx.x * 64, i = b0 + lane;
+  const int b0 = blockIdx.x * B, own = b0 & ~63;
   // (an id of no row sorts as V, a place behind the items before all)
-  auto in = [&](int j) { return j < T ? (int)min((unsigned)ids[j], (unsigned)V) : 0x7FFFFFFF; };
-  const int k = in(i);
-  int n = 0;
-  for (int j = 64 * w; j < T; j += 1024) {
-    const int q = in(j + lane);
-    // (as one comparison: those before the block's sort before equal ones)
-    const int kk = j < b0 ? k : k - 1;
+  auto in = [&](int j) { return j < T ? (int)min((unsigned)ids[j], (unsigned)V) : kNone; };
+  int k[B], cnt[B];
 #pragma unroll
-    for (int u = 0; u < 64; ++u) {
-      const int o = __builtin_amdgcn_readlane(q, u);
-      n += o <= kk;
-      if (j == b0) n += o == k && u < lane;
+  for (int u = 0; u < B; ++u) {
+    k[u] = in(b0 + u);
+    cnt[u] = 0;
+  }
+  int next = in(64 * w + lane);
+  for (int j = 64 * w; j < T; j += 1024) {
+    const int q = next + (j > own ? 1 : 0);  // (equal ones behind the block sort behind it)
+    next = in(j + 1024 + lane);
+    if (j == own) {
+#pragma unroll
+      for (int u = 0; u < B; ++u)
+        cnt[u] += __popcll(__ballot(q + (j + lane >= b0 + u ? 1 : 0) <= k[u]));
+    } else {
+#pragma unroll
+      for (int u = 0; u < B; ++u) cnt[u] += __popcll(__ballot(q <= k[u]));
     }
   }
-  part[w][lane] = n;
+  int n = 0;
+#pragma unroll
+  for (int u = 0; u < B; ++u) n = lane == u ? cnt[u] : n;
+  if (lane < B) part[w][lane] = n;
   __syncthreads();
-  if (w != 0 || i >= T) return;
+  const int i = b0 + lane;
+  if (w != 0 || lane >= B || i >= T) return;
   n = 0;
 #pragma unroll
   for (int u = 0; u < 16; ++u) n += part[u][lane];
-  key[n] = k;
+  key[n] = in(i);
   val[n] = i;
 }
 
@@ -304,12 +317,22 @@ __device__ __forceinline__ void zero_absent(const EmbedArgs& a, long v0, int lan
   }
 }
 
+// Waves 0 .. chunks * slabs - 1: the chunks' sums, and in the next launch the joins. The waves behind
+// them clear the rows without tokens, in one of the two: beside the joins, whose latencies they
+// hide, where rows are wide (us beside the sums and so: 16384 tokens of one id, 32000 rows of 1024
+// 111, 104; 40000 of 2048, 50021 rows 150, 143), beside the sums where narrow ones take longer for
+// their searches than the joins (16384 of 264, 70000 rows 50, 57; of 64, 200000 48, 54).
 template <typename T, int C, bool ADD, bool NT>
 __global__ __launch_bounds__(256) void embed_bwd_kernel(EmbedArgs a) {
   const int lane = threadIdx.x & 63, slabs = (a.M + 511) / 512;
   const long u = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (u < ((long)a.T + C - 1) / C * slabs)
+  const long sums = ((long)a.T + C - 1) / C * slabs;
+  if (u < sums) {
     sum_chunk<T, C, ADD, NT>(a, (int)(u / slabs), (int)(u % slabs) * 512 + 8 * lane, lane);
+  } else if constexpr (!ADD) {
+    const long v0 = (u - sums) * a.rows;
+    if (a.zero && v0 < a.V) zero_absent<NT>(a, v0, lane);
+  }
 }
 
 // a run that crosses chunks: the wave of the chunk ch where it begins adds up its parts
@@ -345,8 +368,6 @@ __device__ __forceinline__ void join_chunk(const EmbedArgs& a, int ch, int c, in
   if (on) store8(a.dtable + (long)id * a.M + c, acc);
 }
 
-// Waves 0 .. chunks * slabs - 1 join runs; the others clear the rows without tokens, which hides
-// the joins' latencies (16384 tokens of one id, 32000 rows of 1024: 104 us, beside the sums 111).
 template <int C, bool ADD, bool NT>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a) {
   const int lane = threadIdx.x & 63, slabs = (a.M + 511) / 512;
@@ -356,7 +377,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a) {
     join_chunk<C, ADD>(a, (int)(u / slabs), (int)(u % slabs) * 512 + 8 * lane, lane);
   } else if constexpr (!ADD) {
     const long v0 = (u - sums) * a.rows;
-    if (v0 < a.V) zero_absent<NT>(a, v0, lane);
+    if (a.zero && v0 < a.V) zero_absent<NT>(a, v0, lane);
   }
 }
 
@@ -474,8 +495,10 @@ int key_passes(int V) {  // keys 0 .. V
 // 55; 16384 65, 69, all of one id 248, 114; 32768 x 2048, 50021 rows 169, 135.
 int embed_chunk(int T) { return T <= kFew ? 8 : 32; }
 
-// Ranked, in one launch, or sorted in two a pass? us of the whole gradient ranked and sorted: 4096 46, 44; 8192 63, 50.
-bool ranked(int T, int V) { return T <= (key_passes(V) > 2 ? 4096 : 2048); }
+// Ranked, in one launch, or sorted in two a pass? us of the whole gradient ranked and sorted, rows of
+// 264, two passes (5003 rows) and three (70000): 2048 tokens 18, 24 and 28, 40; 4096 22, 26 and
+// 31, 44; 8192 29, 31 and 36, 44; 12000 54, 38 and 68, 58. One pass is half of two's.
+bool ranked(int T, int V) { return T <= (key_passes(V) > 1 ? 8192 : 2048); }
 int sort_per(int T) { return std::max(1, (int)(((long)T + 262143) / 262144)) * 1024; }
 int sort_blocks(int T) { return (int)(((long)T + sort_per(T) - 1) / sort_per(T)); }
 
@@ -499,7 +522,7 @@ hipError_t sort_tokens(int T, int V, const int32_t* ids, const EmbedWs& w, char*
   int32_t* y = reinterpret_cast<int32_t*>(ws + w.a);
   if (ranked(T, V))
     return traced(FLOWMOE_K_EMBED_SORT, st, [&] {
-      hipLaunchKernelGGL(embed_rank_kernel, dim3((T + 63) / 64), dim3(1024), 0, st, ids, y, y + T, T, V);
+      hipLaunchKernelGGL(embed_rank_kernel, dim3((T + kRankItems - 1) / kRankItems), dim3(1024), 0, st, ids, y, y + T, T, V);
     });
   SortArgs a = {ids, nullptr, nullptr, nullptr, reinterpret_cast<int32_t*>(ws + w.hist), T, V,
                 sort_per(T), 0};
@@ -624,8 +647,10 @@ hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const i
   a.tok = a.ids + T;
   a.part = reinterpret_cast<float*>(base + w.part);
   a.rows = embed_rows(M, V);
-  const dim3 g((unsigned)((embed_waves(T, M, V, true) + 3) / 4)), b(256);
-  const dim3 gj((unsigned)((embed_waves(T, M, V, accumulate) + 3) / 4));
+  const bool late = M >= 512;  // (clearing beside the joins)
+  const dim3 g((unsigned)((embed_waves(T, M, V, accumulate || late) + 3) / 4)), b(256);
+  const dim3 gj((unsigned)((embed_waves(T, M, V, accumulate || !late) + 3) / 4));
+  a.zero = !late;
   const hipError_t e = traced(FLOWMOE_K_EMBED_BWD, st, [&] {
 #define FLOWMOE_EMBED_BWD(T, C)                                                                 \
   if (accumulate) hipLaunchKernelGGL((embed_bwd_kernel<T, C, true, false>), g, b, 0, st, a);    \
@@ -642,6 +667,7 @@ hipError_t launch_embed_bwd(int dtype, int T, int M, int V, float scale, const i
     }
   });
   if (e != hipSuccess) return e;
+  a.zero = late;
   return traced(FLOWMOE_K_EMBED_BWD, st, [&] {
 #define FLOWMOE_EMBED_JOIN(C)                                                                \
   if (accumulate) hipLaunchKernelGGL((embed_join_kernel<C, true, false>), gj, b, 0, st, a);  \

@@ -238,3 +238,22 @@ def test_few_tokens_graph_and_stream():
         s.synchronize()
         assert torch.equal(c.dtable, o.dtable)
         c.check_bwd()
+
+
+@pytest.mark.parametrize("T,M,vocab", [
+    (1025, 520, 3), (2047, 8, 200), (2049, 8, 255), (3000, 72, 70000), (8191, 8, 40), (8192, 512, 300),
+    (8193, 512, 300), (8193, 504, 70000), (8192, 8, 1 << 17),
+])
+def test_ranked_and_sorted(T, M, vocab):
+    """Either side of the sizes at which ids are ranked or sorted and rows are wide or narrow."""
+    c = Case(T, M, vocab, "f32" if T % 2 else "bf16")
+    c.bwd()
+    c.check_bwd()
+    first = c.dtable.clone()
+    c.dtable.fill_(float("nan"))
+    c.bwd()
+    assert torch.equal(first, c.dtable)
+    base = torch.randn(vocab, M, device=dev())
+    c.dtable.copy_(base)
+    c.bwd(True)
+    c.check_bwd(base)

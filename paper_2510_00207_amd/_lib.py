@@ -551,9 +551,15 @@ def kind_mask(names) -> int:
 
 
 def flowmoe_trace_start(events, kinds, pairs: int, mask: int):
-    """events: ctypes array of 2*pairs hipEvent_t; kinds: ctypes int32 array."""
+    """events: ctypes array of 2*pairs hipEvent_t; kinds: ctypes int32 array.
+
+    A mask that names kinds past 31 beside some of the first 32 (kind_mask(K_NAMES), -1 or another
+    complement) goes to flowmoe_trace_start64, so that none is cut off."""
     if mask >> 32:
-        raise ValueError("the mask names kinds past 31: flowmoe_trace_start64 takes them")
+        if not mask & 0xFFFFFFFF:
+            raise ValueError("the mask names kinds past 31 alone: flowmoe_trace_start64 takes them")
+        flowmoe_trace_start64(events, kinds, pairs, mask)
+        return
     _check(load().flowmoe_trace_start(ctypes.cast(events, ctypes.c_void_p),
                                       ctypes.cast(kinds, ctypes.c_void_p), pairs, mask))
 

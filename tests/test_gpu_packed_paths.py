@@ -74,3 +74,18 @@ def test_long_among_empty_and_tiny(lens, D):
         c.check_fwd()
         assert launches(c.bwd) == SHORT
         c.check_bwd()
+
+
+@pytest.mark.parametrize("lens,heads,kv,D,causal", [
+    ([8200], 16, 16, 128, True), ([4000] + [200] * 21, 32, 16, 128, False),
+    ([4000] + [150] * 28, 32, 32, 64, True),
+])
+def test_join_of_two_units(lens, heads, kv, D, causal):
+    """So many rows that a tile is cut in two at most."""
+    c = Case(lens, heads, kv, D, causal)
+    rows32 = c.T // 32 + len(lens) + 1
+    assert c.n == 2 * rows32 * kv * 64 * D * 4
+    c.fwd()
+    c.check_fwd()
+    assert launches(c.bwd) == JOINED
+    c.check_bwd()

@@ -89,3 +89,48 @@ def test_join_of_two_units(lens, heads, kv, D, causal):
     c.check_fwd()
     assert launches(c.bwd) == JOINED
     c.check_bwd()
+
+
+# (lens, heads, kv, D, causal): waves of short sequences; blocks of uncut tiles; blocks of two
+# groups of waves forward, and cut tiles; one group and cut tiles
+PATHS = [([20, 3, 0, 41, 9], 8, 2, 128, True), ([20, 3, 0, 41, 9], 6, 2, 64, False),
+         ([100, 140], 2, 2, 64, True), ([2100], 4, 2, 128, True), ([1200, 300], 4, 1, 64, False),
+         ([700, 20, 300], 4, 2, 64, True), ([700, 20, 300], 8, 2, 128, False)]
+
+
+@pytest.mark.parametrize("lens,heads,kv,D,causal", PATHS)
+def test_repeats_on_another_stream(lens, heads, kv, D, causal):
+    """The same bits from buffers that held none of them, scratch included."""
+    c = Case(lens, heads, kv, D, causal, 11)
+    c.fwd()
+    c.bwd()
+    want = [getattr(c, n).clone() for n in OUT]
+    for n in OUT:
+        getattr(c, n).fill_(NAN)
+    c.ws.fill_(255)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    c.fwd(s)
+    c.bwd(s)
+    s.synchronize()
+    # (delta: intermediate, but every row of it is written)
+    for n, w in zip(OUT, want):
+        assert torch.isfinite(w).all() and torch.equal(getattr(c, n), w), n
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_gradient_of_equal_lengths(causal, D):
+    """Sequences of one length and heads of their own: flowmoe_attention_bwd's gradient, each
+    within its tolerance of the definition."""
+    c = Case([256] * 4, 4, 4, D, causal, poison=False)
+    c.fwd()
+    c.bwd()
+    c.check_bwd()
+    d_qkv, delta = torch.full_like(c.d_qkv, NAN), torch.full_like(c.delta, NAN)
+    L.flowmoe_attention_bwd(c.shape, L.make_mha_shape(256, 4, D, causal), c.qkv, c.attn, c.lse, c.d_attn,
+                            d_qkv, delta)
+    d, rnd, mag = R.attention_bwd(c.qkv, c.lens, 4, 4, D, causal, c.attn, c.lse, c.d_attn)
+    tol = HALF * rnd + 2.0 ** -10 * mag + HALF * d.abs()
+    within(d_qkv, d, tol)
+    within(d_qkv, c.d_qkv.double(), 2 * tol)

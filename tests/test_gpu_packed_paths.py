@@ -134,3 +134,25 @@ def test_gradient_of_equal_lengths(causal, D):
     tol = HALF * rnd + 2.0 ** -10 * mag + HALF * d.abs()
     within(d_qkv, d, tol)
     within(d_qkv, c.d_qkv.double(), 2 * tol)
+
+
+@pytest.mark.parametrize("lens,heads,kv,D,causal", PATHS)
+def test_starts_out_of_order_on_every_path(lens, heads, kv, D, causal):
+    """Starts that are no list of starts: every buffer's surroundings stay as they are, the
+    scratch's too."""
+    c = Case(lens, heads, kv, D, causal, poison=False)
+    T, n, guard = c.T, len(lens), {}
+    for name in OUT + ("ws",):
+        t = getattr(c, name)
+        fill = 7 if name == "ws" else 7.0
+        guard[name] = torch.full((t.numel() + 4096,), fill, dtype=t.dtype, device=dev())
+        setattr(c, name, guard[name][2048:2048 + t.numel()].view(t.shape))
+    up = lambda *s: (list(s) * (n + 1))[:n + 1]
+    for s in (up(T, 0), up(5, -3, 1 << 30, T), up(0, T, T // 3), up(-1), up(T - 1, T // 2, 1),
+              [T - i * (T // (n + 1)) for i in range(n + 1)]):
+        c.starts = torch.tensor(s, dtype=torch.int32, device=dev())
+        c.fwd()
+        c.bwd()
+        torch.cuda.synchronize()
+        for name, g in guard.items():
+            assert (g[:2048] == 7).all() and (g[-2048:] == 7).all(), (name, s)

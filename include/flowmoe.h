@@ -663,9 +663,17 @@ flowmoe_status_t flowmoe_diff_mha_bwd(const flowmoe_shape_t* shape,
  * h / (heads / kv_heads). bf16 only; 16-byte aligned; only shape->T, M (at most 2^21) and
  * dtype are used. heads times (T / 32 + 2 nseq + 2) stay below 2^24. A call's blocks depend on
  * its sizes, and in the backward on the lengths: the same sequence in another batch may be
- * summed in another order. The kernels are chosen by T / nseq, so that sequences without tokens
- * that fill up a list of a fixed length cost time where they are many (16 of 512 tokens: 20 % with
- * 112 more, 16 heads of 64). */
+ * summed in another order.
+ *
+ * The kernels are chosen by T / nseq, which counts rows behind the last sequence and entries without
+ * tokens as well: where T <= 96 nseq forward and T <= 48 nseq backward (24 nseq with more than two
+ * query heads a key head) those for short sequences run, which take long over a long one, in the
+ * backward in proportion to the heads of a group. So a few long sequences in a list that is filled up to a fixed
+ * length, or among tiny ones, run up to 2 times longer forward and 8 times backward. us without the
+ * others, and with: 2 of 2048, 254 empty, 32 heads on 8 of 128 forward 84, 112, backward 302, 772;
+ * 16 on 2 179, 1268 backward; 8 on 4 of 64 25, 45 and 72, 227; one of 4000, 250 of 5, 32 on 8 of 128
+ * 147, 194 and 503, 1428; 16384 tokens in 12 of 46 to 8021, 1012 empty 655, 903 and 2213, 5853. Lists
+ * of fixed lengths are best kept below T / 96 entries. */
 typedef struct {
   int32_t nseq;     /* sequences, >= 0 */
   int32_t heads;

@@ -1151,9 +1151,10 @@ unsigned packed_blocks(const AttnArgs& a, int rows, int per) {
   return (unsigned)((a.T / rows + a.nseq + 1) * (long)per);
 }
 
-// The most units of a tile: as many as leave the units' sums at 128 MB or so in all; few rows
-// are cut the most. None where no tile has the steps, or so many sequences that a block's
-// sum over them would take as long as it saves.
+// The most units of a tile: as many as bring the units' sums to 256 MiB (K and V in float: 8 D bytes
+// a row and unit), rounded up, so that they are below 512; few rows are cut the most. None where no
+// tile has the steps, or so many sequences that a block's sum over them would take as long as it
+// saves.
 void packed_units(const PackedShape& m, int T, AttnArgs& a) {
   const long rows32 = T / 32 + (long)m.nseq + 1, steps = (T + 31) / 32 * (m.heads / m.kv);
   const long most = (262144L * 128 / m.D + rows32 * 32 * m.kv - 1) / (rows32 * 32 * m.kv);

@@ -747,7 +747,7 @@ typedef struct {
 
 /* In the place of flowmoe_mha_fwd: qkv = in [W^Q | W^K | W^V], Q and K turned by their
  * positions (rope: heads = packed's heads + kv_heads of head_dim columns, at most the
- * tokens of flowmoe_rope_fwd; its seq_len is not used; null: not turned), the attention over
+ * tokens of flowmoe_rope_fwd; its seq_len, at least 1, is not used; null: not turned), the attention over
  * the packed sequences, out = attn W^O. bf16 only. Rows of no sequence are zeros in out
  * and in the backward's d_in, and add nothing to a gradient; unlike the attention's own they
  * have to be finite in `in` and d_out, as the products of dw_qkv and dw_o multiply them by

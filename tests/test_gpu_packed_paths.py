@@ -156,3 +156,67 @@ def test_starts_out_of_order_on_every_path(lens, heads, kv, D, causal):
         torch.cuda.synchronize()
         for name, g in guard.items():
             assert (g[:2048] == 7).all() and (g[-2048:] == 7).all(), (name, s)
+
+
+def test_one_document_of_100003_tokens():
+    """The last rows of the forward and of dQ, the first keys' gradients. A sum over n rows in 32 bits
+    is off by n 2^-24 of its terms' magnitudes beside the other tolerances."""
+    n, D, rows = 100003, 128, 96
+    c = Case([n], 2, 1, D, True, 5)
+    assert launches(c.fwd) == ["attn_fwd"] and launches(c.bwd) == JOINED
+    x, s24, rs = c.qkv[:n].double(), n * 2.0 ** -24, D ** -0.5
+    k, v = x[:, 2 * D:3 * D], x[:, 3 * D:]
+    late = torch.arange(n - rows, n, device=dev())
+    hidden = torch.arange(n, device=dev())[None] > late[:, None]
+    dk, dv, rk, rv, mk, mv = (torch.zeros(rows, D, dtype=torch.float64, device=dev()) for _ in range(6))
+    for h in range(2):
+        q, o, do = (t[:, h * D:h * D + D] for t in (x, c.attn[:n].double(), c.d_attn[:n].double()))
+        s = (q[late] @ k.T * rs).masked_fill(hidden, -float("inf"))
+        p, lse = torch.softmax(s, 1), torch.logsumexp(s, 1)
+        within(c.attn[late, h * D:h * D + D], p @ v,
+               (HALF + 2.0 ** -12 + s24) * (p @ v.abs()) + HALF * (p @ v).abs())
+        smax = float((q[late].abs() @ k.abs().T).max()) * rs
+        within(c.lse[h, late], lse, D * 2.0 ** -24 * smax + 2.0 ** -20 + s24 + 2.0 ** -22 * lse.abs())
+        delta, dmag = (do * o).sum(1), (do * o).abs().sum(1)
+        p = torch.exp(s - c.lse[h, late].double()[:, None])
+        ds = p * (do[late] @ v.T - delta[late, None])
+        mag = p * (do[late].abs() @ v.abs().T + dmag[late, None])
+        dq = ds @ k * rs
+        within(c.d_qkv[late, h * D:h * D + D], dq, HALF * (ds.abs() @ k.abs() * rs) +
+               (2.0 ** -10 + s24) * (mag @ k.abs() * rs) + HALF * dq.abs())
+        # the first keys, seen by every query from their own on
+        s = q @ k[:rows].T * rs
+        s = s.masked_fill(torch.arange(rows, device=dev())[None] > torch.arange(n, device=dev())[:, None],
+                          -float("inf"))
+        p = torch.exp(s - c.lse[h, :n].double()[:, None])
+        ds = p * (do @ v[:rows].T - delta[:, None])
+        mag = p * (do.abs() @ v[:rows].abs().T + dmag[:, None])
+        dk += ds.T @ q * rs
+        rk += ds.abs().T @ q.abs() * rs
+        mk += mag.T @ q.abs() * rs
+        dv += p.T @ do
+        rv += p.T @ do.abs()
+        mv += p.T @ do.abs()
+    for got, d, r, m in ((c.d_qkv[:rows, 2 * D:3 * D], dk, rk, mk), (c.d_qkv[:rows, 3 * D:], dv, rv, mv)):
+        within(got, d, HALF * r + (2.0 ** -10 + 2 * s24) * m + HALF * d.abs())
+    for t in (c.attn, c.d_qkv):
+        assert not t[n:].any()
+
+
+@pytest.mark.parametrize("size,path", [(100, BLOCKS), (5, SHORT)])
+def test_more_sequences_than_units_are_made_for(size, path):
+    """4101 sequences: a block's search takes three steps, no tile is cut."""
+    lens = [size] * 4100 + [700]
+    c = Case(lens, 2, 1, 64, True, 40)
+    c.fwd()
+    assert c.n == 0 and launches(c.bwd) == path
+    for lo, hi, part in ((0, 2 * size, [size] * 2), (64 * size, 65 * size, [size]),
+                         (c.live - 700 - size, c.live, [size, 700])):
+        a = (part, 2, 1, 64, True)
+        ref, lse, mag, smax = R.attention(c.qkv[lo:hi], *a)
+        within(c.attn[lo:hi], ref, (HALF + 2.0 ** -12) * mag + HALF * ref.abs())
+        within(c.lse[:, lo:hi], lse, 64 * 2.0 ** -24 * smax + 2.0 ** -20 + 2.0 ** -22 * lse.abs())
+        d, rnd, mag = R.attention_bwd(c.qkv[lo:hi], *a, c.attn[lo:hi], c.lse[:, lo:hi], c.d_attn[lo:hi])
+        within(c.d_qkv[lo:hi], d, HALF * rnd + 2.0 ** -10 * mag + HALF * d.abs())
+    for t in (c.attn, c.d_qkv):
+        assert not t[c.live:].any()
